@@ -373,6 +373,169 @@ fno_status fno_block_epilogue_bwd_data(const fno_block_desc *desc, const void *g
                                        const void *w_skip, const void *gx_spec,
                                        const void *g_out, void *gx, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Group norm with an activation, for the blocks' outputs (z of the epilogue
+ * with act NONE, or any activation tensor of a model around the layers):
+ *
+ *     xh = (x - mean) / sqrt(var + eps),  out = act(gamma xh + beta) (+ residual)
+ *
+ * mean and var (the population variance) over all points of the channels of
+ * one group of one sample: groups equal consecutive sets of channels / groups
+ * channels (groups = channels normalises every plane by itself, groups = 1 a
+ * whole sample).
+ *
+ * Tensors x, residual, out, g_out, gx are of one element type (fno_dtype) and
+ * one layout: CHANNELS_FIRST [batch][channels][points], the layout of the
+ * spectral convolution's tensors, or CHANNELS_LAST [batch][points][channels].
+ * gamma, beta [channels] and their gradients are fp32, and so are the
+ * statistics [batch][groups][2] = (mean, 1 / sqrt(var + eps)).  Sums are
+ * formed in at least fp32, the statistics joined in double, results rounded
+ * once.  Every sum has a fixed order: results are bit-identical from run to
+ * run.  A group that holds a non-finite value gives NaN throughout.
+ * ------------------------------------------------------------------------ */
+typedef enum { FNO_DTYPE_F32 = 0, FNO_DTYPE_F16 = 1, FNO_DTYPE_BF16 = 2 } fno_dtype;
+
+typedef enum { FNO_LAYOUT_CHANNELS_FIRST = 0, FNO_LAYOUT_CHANNELS_LAST = 1 } fno_layout;
+
+typedef enum {
+  FNO_NORM_ACT_NONE = 0,
+  FNO_NORM_ACT_GELU = 1,  /* z Phi(z), Phi the exact normal distribution function */
+  FNO_NORM_ACT_SILU = 2   /* z / (1 + exp(-z)) */
+} fno_norm_activation;
+
+typedef struct {
+  int32_t dtype;       /* fno_dtype of the tensors */
+  int32_t layout;      /* fno_layout */
+  int32_t activation;  /* fno_norm_activation */
+  float eps;           /* >= 0, finite */
+  int64_t batch, points, channels;
+  int64_t groups;      /* divides channels */
+} fno_norm_desc;
+
+/* Workspace bytes of a call, FNO_OP_FWD or FNO_OP_BWD (>= 256).
+ * FNO_ERR_INVALID_ARGUMENT for a malformed descriptor (extents of at least 1,
+ * channels up to 65536, batch x points x channels up to 2^38) or another op. */
+fno_status fno_group_norm_act_workspace_size(const fno_norm_desc *desc, fno_op op,
+                                             size_t *bytes);
+
+/* Forward.  gamma and beta may be null (1 and 0), residual too (none added).
+ * stats, if not null, receives the statistics that the backward takes (null
+ * for inference).  out may be the same buffer as x or residual (in place). */
+fno_status fno_group_norm_act_fwd(const fno_norm_desc *desc, const void *x,
+                                  const float *gamma, const float *beta, const void *residual,
+                                  void *out, float *stats, void *ws, size_t ws_len,
+                                  hipStream_t stream);
+
+/* Backward, from the forward's x, gamma, beta and stats and the output's
+ * gradient: gx, and the parameter gradients g_gamma, g_beta (each may be null;
+ * overwritten, not accumulated).  The residual's gradient is g_out itself.
+ * gx may be the same buffer as g_out or x. */
+fno_status fno_group_norm_act_bwd(const fno_norm_desc *desc, const void *x,
+                                  const float *gamma, const float *beta, const float *stats,
+                                  const void *g_out, void *gx, float *g_gamma, float *g_beta,
+                                  void *ws, size_t ws_len, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The optimizer step over all tensors of a model at once: AdamW (Adam with
+ * decoupled weight decay), element by element
+ *
+ *     g = grad s;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
+ *     p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
+ *
+ * in fp32, t the step's number (from 1).  Complex weights are their
+ * interleaved (re, im) pairs, each a parameter of its own.  A list holds any
+ * number of tensors of any sizes and types; one launch takes up to
+ * FNO_ADAMW_LAUNCH_TENSORS of them.
+ *
+ * Parameters are fp32, or of a 16-bit type; then `master`, if not null, holds
+ * the fp32 values that the step works on and `param` receives them rounded
+ * (without a master the step works on the 16-bit values themselves, and
+ * updates below half their last place are lost).  Gradients are fp32 (as the
+ * weight gradients of this library are) or of the parameter's type.
+ *
+ * Moments take 32 bits each (exp_avg = m, exp_avg_sq = v, fp32 [n]) or 8 bits:
+ * codes [n] with one fp32 scale per FNO_ADAMW_BLOCK consecutive elements of
+ * the tensor (the last block may be short),
+ *     m       = (A / 127^2) q |q|  int8 q,   A = max |m| of the block
+ *     sqrt(v) = (B / 255^2) q^2    uint8 q,  B = max sqrt(v) of the block
+ * rounded to nearest in the square root of the value, with q >= 1 wherever
+ * v > 0: a second moment that is not zero does not become zero, so that the
+ * next step's quotient stays bounded.  The step itself uses the new moments
+ * before they are rounded.  A block that holds a non-finite moment stands for
+ * non-finite values throughout.
+ *
+ * An element's update has one fixed order of rounded operations and no sum
+ * over other elements (8-bit blocks: a maximum), so it does not depend on how
+ * a list is split.  Tensors of a list must not overlap.
+ * ------------------------------------------------------------------------ */
+#define FNO_ADAMW_BLOCK 256
+#define FNO_ADAMW_LAUNCH_TENSORS 40
+
+typedef struct {
+  void *param;              /* [n] of param_dtype */
+  float *master;            /* [n], or null; null where param_dtype is F32 */
+  const void *grad;         /* [n] of grad_dtype */
+  void *exp_avg;            /* [n] fp32, or int8 codes */
+  void *exp_avg_sq;         /* [n] fp32, or uint8 codes */
+  float *exp_avg_scale;     /* 8-bit states: [ceil(n / 256)], else null */
+  float *exp_avg_sq_scale;  /* 8-bit states: [ceil(n / 256)], else null */
+  int64_t n;                /* elements, 0 .. 2^34 (0: nothing is read or written) */
+  int32_t param_dtype;      /* fno_dtype */
+  int32_t grad_dtype;       /* FNO_DTYPE_F32 or param_dtype */
+  int32_t state_bits;       /* 32 or 8 */
+  float weight_decay;       /* >= 0, finite */
+} fno_adamw_tensor;
+
+typedef struct {
+  double lr;          /* >= 0, finite */
+  double beta1;       /* [0, 1) */
+  double beta2;       /* [0, 1) */
+  double eps;         /* >= 0, finite */
+} fno_adamw_desc;
+
+/* What steps of one optimizer share on the device, for training without a
+ * host read between backward and update, and under HIP graph capture: 32
+ * bytes of device memory, zeroed by the caller before first use except for
+ * lr_factor = 1.  fno_grad_norm writes all but lr_factor. */
+typedef struct {
+  int64_t step;       /* steps taken */
+  int64_t skipped;    /* steps left out for non-finite gradients */
+  float grad_norm;    /* L2 norm of the unscaled gradients of the last call */
+  float grad_scale;   /* what the step multiplies gradients with */
+  int32_t skip;       /* 1: the last gradients were not finite */
+  float lr_factor;    /* multiplies lr (the caller's: a schedule under replay) */
+} fno_adamw_control;
+
+/* The global gradient norm with clip, loss-scale removal and non-finite check:
+ * over all gradients of the list (read only; the other pointers are ignored),
+ *     grad_norm  = inv_loss_scale sqrt(sum grad^2)      (sum in double)
+ *     grad_scale = inv_loss_scale min(1, max_norm / grad_norm)
+ * into `control`, and step += 1; where the sum is not finite instead skip = 1
+ * and skipped += 1, and the fno_adamw_step that follows changes nothing.
+ * max_norm > 0 (INFINITY: no clip), inv_loss_scale > 0 and finite.  The sum
+ * has a fixed order: bit-identical from run to run. */
+fno_status fno_grad_norm_workspace_size(const fno_adamw_tensor *tensors, int64_t count,
+                                        size_t *bytes);
+fno_status fno_grad_norm(const fno_adamw_tensor *tensors, int64_t count, double max_norm,
+                         double inv_loss_scale, fno_adamw_control *control, void *ws,
+                         size_t ws_len, hipStream_t stream);
+
+/* One step.  control null: step number `step` (>= 1) with gradients as they
+ * are (s = 1).  control (device memory) not null: the step number, s and skip
+ * that fno_grad_norm left there; `step` is ignored.  `tensors` is read during
+ * the call only.  count 0 does nothing. */
+fno_status fno_adamw_step(const fno_adamw_desc *desc, const fno_adamw_tensor *tensors,
+                          int64_t count, int64_t step, const fno_adamw_control *control,
+                          hipStream_t stream);
+
+/* Reads 8-bit moments out as the values they stand for, of element type
+ * `dtype`: exp_avg_out[i], exp_avg_sq_out[i] (arrays of device pointers, [n]
+ * each) for tensor i of the list (for checkpoints, or to go on with 32-bit
+ * states).  Entries with 32-bit states are FNO_ERR_INVALID_ARGUMENT. */
+fno_status fno_adamw_moments(const fno_adamw_tensor *tensors, int64_t count, fno_dtype dtype,
+                             void *const *exp_avg_out, void *const *exp_avg_sq_out,
+                             hipStream_t stream);
+
 /* Per-kernel timing with HIP events (a profiling aid, off by default).
  * While enabled, every kernel the library launches is bracketed by a pair of
  * HIP events recorded on the launch stream (events are created per launch, so

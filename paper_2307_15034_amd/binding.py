@@ -84,6 +84,70 @@ class FnoBlockDesc(ctypes.Structure):
     ]
 
 
+FNO_DTYPE_F32 = 0
+FNO_DTYPE_F16 = 1
+FNO_DTYPE_BF16 = 2
+FNO_LAYOUT_CHANNELS_FIRST = 0
+FNO_LAYOUT_CHANNELS_LAST = 1
+FNO_NORM_ACT_NONE = 0
+FNO_NORM_ACT_GELU = 1
+FNO_NORM_ACT_SILU = 2
+
+
+class FnoNormDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("batch", ctypes.c_int64),
+        ("points", ctypes.c_int64),
+        ("channels", ctypes.c_int64),
+        ("groups", ctypes.c_int64),
+    ]
+
+
+FNO_ADAMW_BLOCK = 256
+
+
+class FnoAdamwTensor(ctypes.Structure):
+    _fields_ = [
+        ("param", ctypes.c_void_p),
+        ("master", ctypes.c_void_p),
+        ("grad", ctypes.c_void_p),
+        ("exp_avg", ctypes.c_void_p),
+        ("exp_avg_sq", ctypes.c_void_p),
+        ("exp_avg_scale", ctypes.c_void_p),
+        ("exp_avg_sq_scale", ctypes.c_void_p),
+        ("n", ctypes.c_int64),
+        ("param_dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("state_bits", ctypes.c_int32),
+        ("weight_decay", ctypes.c_float),
+    ]
+
+
+class FnoAdamwDesc(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+    ]
+
+
+class FnoAdamwControl(ctypes.Structure):
+    """Layout of the control block (device memory)."""
+    _fields_ = [
+        ("step", ctypes.c_int64),
+        ("skipped", ctypes.c_int64),
+        ("grad_norm", ctypes.c_float),
+        ("grad_scale", ctypes.c_float),
+        ("skip", ctypes.c_int32),
+        ("lr_factor", ctypes.c_float),
+    ]
+
+
 class FnoWeights(ctypes.Structure):
     _fields_ = [
         ("dense", ctypes.c_void_p),
@@ -116,6 +180,8 @@ def _load() -> ctypes.CDLL:
     D = P(FnoConvDesc)
     vp, sz, i32, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
     BD = P(FnoBlockDesc)
+    ND = P(FnoNormDesc)
+    AT, f64 = P(FnoAdamwTensor), ctypes.c_double
     sig = {
         "fno_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "fno_last_error": (ctypes.c_char_p, []),
@@ -140,6 +206,14 @@ def _load() -> ctypes.CDLL:
         "fno_block_epilogue_bwd_weight": (ctypes.c_int,
                                           [BD, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "fno_block_epilogue_bwd_data": (ctypes.c_int, [BD, vp, vp, vp, vp, vp, vp]),
+        "fno_group_norm_act_workspace_size": (ctypes.c_int, [ND, ctypes.c_int, P(sz)]),
+        "fno_group_norm_act_fwd": (ctypes.c_int, [ND, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "fno_group_norm_act_bwd": (ctypes.c_int,
+                                   [ND, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "fno_grad_norm_workspace_size": (ctypes.c_int, [AT, i64, P(sz)]),
+        "fno_grad_norm": (ctypes.c_int, [AT, i64, f64, f64, vp, vp, sz, vp]),
+        "fno_adamw_step": (ctypes.c_int, [P(FnoAdamwDesc), AT, i64, i64, vp, vp]),
+        "fno_adamw_moments": (ctypes.c_int, [AT, i64, ctypes.c_int, P(vp), P(vp), vp]),
         "fno_release_caches": (ctypes.c_int, []),
         "fno_profile_enable": (ctypes.c_int, [i32]),
         "fno_profile_reset": (ctypes.c_int, []),
@@ -165,6 +239,8 @@ EXPORTED = [
     "fno_profile_enable", "fno_profile_reset", "fno_profile_read",
     "fno_block_epilogue_workspace_size", "fno_block_epilogue_fwd",
     "fno_block_epilogue_bwd_weight", "fno_block_epilogue_bwd_data",
+    "fno_group_norm_act_workspace_size", "fno_group_norm_act_fwd", "fno_group_norm_act_bwd",
+    "fno_grad_norm_workspace_size", "fno_grad_norm", "fno_adamw_step", "fno_adamw_moments",
 ]
 
 
@@ -361,6 +437,80 @@ def fno_block_epilogue_bwd_data(desc, g_z: int, w_skip: int, gx_spec: int, g_out
                                           stream or None)
     if check:
         _check(st, "fno_block_epilogue_bwd_data")
+    return st
+
+
+def make_norm_desc(batch: int, points: int, channels: int, groups: int,
+                   dtype: int = FNO_DTYPE_F16, layout: int = FNO_LAYOUT_CHANNELS_FIRST,
+                   activation: int = FNO_NORM_ACT_GELU, eps: float = 1e-5) -> FnoNormDesc:
+    d = FnoNormDesc()
+    d.dtype, d.layout, d.activation, d.eps = dtype, layout, activation, eps
+    d.batch, d.points, d.channels, d.groups = batch, points, channels, groups
+    return d
+
+
+def fno_group_norm_act_workspace_size(desc: FnoNormDesc, op: int) -> int:
+    b = ctypes.c_size_t()
+    _check(_lib.fno_group_norm_act_workspace_size(ctypes.byref(desc), op, ctypes.byref(b)),
+           "fno_group_norm_act_workspace_size")
+    return b.value
+
+
+def fno_group_norm_act_fwd(desc, x: int, gamma: int, beta: int, residual: int, out: int,
+                           stats: int, ws: int, ws_bytes: int, stream: int,
+                           check: bool = True) -> int:
+    st = _lib.fno_group_norm_act_fwd(ctypes.byref(desc), x or None, gamma or None, beta or None,
+                                     residual or None, out or None, stats or None, ws or None,
+                                     ws_bytes, stream or None)
+    if check:
+        _check(st, "fno_group_norm_act_fwd")
+    return st
+
+
+def fno_group_norm_act_bwd(desc, x: int, gamma: int, beta: int, stats: int, g_out: int, gx: int,
+                           g_gamma: int, g_beta: int, ws: int, ws_bytes: int, stream: int,
+                           check: bool = True) -> int:
+    st = _lib.fno_group_norm_act_bwd(ctypes.byref(desc), x or None, gamma or None, beta or None,
+                                     stats or None, g_out or None, gx or None, g_gamma or None,
+                                     g_beta or None, ws or None, ws_bytes, stream or None)
+    if check:
+        _check(st, "fno_group_norm_act_bwd")
+    return st
+
+
+def fno_grad_norm_workspace_size(tensors, count: int) -> int:
+    """`tensors`: a ctypes array of FnoAdamwTensor (here and below)."""
+    b = ctypes.c_size_t()
+    _check(_lib.fno_grad_norm_workspace_size(tensors, count, ctypes.byref(b)),
+           "fno_grad_norm_workspace_size")
+    return b.value
+
+
+def fno_grad_norm(tensors, count: int, max_norm: float, inv_loss_scale: float, control: int,
+                  ws: int, ws_bytes: int, stream: int, check: bool = True) -> int:
+    st = _lib.fno_grad_norm(tensors, count, max_norm, inv_loss_scale, control or None, ws or None,
+                            ws_bytes, stream or None)
+    if check:
+        _check(st, "fno_grad_norm")
+    return st
+
+
+def fno_adamw_step(desc, tensors, count: int, step: int, control: int, stream: int,
+                   check: bool = True) -> int:
+    st = _lib.fno_adamw_step(ctypes.byref(desc), tensors, count, step, control or None,
+                             stream or None)
+    if check:
+        _check(st, "fno_adamw_step")
+    return st
+
+
+def fno_adamw_moments(tensors, count: int, dtype: int, exp_avg_out, exp_avg_sq_out, stream: int,
+                      check: bool = True) -> int:
+    """The outputs: ctypes arrays of device addresses."""
+    st = _lib.fno_adamw_moments(tensors, count, dtype, exp_avg_out, exp_avg_sq_out,
+                                stream or None)
+    if check:
+        _check(st, "fno_adamw_moments")
     return st
 
 

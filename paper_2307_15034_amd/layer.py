@@ -311,3 +311,122 @@ class BlockEpilogue:
         s = torch.cuda.current_stream().cuda_stream if stream is None else stream
         B.fno_block_epilogue_bwd_data(self.desc, agz, aw, ags, ago, agx, s)
         return gx
+
+
+DTYPE_CODES = {torch.float32: B.FNO_DTYPE_F32, torch.float16: B.FNO_DTYPE_F16,
+               torch.bfloat16: B.FNO_DTYPE_BF16}
+
+
+def _stream_of(device: torch.device, stream: Optional[int]) -> int:
+    """The stream a call runs on: `stream`, or torch's current one on
+    `device`, which has to be the current device (the library launches
+    there)."""
+    if device.index is not None and device.index != torch.cuda.current_device():
+        raise ValueError(f"the current device is cuda:{torch.cuda.current_device()}, the tensors "
+                         f"live on {device}")
+    return torch.cuda.current_stream().cuda_stream if stream is None else stream
+
+
+class GroupNormAct:
+    """Group norm with an activation (the fno_group_norm_act_* calls):
+    out = act(gamma (x - mean) / sqrt(var + eps) + beta) (+ residual).
+
+    x, residual, out and the gradients g_out, gx are [batch, channels, *grid],
+    or [batch, *grid, channels] with channels_last, of `dtype` (float32,
+    float16 or bfloat16); gamma, beta [channels] and their gradients float32
+    (gamma None: ones, beta None: zeros); stats [batch, groups, 2] float32,
+    (mean, 1 / sqrt(var + eps)), from the forward to the backward.
+
+    An object keeps one workspace, so its calls belong on one stream (or on
+    streams that wait for each other).  Where `stream` is given, outputs are
+    the caller's too: memory that torch hands out belongs to its current
+    stream.
+    """
+
+    def __init__(self, grid: Sequence[int], batch: int, channels: int, groups: int,
+                 dtype: torch.dtype = torch.float16, activation: int = B.FNO_NORM_ACT_GELU,
+                 channels_last: bool = False, eps: float = 1e-5, device: str = "cuda"):
+        self.grid = tuple(int(v) for v in grid)
+        self.batch, self.channels, self.groups = int(batch), int(channels), int(groups)
+        if dtype not in DTYPE_CODES:
+            raise ValueError(f"dtype {dtype}, expected float32, float16 or bfloat16")
+        points = 1
+        for v in self.grid:
+            points *= v
+        self.dtype, self.device = dtype, torch.device(device)
+        self.channels_last = bool(channels_last)
+        self.shape = ((self.batch,) + self.grid + (self.channels,) if channels_last
+                      else (self.batch, self.channels) + self.grid)
+        self.desc = B.make_norm_desc(self.batch, points, self.channels, self.groups,
+                                     DTYPE_CODES[dtype],
+                                     B.FNO_LAYOUT_CHANNELS_LAST if channels_last
+                                     else B.FNO_LAYOUT_CHANNELS_FIRST, activation, eps)
+        # descriptor checks run in the library
+        self.ws_bytes = {op: B.fno_group_norm_act_workspace_size(self.desc, op)
+                         for op in (B.FNO_OP_FWD, B.FNO_OP_BWD)}
+        self._ws: Optional[torch.Tensor] = None
+
+    def _workspace(self, device):
+        if self._ws is None or self._ws.device != device:
+            self._ws = torch.empty(max(self.ws_bytes.values()), dtype=torch.uint8, device=device)
+        return self._ws
+
+    def _t(self, t, name, device):
+        return _addr(t, self.shape, self.dtype, name, device)
+
+    def _c(self, t, name, device):
+        return _addr(t, (self.channels,), torch.float32, name, device)
+
+    def _s(self, t, device):
+        return _addr(t, (self.batch, self.groups, 2), torch.float32, "stats", device)
+
+    def _new(self, t, shape, dtype, stream, name):
+        if t is not None:
+            return t
+        if stream is not None:
+            raise ValueError(f"{name} is required where a stream is given")
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def fwd(self, x, gamma=None, beta=None, residual=None, out=None, stats=None,
+            keep_stats: bool = True, stream: Optional[int] = None):
+        """Returns (out, stats); stats is None unless kept (for the backward).
+        out may be x or residual (in place)."""
+        if x is None:
+            raise ValueError("x is required")
+        ax, dev = self._t(x, "x", self.device), x.device
+        ar = self._t(residual, "residual", dev)
+        ag, ab = self._c(gamma, "gamma", dev), self._c(beta, "beta", dev)
+        self._t(out, "out", dev)
+        self._s(stats, dev)
+        s = _stream_of(dev, stream)
+        out = self._new(out, self.shape, self.dtype, stream, "out")
+        if keep_stats:
+            stats = self._new(stats, (self.batch, self.groups, 2), torch.float32, stream, "stats")
+        ws = self._workspace(dev)
+        B.fno_group_norm_act_fwd(self.desc, ax, ag, ab, ar, out.data_ptr(),
+                                 stats.data_ptr() if stats is not None else 0, ws.data_ptr(),
+                                 ws.numel(), s)
+        return out, stats
+
+    def bwd(self, x, g_out, stats, gamma=None, beta=None, gx=None, g_gamma=None, g_beta=None,
+            stream: Optional[int] = None):
+        """Returns (gx, g_gamma, g_beta); the residual's gradient is g_out.
+        gx may be g_out or x (in place)."""
+        for t, name in ((x, "x"), (g_out, "g_out"), (stats, "stats")):
+            if t is None:
+                raise ValueError(f"{name} is required")
+        ax, dev = self._t(x, "x", self.device), x.device
+        ago, ast = self._t(g_out, "g_out", dev), self._s(stats, dev)
+        ag, ab = self._c(gamma, "gamma", dev), self._c(beta, "beta", dev)
+        self._t(gx, "gx", dev)
+        self._c(g_gamma, "g_gamma", dev)
+        self._c(g_beta, "g_beta", dev)
+        s = _stream_of(dev, stream)
+        gx = self._new(gx, self.shape, self.dtype, stream, "gx")
+        g_gamma = self._new(g_gamma, (self.channels,), torch.float32, stream, "g_gamma")
+        g_beta = self._new(g_beta, (self.channels,), torch.float32, stream, "g_beta")
+        ws = self._workspace(dev)
+        B.fno_group_norm_act_bwd(self.desc, ax, ag, ab, ast, ago, gx.data_ptr(),
+                                 g_gamma.data_ptr(), g_beta.data_ptr(), ws.data_ptr(),
+                                 ws.numel(), s)
+        return gx, g_gamma, g_beta

@@ -1,0 +1,239 @@
+"""AdamW over all tensors of a model at once (the fno_adamw_* and fno_grad_norm
+calls), on torch tensors.
+
+PyTorch supplies memory and streams only; every step runs in the HIP kernels.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Dict, List, Optional, Sequence, Union
+
+import torch
+
+from . import binding as B
+from .layer import DTYPE_CODES, _addr, _stream_of
+
+
+class AdamW:
+    """AdamW on the lists `params` and `grads`.
+
+    params: float32, float16 or bfloat16 tensors of any shapes (complex weights
+    as their (re, im) pairs); grads: float32 or the parameter's type, the same
+    shapes.  All contiguous, on one GPU, 16-byte aligned, none overlapping
+    another.  masters: the float32 values that 16-bit parameters round (one
+    entry each, None for a float32 parameter or to go without), made by
+    `make_masters`.  weight_decay: one value, or one per tensor.
+
+    state_bits 32 keeps the moments as float32, 8 as codes with a scale per
+    256 elements (one value, or one per tensor).  `states` takes up moments
+    that exist (one dict per tensor: exp_avg and exp_avg_sq, with
+    exp_avg_scale and exp_avg_sq_scale in 8 bits), after `step` steps;
+    otherwise they start at zero.
+
+    The object writes the addresses of its tensors down once and keeps their
+    storage; `set_grads` (and `step(grads=...)`) takes other gradients.  A
+    parameter that is to change its storage needs a new object.
+
+    device_control: the step number, the clipped scale and the skip of
+    non-finite gradients live on the GPU; each `step` then follows one
+    `clip_grads`, nothing is read by the host, and both can be captured in a
+    HIP graph.  Calls of one object belong on one stream.
+    """
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
+                 masters: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 states: Optional[Sequence[Dict[str, torch.Tensor]]] = None, lr: float = 1e-3,
+                 betas: Sequence[float] = (0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: Union[float, Sequence[float]] = 1e-2,
+                 state_bits: Union[int, Sequence[int]] = 32, step: int = 0,
+                 device_control: bool = False):
+        self.params = list(params)
+        n = len(self.params)
+        if n == 0:
+            raise ValueError("params is empty")
+        self.device = self.params[0].device
+        self.masters = self._per_tensor(masters if masters is not None else [None] * n, "masters")
+        self.state_bits = self._per_tensor([state_bits] * n if isinstance(state_bits, int)
+                                           else state_bits, "state_bits")
+        decay = self._per_tensor([weight_decay] * n if isinstance(weight_decay, (int, float))
+                                 else weight_decay, "weight_decay")
+        for b in self.state_bits:
+            if b not in (32, 8):
+                raise ValueError(f"state_bits {b}, expected 32 or 8")
+        if step < 0:
+            raise ValueError(f"step {step}, expected at least 0")
+        self.steps = int(step)
+        self.desc = B.FnoAdamwDesc(float(lr), float(betas[0]), float(betas[1]), float(eps))
+        self.states: List[Dict[str, torch.Tensor]] = (
+            [self._zero_state(p, b) for p, b in zip(self.params, self.state_bits)]
+            if states is None else [dict(s) for s in self._per_tensor(states, "states")])
+        self._list = (B.FnoAdamwTensor * n)()
+        seen = set()
+        for i, (t, p) in enumerate(zip(self._list, self.params)):
+            if p.dtype not in DTYPE_CODES:
+                raise ValueError(f"params[{i}]: dtype {p.dtype}, expected float32, float16 or "
+                                 "bfloat16")
+            t.param = _addr(p, None, None, f"params[{i}]", self.device) or None
+            t.param_dtype, t.n = DTYPE_CODES[p.dtype], p.numel()
+            m = self.masters[i]
+            if m is not None and p.dtype == torch.float32:
+                raise ValueError(f"masters[{i}]: a float32 parameter has none")
+            t.master = _addr(m, p.shape, torch.float32, f"masters[{i}]", self.device) or None
+            t.state_bits, t.weight_decay = self.state_bits[i], float(decay[i])
+            own = [t.param, t.master] + self._set_state(t, i)
+            own = [v for v in own if v] if t.n else []
+            if len(set(own)) != len(own) or seen & set(own):
+                raise ValueError(f"params[{i}]: a parameter, master or state is used twice")
+            seen |= set(own)
+        self.set_grads(grads)
+        self.control: Optional[torch.Tensor] = None
+        if device_control:
+            c = B.FnoAdamwControl(step=self.steps, lr_factor=1.0, grad_scale=1.0)
+            self.control = torch.frombuffer(bytearray(bytes(c)), dtype=torch.uint8).to(self.device)
+            self._norm = self.control[16:20].view(torch.float32)
+            self._factor = self.control[28:32].view(torch.float32)
+            self._ws = torch.empty(B.fno_grad_norm_workspace_size(self._list, n),
+                                   dtype=torch.uint8, device=self.device)
+
+    # -- construction ------------------------------------------------------------
+    def _per_tensor(self, v, name):
+        v = list(v)
+        if len(v) != len(self.params):
+            raise ValueError(f"{name}: {len(v)} entries for {len(self.params)} parameters")
+        return v
+
+    @staticmethod
+    def make_masters(params: Sequence[torch.Tensor]) -> List[Optional[torch.Tensor]]:
+        """float32 copies of the 16-bit parameters (None for float32 ones)."""
+        return [None if p.dtype == torch.float32 else p.detach().float().clone() for p in params]
+
+    @staticmethod
+    def _zero_state(p, bits):
+        z = dict(device=p.device)
+        if bits == 32:
+            return {k: torch.zeros(p.numel(), dtype=torch.float32, **z)
+                    for k in ("exp_avg", "exp_avg_sq")}
+        blocks = -(-p.numel() // B.FNO_ADAMW_BLOCK)
+        return {"exp_avg": torch.zeros(p.numel(), dtype=torch.int8, **z),
+                "exp_avg_sq": torch.zeros(p.numel(), dtype=torch.uint8, **z),
+                "exp_avg_scale": torch.zeros(blocks, dtype=torch.float32, **z),
+                "exp_avg_sq_scale": torch.zeros(blocks, dtype=torch.float32, **z)}
+
+    def _set_state(self, t, i):
+        s, n = self.states[i], t.n
+        blocks = -(-n // B.FNO_ADAMW_BLOCK)
+        want = ({"exp_avg": (n, torch.float32), "exp_avg_sq": (n, torch.float32)}
+                if t.state_bits == 32 else
+                {"exp_avg": (n, torch.int8), "exp_avg_sq": (n, torch.uint8),
+                 "exp_avg_scale": (blocks, torch.float32),
+                 "exp_avg_sq_scale": (blocks, torch.float32)})
+        if set(s) != set(want):
+            raise ValueError(f"states[{i}]: {sorted(s)}, expected {sorted(want)}")
+        got = []
+        for k, (count, dtype) in want.items():
+            if s[k].numel() != count:
+                raise ValueError(f"states[{i}].{k}: {s[k].numel()} elements, expected {count}")
+            got.append(_addr(s[k], None, dtype, f"states[{i}].{k}", self.device) or None)
+            setattr(t, k, got[-1])
+        return got
+
+    def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
+        """Takes `grads` as the gradients of the following steps."""
+        grads = self._per_tensor(grads, "grads")
+        addr = []
+        for i, (p, g) in enumerate(zip(self.params, grads)):
+            if g is None:
+                raise ValueError(f"grads[{i}] is required")
+            if g.dtype not in (torch.float32, p.dtype):
+                raise ValueError(f"grads[{i}]: dtype {g.dtype}, expected float32 or {p.dtype}")
+            addr.append(_addr(g, p.shape, None, f"grads[{i}]", self.device))
+        for t, g, a in zip(self._list, grads, addr):
+            t.grad, t.grad_dtype = a or None, DTYPE_CODES[g.dtype]
+        self.grads = grads
+        # what the addresses point to stays, whatever becomes of the tensors
+        self._held = [v.untyped_storage() for v in self.params + self.grads + [
+            m for m in self.masters if m is not None] + [
+                v for s in self.states for v in s.values()]]
+
+    # -- the calls ---------------------------------------------------------------
+    def clip_grads(self, max_norm: float = float("inf"), loss_scale: float = 1.0,
+                   stream: Optional[int] = None) -> torch.Tensor:
+        """The global norm of the gradients over `loss_scale` (returned, a
+        tensor of one element that later calls overwrite), and the next step's
+        gradient scale, step number and skip, on the device."""
+        if self.control is None:
+            raise ValueError("clip_grads needs device_control=True")
+        if not loss_scale > 0:
+            raise ValueError(f"loss_scale {loss_scale}, expected more than 0")
+        B.fno_grad_norm(self._list, len(self.params), max_norm, 1.0 / loss_scale,
+                        self.control.data_ptr(), self._ws.data_ptr(), self._ws.numel(),
+                        _stream_of(self.device, stream))
+        return self._norm
+
+    def step(self, grads: Optional[Sequence[torch.Tensor]] = None, lr: Optional[float] = None,
+             stream: Optional[int] = None) -> None:
+        """One step (with device_control: the one that clip_grads prepared).
+        lr: the learning rate from this step on."""
+        if grads is not None:
+            if self.control is not None:
+                raise ValueError("set_grads before clip_grads: the clip reads the gradients")
+            self.set_grads(grads)
+        if lr is not None:
+            self.desc.lr = float(lr)
+        s = _stream_of(self.device, stream)
+        if self.control is not None:
+            B.fno_adamw_step(self.desc, self._list, len(self.params), 0, self.control.data_ptr(), s)
+        else:
+            B.fno_adamw_step(self.desc, self._list, len(self.params), self.steps + 1, 0, s)
+            self.steps += 1
+
+    def set_lr_factor(self, factor: float) -> None:
+        """Multiplies lr on the device (a schedule for captured steps), in the
+        order of the current stream."""
+        if self.control is None:
+            raise ValueError("set_lr_factor needs device_control=True")
+        self._factor.fill_(float(factor))
+
+    def read_control(self) -> Dict[str, float]:
+        """The control block's fields (waits for the current stream)."""
+        if self.control is None:
+            raise ValueError("read_control needs device_control=True")
+        c = B.FnoAdamwControl.from_buffer_copy(bytes(self.control.cpu().numpy()))
+        return {k: getattr(c, k) for k, _ in c._fields_}
+
+    def moments(self, exp_avg: Optional[Sequence[torch.Tensor]] = None,
+                exp_avg_sq: Optional[Sequence[torch.Tensor]] = None,
+                dtype: torch.dtype = torch.float32, stream: Optional[int] = None):
+        """The moments as values, two lists: 32-bit states themselves, 8-bit
+        ones read out into tensors of the parameter's element count, made here
+        in `dtype` or the caller's (then a full list of one type each; entries
+        of 32-bit states stay as they are)."""
+        eight = [i for i, b in enumerate(self.state_bits) if b == 8]
+        s = _stream_of(self.device, stream)
+        outs = []
+        for k, given in (("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq)):
+            if given is None:
+                if stream is not None:
+                    raise ValueError(f"{k} is required where a stream is given")
+                given = [torch.empty(self.params[i].numel(), dtype=dtype, device=self.device)
+                         if b == 8 else self.states[i][k] for i, b in enumerate(self.state_bits)]
+            given = self._per_tensor(given, k)
+            if eight:
+                dtype = given[eight[0]].dtype
+                if dtype not in DTYPE_CODES:
+                    raise ValueError(f"{k}: dtype {dtype}")
+            outs.append(given)
+        if not eight:
+            return outs[0], outs[1]
+        sub = (B.FnoAdamwTensor * len(eight))(*[self._list[i] for i in eight])
+        ptrs = []
+        for k, out in zip(("exp_avg", "exp_avg_sq"), outs):
+            a = (ctypes.c_void_p * len(eight))()
+            for j, i in enumerate(eight):
+                if out[i].numel() != self.params[i].numel():
+                    raise ValueError(f"{k}[{i}]: {out[i].numel()} elements, expected "
+                                     f"{self.params[i].numel()}")
+                a[j] = _addr(out[i], None, dtype, f"{k}[{i}]", self.device) or None
+            ptrs.append(a)
+        B.fno_adamw_moments(sub, len(eight), DTYPE_CODES[dtype], ptrs[0], ptrs[1], s)
+        return outs[0], outs[1]
