@@ -494,12 +494,15 @@ typedef struct {
 } fno_adamw_desc;
 
 /* What steps of one optimizer share on the device, for training without a
- * host read between backward and update, and under HIP graph capture: 32
+ * host read between backward and update, and under HIP graph capture: 48
  * bytes of device memory, zeroed by the caller before first use except for
- * lr_factor = 1.  fno_grad_norm writes all but lr_factor. */
+ * lr_factor = 1 (and step, to go on from a checkpoint).  fno_grad_norm writes
+ * all but lr_factor. */
 typedef struct {
   int64_t step;       /* steps taken */
   int64_t skipped;    /* steps left out for non-finite gradients */
+  double bias1;       /* 1 / (1 - beta1^step) */
+  double bias2;       /* 1 / sqrt(1 - beta2^step) */
   float grad_norm;    /* L2 norm of the unscaled gradients of the last call */
   float grad_scale;   /* what the step multiplies gradients with */
   int32_t skip;       /* 1: the last gradients were not finite */
@@ -507,18 +510,21 @@ typedef struct {
 } fno_adamw_control;
 
 /* The global gradient norm with clip, loss-scale removal and non-finite check:
- * over all gradients of the list (read only; the other pointers are ignored),
+ * over all gradients of the list (read only; the tensors' other pointers are
+ * ignored),
  *     grad_norm  = inv_loss_scale sqrt(sum grad^2)      (sum in double)
  *     grad_scale = inv_loss_scale min(1, max_norm / grad_norm)
- * into `control`, and step += 1; where the sum is not finite instead skip = 1
- * and skipped += 1, and the fno_adamw_step that follows changes nothing.
- * max_norm > 0 (INFINITY: no clip), inv_loss_scale > 0 and finite.  The sum
- * has a fixed order: bit-identical from run to run. */
+ * into `control`, step += 1 and the new step's bias corrections (desc's beta1
+ * and beta2); where the sum is not finite instead skip = 1 and skipped += 1,
+ * and the fno_adamw_step that follows changes nothing.  max_norm > 0
+ * (INFINITY: no clip), inv_loss_scale > 0 and finite.  The sum has a fixed
+ * order: bit-identical from run to run. */
 fno_status fno_grad_norm_workspace_size(const fno_adamw_tensor *tensors, int64_t count,
                                         size_t *bytes);
-fno_status fno_grad_norm(const fno_adamw_tensor *tensors, int64_t count, double max_norm,
-                         double inv_loss_scale, fno_adamw_control *control, void *ws,
-                         size_t ws_len, hipStream_t stream);
+fno_status fno_grad_norm(const fno_adamw_desc *desc, const fno_adamw_tensor *tensors,
+                         int64_t count, double max_norm, double inv_loss_scale,
+                         fno_adamw_control *control, void *ws, size_t ws_len,
+                         hipStream_t stream);
 
 /* One step.  control null: step number `step` (>= 1) with gradients as they
  * are (s = 1).  control (device memory) not null: the step number, s and skip

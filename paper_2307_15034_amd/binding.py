@@ -141,6 +141,8 @@ class FnoAdamwControl(ctypes.Structure):
     _fields_ = [
         ("step", ctypes.c_int64),
         ("skipped", ctypes.c_int64),
+        ("bias1", ctypes.c_double),
+        ("bias2", ctypes.c_double),
         ("grad_norm", ctypes.c_float),
         ("grad_scale", ctypes.c_float),
         ("skip", ctypes.c_int32),
@@ -211,7 +213,7 @@ def _load() -> ctypes.CDLL:
         "fno_group_norm_act_bwd": (ctypes.c_int,
                                    [ND, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "fno_grad_norm_workspace_size": (ctypes.c_int, [AT, i64, P(sz)]),
-        "fno_grad_norm": (ctypes.c_int, [AT, i64, f64, f64, vp, vp, sz, vp]),
+        "fno_grad_norm": (ctypes.c_int, [P(FnoAdamwDesc), AT, i64, f64, f64, vp, vp, sz, vp]),
         "fno_adamw_step": (ctypes.c_int, [P(FnoAdamwDesc), AT, i64, i64, vp, vp]),
         "fno_adamw_moments": (ctypes.c_int, [AT, i64, ctypes.c_int, P(vp), P(vp), vp]),
         "fno_release_caches": (ctypes.c_int, []),
@@ -486,10 +488,10 @@ def fno_grad_norm_workspace_size(tensors, count: int) -> int:
     return b.value
 
 
-def fno_grad_norm(tensors, count: int, max_norm: float, inv_loss_scale: float, control: int,
-                  ws: int, ws_bytes: int, stream: int, check: bool = True) -> int:
-    st = _lib.fno_grad_norm(tensors, count, max_norm, inv_loss_scale, control or None, ws or None,
-                            ws_bytes, stream or None)
+def fno_grad_norm(desc, tensors, count: int, max_norm: float, inv_loss_scale: float,
+                  control: int, ws: int, ws_bytes: int, stream: int, check: bool = True) -> int:
+    st = _lib.fno_grad_norm(ctypes.byref(desc), tensors, count, max_norm, inv_loss_scale,
+                            control or None, ws or None, ws_bytes, stream or None)
     if check:
         _check(st, "fno_grad_norm")
     return st

@@ -18,7 +18,8 @@ namespace {
 
 constexpr int kBatch = FNO_ADAMW_LAUNCH_TENSORS;
 constexpr int kBlk = FNO_ADAMW_BLOCK;
-constexpr int64_t kChunk = 2048;             // elements of a work-group
+constexpr int64_t kChunk = 2048;             // elements of a work-group of the step
+constexpr int64_t kNormChunk = 16384;        // elements of a work-group of the norm
 constexpr int64_t kMaxN = (int64_t)1 << 34;  // elements of a tensor
 constexpr int64_t kMaxGrid = (int64_t)1 << 23;  // work-groups of a launch
 
@@ -42,8 +43,8 @@ struct AdamArgs {
 };
 
 struct AdamHyper {
-  double lr, b1, b2, size, root;  // size = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
-  float eps, gs;
+  double lr, b1, b2, bias1, bias2;  // bias1 = 1 / (1 - b1^t), bias2 = 1 / sqrt(1 - b2^t)
+  float eps;
 };
 
 // x^t by repeated squaring, the same on the host and on the device.
@@ -56,31 +57,65 @@ __host__ __device__ inline double int_pow(double x, int64_t t) {
   return r;
 }
 
-__host__ __device__ inline void bias_correct(AdamHyper* h, int64_t t) {
-  h->size = h->lr / (1.0 - int_pow(h->b1, t));
-  h->root = 1.0 / sqrt(1.0 - int_pow(h->b2, t));
-}
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+typedef int8_t c4 __attribute__((ext_vector_type(4)));
+typedef uint8_t u4 __attribute__((ext_vector_type(4)));
+template <typename T>
+struct Vec4;
+template <>
+struct Vec4<float> {
+  typedef f4 type;
+};
+template <>
+struct Vec4<_Float16> {
+  typedef h4 type;
+};
+template <>
+struct Vec4<__bf16> {
+  typedef b4 type;
+};
 
-__device__ inline float load_as_float(const void* p, int64_t i, int dt) {
-  if (dt == FNO_DTYPE_F32) return static_cast<const float*>(p)[i];
-  if (dt == FNO_DTYPE_F16) return (float)static_cast<const _Float16*>(p)[i];
-  return (float)static_cast<const __bf16*>(p)[i];
+// Elements e .. e + 4 of an array of n (e a multiple of four): in one access
+// where all four are there, one by one at the tensor's end (others read as 0
+// and are not written).
+template <typename V, typename T>
+__device__ __forceinline__ V load4(const T* p, int64_t e, int64_t n) {
+  if (e + 4 <= n) return *reinterpret_cast<const V*>(p + e);
+  V v = {};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (e + j < n) v[j] = p[e + j];
+  return v;
 }
-__device__ inline void store_rounded(void* p, int64_t i, int dt, float v) {
-  if (dt == FNO_DTYPE_F32) static_cast<float*>(p)[i] = v;
-  else if (dt == FNO_DTYPE_F16) static_cast<_Float16*>(p)[i] = (_Float16)v;
-  else static_cast<__bf16*>(p)[i] = (__bf16)v;
-}
-
-// The tensor of chunk c: the last i with first[i] <= c.
-__device__ inline int find_tensor(const int32_t* first, int count, int c) {
-  int lo = 0, hi = count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= c) lo = mid;
-    else hi = mid - 1;
+template <typename V, typename T>
+__device__ __forceinline__ void store4(T* p, int64_t e, int64_t n, const V& v) {
+  if (e + 4 <= n) {
+    *reinterpret_cast<V*>(p + e) = v;
+    return;
   }
-  return lo;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (e + j < n) p[e + j] = v[j];
+}
+
+// An fp32 result rounded to the storage type: two roundings, as stated.  (The
+// compiler otherwise folds a last product or sum and its conversion to fp16
+// into one instruction with one rounding.)
+template <typename T>
+__device__ __forceinline__ T rounded(float x) {
+  asm("" : "+v"(x));
+  return (T)x;
+}
+
+// The tensor of chunk c: the last i with first[i] <= c.  Every lane looks at
+// one entry (kBatch <= 64), all in one load.
+__device__ __forceinline__ int find_tensor(const int32_t* first, int count, int c) {
+  static_assert(kBatch <= 64, "one entry per lane");
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = __ballot(lane < count && first[lane < count ? lane : 0] <= c);
+  return 63 - __builtin_clzll(below);
 }
 
 struct Consts {  // an element's step in floats
@@ -98,23 +133,18 @@ __device__ inline float adam_element(const Consts& k, float p, float g, float* m
   return p * k.keep - (*m * k.size) / (*w * k.root + k.eps);
 }
 
-__device__ inline Consts consts_of(const AdamHyper& h0, const fno_adamw_control* ctl, float wd) {
-  AdamHyper h = h0;
-  if (ctl) {
-    h.lr *= (double)ctl->lr_factor;
-    bias_correct(&h, ctl->step);
-    h.gs = ctl->grad_scale;
-  }
+__device__ __forceinline__ Consts consts_of(const AdamHyper& h, const fno_adamw_control* ctl, float wd) {
+  const double lr = ctl ? h.lr * (double)ctl->lr_factor : h.lr;
   Consts k;
   k.b1 = (float)h.b1;
   k.c1 = (float)(1.0 - h.b1);
   k.b2 = (float)h.b2;
   k.c2 = (float)(1.0 - h.b2);
-  k.size = (float)h.size;
-  k.root = (float)h.root;
+  k.size = (float)(lr * (ctl ? ctl->bias1 : h.bias1));
+  k.root = (float)(ctl ? ctl->bias2 : h.bias2);
   k.eps = h.eps;
-  k.gs = h.gs;
-  k.keep = (float)(1.0 - h.lr * (double)wd);
+  k.gs = ctl ? ctl->grad_scale : 1.0f;
+  k.keep = (float)(1.0 - lr * (double)wd);
   return k;
 }
 
@@ -135,13 +165,241 @@ __device__ inline float decode_v(float b, int q) {
   const float s = (b * (1.0f / 65025.0f)) * (float)(q * q);
   return s * s;
 }
-// Codes of the fractions |m| / A and sqrt(v) / B; top = 0 or a value that is
-// not a number gives 0 (the scale then tells).
-__device__ inline int code_of(float x, float top, float levels) {
+// Four elements of an array of any type as floats, all loads before the first use.
+__device__ __forceinline__ void load_any(const void* p, int dt, const int64_t (&at)[4], float (&x)[4]) {
+  uint32_t raw[4];
+  if (dt == FNO_DTYPE_F32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) raw[j] = static_cast<const uint32_t*>(p)[at[j]];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) raw[j] = static_cast<const uint16_t*>(p)[at[j]];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    x[j] = dt == FNO_DTYPE_F32   ? __uint_as_float(raw[j])
+           : dt == FNO_DTYPE_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)raw[j])
+                                 : __uint_as_float(raw[j] << 16);
+}
+
+// A code with its moment's sign; a second moment's, at least 1 where w > 0.
+// (Blocks that hold a value that is not finite: some code within the range.)
+__device__ __forceinline__ int8_t signed_code(float q, float m) {
+  const int c = (int)__builtin_fminf(q, 127.0f);
+  return (int8_t)(m < 0.0f ? -c : c);
+}
+__device__ __forceinline__ uint8_t unsigned_code(float q, float w) {
+  return (uint8_t)(int)__builtin_fminf(__builtin_fmaxf(q, w > 0.0f ? 1.0f : 0.0f), 255.0f);
+}
+
+// rint(levels sqrt(x / top)), quotient, root and product rounded to fp32:
+// the code of the fraction x / top; a top that is 0 or not a number gives
+// some code (0 for 0; the scale then tells).
+__device__ __forceinline__ float code_exact(float x, float top, float levels) {
 #pragma clang fp contract(off)
-  if (!(top > 0.0f)) return 0;
-  const float q = rintf(__builtin_sqrtf(x / top) * levels);
-  return q == q ? (int)q : 0;
+  return rintf(__builtin_sqrtf(x / (top > 0.0f ? top : 1.0f)) * levels);
+}
+
+// The codes of four fractions.  A reciprocal of the block's top and the
+// hardware's root are within 3.5 x 2^-23 of the rounded quotient's root, so
+// the product with at most 255 levels is within 2^-13 of the exact one, and
+// the nearest integer is the same unless a half lies that near.  Where one of
+// the wave's values is (about one wave in nine), all take the divisions and
+// rounded roots.  (These cost 60 operations an element for both moments: the
+// step of 2^28 fp32 parameters took @SLOW@ us with them everywhere, @FAST@ us so.)
+__device__ __forceinline__ void codes4(const f4& x, float top, float levels, f4* q) {
+  const float r = __builtin_amdgcn_rcpf(top > 0.0f ? top : 1.0f);
+  bool near = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float z = __builtin_amdgcn_sqrtf(x[j] * r) * levels;
+    (*q)[j] = __builtin_rintf(z);
+    near |= !(__builtin_fabsf(z - (*q)[j]) < 0.5f - 0x1p-13f);
+  }
+  if (__any(near)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) (*q)[j] = code_exact(x[j], top, levels);
+  }
+}
+
+// A chunk that lies inside its tensor: each thread takes four consecutive
+// elements at a time, so that a wave covers 256, a block of the 8-bit states;
+// all loads of the chunk are in flight before the first element's step.
+template <typename P, typename G, bool MASTER, int BITS>
+__device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, const Consts& k) {
+  constexpr int U = (int)kChunk / 1024;
+  using PV = typename Vec4<P>::type;
+  using GV = typename Vec4<G>::type;
+  const int64_t e0 = base + 4 * threadIdx.x;
+  P* pp = static_cast<P*>(t.p) + e0;
+  const G* gp = static_cast<const G*>(t.g) + e0;
+  float* master = t.master + e0;
+  float *m32 = static_cast<float*>(t.m) + e0, *v32 = static_cast<float*>(t.v) + e0;
+  int8_t* m8 = static_cast<int8_t*>(t.m) + e0;
+  uint8_t* v8 = static_cast<uint8_t*>(t.v) + e0;
+  const int64_t b0 = __builtin_amdgcn_readfirstlane((int)(e0 / kBlk));
+  f4 pm[U], m[U], v[U];
+  PV pl[U];
+  GV g[U];
+  c4 qm[U];
+  u4 qv[U];
+  float as[U], bs[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (MASTER) pm[u] = *reinterpret_cast<const f4*>(master + 1024 * u);
+    else pl[u] = *reinterpret_cast<const PV*>(pp + 1024 * u);
+    g[u] = *reinterpret_cast<const GV*>(gp + 1024 * u);
+    if (BITS == 32) {
+      m[u] = *reinterpret_cast<const f4*>(m32 + 1024 * u);
+      v[u] = *reinterpret_cast<const f4*>(v32 + 1024 * u);
+    } else {
+      qm[u] = *reinterpret_cast<const c4*>(m8 + 1024 * u);
+      qv[u] = *reinterpret_cast<const u4*>(v8 + 1024 * u);
+      as[u] = t.ms[b0 + 4 * u];
+      bs[u] = t.vs[b0 + 4 * u];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    f4 p, w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (BITS == 8) {
+        m[u][j] = decode_m(as[u], qm[u][j]);
+        v[u][j] = decode_v(bs[u], qv[u][j]);
+      }
+      float mj = m[u][j], vj = v[u][j], wj;
+      p[j] = adam_element(k, MASTER ? pm[u][j] : (float)pl[u][j], (float)g[u][j], &mj, &vj, &wj);
+      m[u][j] = mj;
+      v[u][j] = vj;
+      w[j] = wj;
+    }
+    if (MASTER) *reinterpret_cast<f4*>(master + 1024 * u) = p;
+    PV pr;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) pr[j] = rounded<P>(p[j]);
+    *reinterpret_cast<PV*>(pp + 1024 * u) = pr;
+    if (BITS == 32) {
+      *reinterpret_cast<f4*>(m32 + 1024 * u) = m[u];
+      *reinterpret_cast<f4*>(v32 + 1024 * u) = v[u];
+    } else {
+      f4 am, cm, cv;
+      uint32_t ma = 0, mb = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        am[j] = __builtin_fabsf(m[u][j]);
+        ma = max(ma, abs_bits(m[u][j]));
+        mb = max(mb, abs_bits(w[j]));
+      }
+      const float A = __uint_as_float(wave_max(ma)), Bt = __uint_as_float(wave_max(mb));
+      codes4(am, A, 127.0f, &cm);
+      codes4(w, Bt, 255.0f, &cv);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        qm[u][j] = signed_code(cm[j], m[u][j]);
+        qv[u][j] = unsigned_code(cv[j], w[j]);
+      }
+      *reinterpret_cast<c4*>(m8 + 1024 * u) = qm[u];
+      *reinterpret_cast<u4*>(v8 + 1024 * u) = qv[u];
+      if ((threadIdx.x & 63) == 0) {
+        t.ms[b0 + 4 * u] = A;
+        t.vs[b0 + 4 * u] = Bt;
+      }
+    }
+  }
+}
+
+// A tensor's last chunk, of any types: elements lie across the lanes, 64 of a
+// block at a time; loads past the end read the last element and are dropped.
+template <int BITS>
+__device__ __forceinline__ void last_chunk(const AdamTensor& t, int64_t base, const Consts& k) {
+  constexpr int U = (int)kChunk / 1024;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll 1
+  for (int u = 0; u < U; ++u) {
+    const int64_t b = base / kBlk + 4 * u + wave;
+    if (b * kBlk >= t.n) break;
+    float p[4], g[4], m[4], v[4];
+    int64_t at[4];
+    f4 w, am;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t e = b * kBlk + 64 * j + lane;
+      at[j] = e < t.n ? e : t.n - 1;
+    }
+    load_any(t.master ? t.master : t.p, t.master ? FNO_DTYPE_F32 : t.pdt, at, p);
+    load_any(t.g, t.gdt, at, g);
+    if (BITS == 32) {
+      load_any(t.m, FNO_DTYPE_F32, at, m);
+      load_any(t.v, FNO_DTYPE_F32, at, v);
+    } else {
+      int qm[4], qv[4];
+      const float as = t.ms[b], bs = t.vs[b];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        qm[j] = static_cast<const int8_t*>(t.m)[at[j]];
+        qv[j] = static_cast<const uint8_t*>(t.v)[at[j]];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        m[j] = decode_m(as, qm[j]);
+        v[j] = decode_v(bs, qv[j]);
+      }
+    }
+    uint32_t ma = 0, mb = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool in = b * kBlk + 64 * j + lane < t.n;
+      float wj;
+      p[j] = adam_element(k, p[j], g[j], &m[j], &v[j], &wj);
+      w[j] = wj;
+      am[j] = __builtin_fabsf(m[j]);
+      ma = max(ma, abs_bits(m[j]));  // past the end: the last element's own, once more
+      mb = max(mb, abs_bits(wj));
+      if (!in) continue;
+      if (t.master) t.master[at[j]] = p[j];
+      if (t.pdt == FNO_DTYPE_F32) static_cast<float*>(t.p)[at[j]] = p[j];
+      else if (t.pdt == FNO_DTYPE_F16) static_cast<_Float16*>(t.p)[at[j]] = rounded<_Float16>(p[j]);
+      else static_cast<__bf16*>(t.p)[at[j]] = rounded<__bf16>(p[j]);
+      if (BITS == 32) {
+        static_cast<float*>(t.m)[at[j]] = m[j];
+        static_cast<float*>(t.v)[at[j]] = v[j];
+      }
+    }
+    if (BITS == 8) {
+      const float A = __uint_as_float(wave_max(ma)), Bt = __uint_as_float(wave_max(mb));
+      f4 cm, cv;
+      codes4(am, A, 127.0f, &cm);
+      codes4(w, Bt, 255.0f, &cv);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (b * kBlk + 64 * j + lane >= t.n) continue;
+        static_cast<int8_t*>(t.m)[at[j]] = signed_code(cm[j], m[j]);
+        static_cast<uint8_t*>(t.v)[at[j]] = unsigned_code(cv[j], w[j]);
+      }
+      if (lane == 0) {
+        t.ms[b] = A;
+        t.vs[b] = Bt;
+      }
+    }
+  }
+}
+
+template <typename P, typename G, bool MASTER>
+__device__ __forceinline__ void full_of(const AdamTensor& t, int64_t base, const Consts& k) {
+  if (t.bits == 32) full_chunk<P, G, MASTER, 32>(t, base, k);
+  else full_chunk<P, G, MASTER, 8>(t, base, k);
+}
+
+template <typename P>
+__device__ __forceinline__ void full_half(const AdamTensor& t, int64_t base, const Consts& k) {
+  if (t.gdt == FNO_DTYPE_F32) {
+    if (t.master) full_of<P, float, true>(t, base, k);
+    else full_of<P, float, false>(t, base, k);
+  } else {
+    if (t.master) full_of<P, P, true>(t, base, k);
+    else full_of<P, P, false>(t, base, k);
+  }
 }
 
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a, AdamHyper h,
@@ -149,55 +407,21 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a, AdamHyper h,
   if (ctl && ctl->skip) return;
   const int i = find_tensor(a.first, a.count, (int)blockIdx.x);
   const AdamTensor& t = a.t[i];
-  const Consts k = consts_of(h, ctl, t.wd);
   const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * kChunk;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (t.bits == 32) {
-    for (int64_t e = base + threadIdx.x; e < base + kChunk && e < t.n; e += 256) {
-      float m = static_cast<float*>(t.m)[e], v = static_cast<float*>(t.v)[e], w;
-      float p = t.master ? t.master[e] : load_as_float(t.p, e, t.pdt);
-      p = adam_element(k, p, load_as_float(t.g, e, t.gdt), &m, &v, &w);
-      static_cast<float*>(t.m)[e] = m;
-      static_cast<float*>(t.v)[e] = v;
-      if (t.master) t.master[e] = p;
-      store_rounded(t.p, e, t.pdt, p);
-    }
-    return;
-  }
-  for (int64_t b = base / kBlk + wave; b < (base + kChunk) / kBlk && b * kBlk < t.n; b += 4) {
-    float m[4], w[4];
-    const float as = t.ms[b], bs = t.vs[b];
-    uint32_t am = 0, bm = 0;
-    for (int j = 0; j < 4; ++j) {
-      const int64_t e = b * kBlk + 64 * j + lane;
-      m[j] = w[j] = 0.0f;
-      if (e >= t.n) continue;
-      m[j] = decode_m(as, static_cast<int8_t*>(t.m)[e]);
-      float v = decode_v(bs, static_cast<uint8_t*>(t.v)[e]);
-      float p = t.master ? t.master[e] : load_as_float(t.p, e, t.pdt);
-      p = adam_element(k, p, load_as_float(t.g, e, t.gdt), &m[j], &v, &w[j]);
-      if (t.master) t.master[e] = p;
-      store_rounded(t.p, e, t.pdt, p);
-      am = max(am, abs_bits(m[j]));
-      bm = max(bm, abs_bits(w[j]));
-    }
-    const float A = __uint_as_float(wave_max(am)), Bt = __uint_as_float(wave_max(bm));
-    for (int j = 0; j < 4; ++j) {
-      const int64_t e = b * kBlk + 64 * j + lane;
-      if (e >= t.n) continue;
-      const int qm = code_of(__builtin_fabsf(m[j]), A, 127.0f);
-      const int qv = code_of(w[j], Bt, 255.0f);
-      static_cast<int8_t*>(t.m)[e] = (int8_t)(m[j] < 0.0f ? -qm : qm);
-      static_cast<uint8_t*>(t.v)[e] = (uint8_t)(w[j] > 0.0f && qv < 1 ? 1 : qv);
-    }
-    if (lane == 0) {
-      t.ms[b] = A;
-      t.vs[b] = Bt;
-    }
+  const Consts k = consts_of(h, ctl, t.wd);
+  if (base + kChunk > t.n) {
+    if (t.bits == 32) last_chunk<32>(t, base, k);
+    else last_chunk<8>(t, base, k);
+  } else if (t.pdt == FNO_DTYPE_F32) {
+    full_of<float, float, false>(t, base, k);
+  } else if (t.pdt == FNO_DTYPE_F16) {
+    full_half<_Float16>(t, base, k);
+  } else {
+    full_half<__bf16>(t, base, k);
   }
 }
 
-// 8-bit moments read out.
+// 8-bit moments read out, four elements per thread at a time.
 struct MomentArgs {
   AdamArgs a;
   void* mo[kBatch];
@@ -205,56 +429,108 @@ struct MomentArgs {
   int32_t dt;
 };
 
+template <typename T>
+__device__ __forceinline__ void moments_chunk(const AdamTensor& t, int64_t base, T* mo, T* vo) {
+  constexpr int U = (int)kChunk / 1024;
+  using V = typename Vec4<T>::type;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t e = base + 1024 * u + 4 * threadIdx.x;
+    if (e >= t.n) return;
+    const c4 qm = load4<c4>(static_cast<int8_t*>(t.m), e, t.n);
+    const u4 qv = load4<u4>(static_cast<uint8_t*>(t.v), e, t.n);
+    const float a = t.ms[e / kBlk], b = t.vs[e / kBlk];
+    V m, v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = rounded<T>(decode_m(a, qm[j]));
+      v[j] = rounded<T>(decode_v(b, qv[j]));
+    }
+    store4(mo, e, t.n, m);
+    store4(vo, e, t.n, v);
+  }
+}
+
 __global__ __launch_bounds__(256) void moments_kernel(MomentArgs a) {
   const int i = find_tensor(a.a.first, a.a.count, (int)blockIdx.x);
   const AdamTensor& t = a.a.t[i];
   const int64_t base = (int64_t)((int)blockIdx.x - a.a.first[i]) * kChunk;
-  for (int64_t e = base + threadIdx.x; e < base + kChunk && e < t.n; e += 256) {
-    store_rounded(a.mo[i], e, a.dt, decode_m(t.ms[e / kBlk], static_cast<int8_t*>(t.m)[e]));
-    store_rounded(a.vo[i], e, a.dt, decode_v(t.vs[e / kBlk], static_cast<uint8_t*>(t.v)[e]));
-  }
+  if (a.dt == FNO_DTYPE_F32)
+    moments_chunk(t, base, static_cast<float*>(a.mo[i]), static_cast<float*>(a.vo[i]));
+  else if (a.dt == FNO_DTYPE_F16)
+    moments_chunk(t, base, static_cast<_Float16*>(a.mo[i]), static_cast<_Float16*>(a.vo[i]));
+  else
+    moments_chunk(t, base, static_cast<__bf16*>(a.mo[i]), static_cast<__bf16*>(a.vo[i]));
+}
+
+// v summed over the work-group's 256 threads in a fixed order.
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double red[4];
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_down(v, d);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
 // Sum of squares of each chunk of the gradients, in double: no fp32 gradient
 // overflows it, so the sum is finite exactly where every value is.
-__global__ __launch_bounds__(256) void grad_sq_kernel(AdamArgs a, double* part) {
-  __shared__ double red[256];
-  const int i = find_tensor(a.first, a.count, (int)blockIdx.x);
-  const AdamTensor& t = a.t[i];
-  const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * kChunk;
+template <typename G>
+__device__ __forceinline__ double square_sum(const G* g, int64_t base, int64_t n) {
+  using V = typename Vec4<G>::type;
+  constexpr int U = 8;
   double s = 0.0;
-  for (int64_t e = base + threadIdx.x; e < base + kChunk && e < t.n; e += 256) {
-    const double g = (double)load_as_float(t.g, e, t.gdt);
-    s += g * g;
+  int64_t b = base;
+  const int64_t end = base + kNormChunk < n ? base + kNormChunk : n;
+  for (; b + 1024 * U <= end; b += 1024 * U) {
+    V v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const V*>(g + b + 1024 * u + 4 * threadIdx.x);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = __builtin_fma((double)(float)v[u][j], (double)(float)v[u][j], s);
   }
-  red[threadIdx.x] = s;
-  __syncthreads();
-  for (int d = 128; d > 0; d >>= 1) {
-    if ((int)threadIdx.x < d) red[threadIdx.x] += red[threadIdx.x + d];
-    __syncthreads();
+  for (; b < end; b += 1024) {  // past the end: zeros
+    const V v = load4<V>(g, b + 4 * threadIdx.x, n);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = __builtin_fma((double)(float)v[j], (double)(float)v[j], s);
   }
-  if (threadIdx.x == 0) part[blockIdx.x] = red[0];
+  return s;
 }
 
-__global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int64_t n, double max_norm,
+__global__ __launch_bounds__(256) void grad_sq_kernel(AdamArgs a, double* part) {
+  const int i = find_tensor(a.first, a.count, (int)blockIdx.x);
+  const AdamTensor& t = a.t[i];
+  const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * kNormChunk;
+  double s;
+  if (t.gdt == FNO_DTYPE_F32) s = square_sum(static_cast<const float*>(t.g), base, t.n);
+  else if (t.gdt == FNO_DTYPE_F16) s = square_sum(static_cast<const _Float16*>(t.g), base, t.n);
+  else s = square_sum(static_cast<const __bf16*>(t.g), base, t.n);
+  s = block_sum(s);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int64_t n, double b1,
+                                                        double b2, double max_norm,
                                                         double inv_scale, fno_adamw_control* ctl) {
-  __shared__ double red[256];
   double s = 0.0;
   for (int64_t e = threadIdx.x; e < n; e += 256) s += part[e];
-  red[threadIdx.x] = s;
-  __syncthreads();
-  for (int d = 128; d > 0; d >>= 1) {
-    if ((int)threadIdx.x < d) red[threadIdx.x] += red[threadIdx.x + d];
-    __syncthreads();
-  }
+  const double sum = block_sum(s);
   if (threadIdx.x != 0) return;
-  const double sum = red[0], norm = sqrt(sum) * inv_scale;
+  const double norm = sqrt(sum) * inv_scale;
   const bool ok = sum <= 1.7976931348623157e308;  // false for inf and NaN
   ctl->grad_norm = (float)norm;
   ctl->grad_scale = (float)(norm > max_norm ? inv_scale * (max_norm / norm) : inv_scale);
   ctl->skip = ok ? 0 : 1;
-  ctl->step += ok ? 1 : 0;
-  ctl->skipped += ok ? 0 : 1;
+  if (!ok) {
+    ctl->skipped += 1;
+    return;
+  }
+  const int64_t t = ctl->step + 1;
+  ctl->step = t;
+  ctl->bias1 = 1.0 / (1.0 - int_pow(b1, t));
+  ctl->bias2 = 1.0 / sqrt(1.0 - int_pow(b2, t));
 }
 
 // --------------------------------------------------------------------------
@@ -281,6 +557,11 @@ bool check_states(const fno_adamw_tensor& t) {
                             : ok16(t.exp_avg_scale) && ok16(t.exp_avg_sq_scale);
 }
 
+bool check_hyper(const fno_adamw_desc* d) {
+  return d && d->lr >= 0.0 && d->lr <= 1.7e308 && d->beta1 >= 0.0 && d->beta1 < 1.0 &&
+         d->beta2 >= 0.0 && d->beta2 < 1.0 && d->eps >= 0.0 && d->eps <= 3.4e38;
+}
+
 bool check_tensor(const fno_adamw_tensor& t) {
   if (!check_grad(t) || !check_states(t)) return false;
   if (!(t.weight_decay >= 0.0f && t.weight_decay <= 3.4e38f)) return false;
@@ -289,13 +570,13 @@ bool check_tensor(const fno_adamw_tensor& t) {
 }
 
 // The next launch's tensors from list position *i on; returns its chunks.
-int64_t next_batch(const fno_adamw_tensor* t, int64_t count, int64_t* i, AdamArgs* a) {
+int64_t next_batch(const fno_adamw_tensor* t, int64_t count, int64_t chunk, int64_t* i, AdamArgs* a) {
   int64_t chunks = 0;
   a->count = 0;
   for (; *i < count && a->count < kBatch; ++*i) {
     const fno_adamw_tensor& x = t[*i];
     if (x.n == 0) continue;
-    const int64_t c = cdiv(x.n, kChunk);
+    const int64_t c = cdiv(x.n, chunk);
     if (a->count && chunks + c > kMaxGrid) break;
     a->t[a->count] = AdamTensor{x.param, x.master, x.grad, x.exp_avg, x.exp_avg_sq,
                                 x.exp_avg_scale, x.exp_avg_sq_scale, x.n, x.param_dtype,
@@ -307,19 +588,19 @@ int64_t next_batch(const fno_adamw_tensor* t, int64_t count, int64_t* i, AdamArg
   return chunks;
 }
 
-int64_t all_chunks(const fno_adamw_tensor* t, int64_t count) {
+int64_t norm_chunks(const fno_adamw_tensor* t, int64_t count) {
   int64_t c = 0;
-  for (int64_t i = 0; i < count; ++i) c += cdiv(t[i].n, kChunk);
+  for (int64_t i = 0; i < count; ++i) c += cdiv(t[i].n, kNormChunk);
   return c;
 }
 
 // Runs `launch(args, chunks, list index of the first tensor)` over the batches of a list.
 template <typename F>
-hipError_t over_batches(const fno_adamw_tensor* t, int64_t count, F launch) {
+hipError_t over_batches(const fno_adamw_tensor* t, int64_t count, int64_t chunk, F launch) {
   AdamArgs a;
   for (int64_t i = 0; i < count;) {
     const int64_t from = i;
-    const int64_t chunks = next_batch(t, count, &i, &a);
+    const int64_t chunks = next_batch(t, count, chunk, &i, &a);
     if (chunks == 0) continue;
     launch(a, chunks, from);
     const hipError_t e = hipGetLastError();
@@ -338,7 +619,7 @@ struct StepLaunch {
 
 hipError_t launch_step(void* ctx) {
   const StepLaunch& L = *static_cast<StepLaunch*>(ctx);
-  return over_batches(L.t, L.count, [&](const AdamArgs& a, int64_t chunks, int64_t) {
+  return over_batches(L.t, L.count, kChunk, [&](const AdamArgs& a, int64_t chunks, int64_t) {
     hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)chunks), dim3(256), 0, L.s, a, L.h, L.ctl);
   });
 }
@@ -346,7 +627,7 @@ hipError_t launch_step(void* ctx) {
 struct NormLaunch {
   const fno_adamw_tensor* t;
   int64_t count;
-  double max_norm, inv_scale;
+  double b1, b2, max_norm, inv_scale;
   fno_adamw_control* ctl;
   double* part;
   hipStream_t s;
@@ -356,13 +637,13 @@ hipError_t launch_norm(void* ctx) {
   const NormLaunch& L = *static_cast<NormLaunch*>(ctx);
   int64_t at = 0;
   const hipError_t e =
-      over_batches(L.t, L.count, [&](const AdamArgs& a, int64_t chunks, int64_t) {
+      over_batches(L.t, L.count, kNormChunk, [&](const AdamArgs& a, int64_t chunks, int64_t) {
         hipLaunchKernelGGL(grad_sq_kernel, dim3((unsigned)chunks), dim3(256), 0, L.s, a, L.part + at);
         at += chunks;
       });
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, L.s, L.part, at, L.max_norm,
-                     L.inv_scale, L.ctl);
+  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, L.s, L.part, at, L.b1, L.b2,
+                     L.max_norm, L.inv_scale, L.ctl);
   return hipGetLastError();
 }
 
@@ -379,7 +660,7 @@ hipError_t launch_moments(void* ctx) {
   const MomentLaunch& L = *static_cast<MomentLaunch*>(ctx);
   MomentArgs ma;
   ma.dt = L.dt;
-  return over_batches(L.t, L.count, [&](const AdamArgs& a, int64_t chunks, int64_t from) {
+  return over_batches(L.t, L.count, kChunk, [&](const AdamArgs& a, int64_t chunks, int64_t from) {
     ma.a = a;
     for (int64_t i = from, j = 0; j < a.count; ++i) {
       if (L.t[i].n == 0) continue;
@@ -405,14 +686,15 @@ extern "C" fno_status fno_grad_norm_workspace_size(const fno_adamw_tensor* t, in
   if (!check_list(t, count) || !bytes) return FNO_ERR_INVALID_ARGUMENT;
   for (int64_t i = 0; i < count; ++i)
     if (t[i].n < 0 || t[i].n > kMaxN) return FNO_ERR_INVALID_ARGUMENT;
-  *bytes = (size_t)(cdiv(all_chunks(t, count) * 8, 256) * 256 + 256);
+  *bytes = (size_t)(cdiv(norm_chunks(t, count) * 8, 256) * 256 + 256);
   return FNO_OK;
 }
 
-extern "C" fno_status fno_grad_norm(const fno_adamw_tensor* t, int64_t count, double max_norm,
-                                    double inv_loss_scale, fno_adamw_control* control, void* ws,
-                                    size_t ws_len, hipStream_t stream) {
-  if (!check_list(t, count) || !ok16(control)) return FNO_ERR_INVALID_ARGUMENT;
+extern "C" fno_status fno_grad_norm(const fno_adamw_desc* d, const fno_adamw_tensor* t,
+                                    int64_t count, double max_norm, double inv_loss_scale,
+                                    fno_adamw_control* control, void* ws, size_t ws_len,
+                                    hipStream_t stream) {
+  if (!check_hyper(d) || !check_list(t, count) || !ok16(control)) return FNO_ERR_INVALID_ARGUMENT;
   if (!(max_norm > 0.0) || !(inv_loss_scale > 0.0 && inv_loss_scale <= 1.7e308))
     return FNO_ERR_INVALID_ARGUMENT;
   for (int64_t i = 0; i < count; ++i)
@@ -422,24 +704,25 @@ extern "C" fno_status fno_grad_norm(const fno_adamw_tensor* t, int64_t count, do
   if (st != FNO_OK) return st;
   if (ws_len < need) return FNO_ERR_WORKSPACE_TOO_SMALL;
   if (!ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
-  NormLaunch L{t, count, max_norm, inv_loss_scale, control, static_cast<double*>(ws), stream};
+  NormLaunch L{t, count, d->beta1, d->beta2, max_norm, inv_loss_scale, control,
+               static_cast<double*>(ws), stream};
   return timed_status("grad_norm", stream, launch_norm, &L);
 }
 
 extern "C" fno_status fno_adamw_step(const fno_adamw_desc* d, const fno_adamw_tensor* t,
                                      int64_t count, int64_t step, const fno_adamw_control* control,
                                      hipStream_t stream) {
-  if (!d || !check_list(t, count)) return FNO_ERR_INVALID_ARGUMENT;
-  if (!(d->lr >= 0.0 && d->lr <= 1.7e308) || !(d->beta1 >= 0.0 && d->beta1 < 1.0) ||
-      !(d->beta2 >= 0.0 && d->beta2 < 1.0) || !(d->eps >= 0.0 && d->eps <= 3.4e38))
-    return FNO_ERR_INVALID_ARGUMENT;
+  if (!check_hyper(d) || !check_list(t, count)) return FNO_ERR_INVALID_ARGUMENT;
   if (control ? !ok16(control) : step < 1) return FNO_ERR_INVALID_ARGUMENT;
   for (int64_t i = 0; i < count; ++i)
     if (!check_tensor(t[i])) return FNO_ERR_INVALID_ARGUMENT;
   if (count == 0) return FNO_OK;
-  StepLaunch L{t, count, AdamHyper{d->lr, d->beta1, d->beta2, 0.0, 0.0, (float)d->eps, 1.0f},
-               control, stream};
-  if (!control) bias_correct(&L.h, step);
+  StepLaunch L{t, count, AdamHyper{d->lr, d->beta1, d->beta2, 0.0, 0.0, (float)d->eps}, control,
+               stream};
+  if (!control) {
+    L.h.bias1 = 1.0 / (1.0 - int_pow(d->beta1, step));
+    L.h.bias2 = 1.0 / std::sqrt(1.0 - int_pow(d->beta2, step));
+  }
   return timed_status("adamw_step", stream, launch_step, &L);
 }
 

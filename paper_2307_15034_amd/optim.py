@@ -90,8 +90,8 @@ class AdamW:
         if device_control:
             c = B.FnoAdamwControl(step=self.steps, lr_factor=1.0, grad_scale=1.0)
             self.control = torch.frombuffer(bytearray(bytes(c)), dtype=torch.uint8).to(self.device)
-            self._norm = self.control[16:20].view(torch.float32)
-            self._factor = self.control[28:32].view(torch.float32)
+            self._norm = self.control[32:36].view(torch.float32)[0]
+            self._factor = self.control[44:48].view(torch.float32)
             self._ws = torch.empty(B.fno_grad_norm_workspace_size(self._list, n),
                                    dtype=torch.uint8, device=self.device)
 
@@ -159,13 +159,13 @@ class AdamW:
     def clip_grads(self, max_norm: float = float("inf"), loss_scale: float = 1.0,
                    stream: Optional[int] = None) -> torch.Tensor:
         """The global norm of the gradients over `loss_scale` (returned, a
-        tensor of one element that later calls overwrite), and the next step's
+        scalar tensor that later calls overwrite), and the next step's
         gradient scale, step number and skip, on the device."""
         if self.control is None:
             raise ValueError("clip_grads needs device_control=True")
         if not loss_scale > 0:
             raise ValueError(f"loss_scale {loss_scale}, expected more than 0")
-        B.fno_grad_norm(self._list, len(self.params), max_norm, 1.0 / loss_scale,
+        B.fno_grad_norm(self.desc, self._list, len(self.params), max_norm, 1.0 / loss_scale,
                         self.control.data_ptr(), self._ws.data_ptr(), self._ws.numel(),
                         _stream_of(self.device, stream))
         return self._norm

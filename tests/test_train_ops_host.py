@@ -104,8 +104,8 @@ def test_grad_norm_refused():
                      ("inv_loss_scale", float("nan"), BAD), ("control", 0, BAD),
                      ("control", A + 8, BAD), ("ws", 0, BAD), ("ws", A + 8, BAD),
                      ("ws_bytes", n - 1, B.FNO_ERR_WORKSPACE_TOO_SMALL)):
-        assert B.fno_grad_norm(t, 1, **{**ok, k: v}, check=False) == st, (k, v)
-    assert B.fno_grad_norm(_list(grad=0), 1, **ok, check=False) == BAD
+        assert B.fno_grad_norm(OPT, t, 1, **{**ok, k: v}, check=False) == st, (k, v)
+    assert B.fno_grad_norm(OPT, _list(grad=0), 1, **ok, check=False) == BAD
     with pytest.raises(B.FnoError):
         B.fno_grad_norm_workspace_size(_list(n=-1), 1)
 
