@@ -132,15 +132,15 @@ struct NormArgs {
 
 // A group's statistics from its sums.
 struct Stat {
-  double mean, rstd;
+  float mean, rstd;
 };
 __device__ __forceinline__ Stat stat_of(const NormArgs& a, const Sums& t) {
   const double m = (double)a.P * a.Cg;
   const double mean = t.s / m, var = __builtin_fmax(t.q / m - mean * mean, 0.0);
   // a value that is not finite makes the sum of squares so
   const bool ok = t.q <= 1.7976931348623157e308;
-  const double nan = __builtin_nan("");
-  return Stat{ok ? mean : nan, ok ? 1.0 / sqrt(var + (double)a.eps) : nan};
+  const float nan = __builtin_nanf("");
+  return Stat{ok ? (float)mean : nan, ok ? (float)(1.0 / sqrt(var + (double)a.eps)) : nan};
 }
 
 __device__ __forceinline__ Sums add(const Sums& a, const Sums& b) { return Sums{a.s + b.s, a.q + b.q}; }
@@ -206,22 +206,28 @@ __device__ __forceinline__ void add_value(Sums* t, float x) {
 // --------------------------------------------------------------------------
 // Channels last, flat
 // --------------------------------------------------------------------------
-// A thread's vectors of a chunk: first, count (full ones), and whether the
-// sample's last, partial vector is its next.
+// A chunk of a sample, `size` vectors from `base` on (an element of the
+// sample), and this thread's vectors of it: threadIdx, threadIdx + A, ...:
+// `count` full ones, then perhaps the sample's last, partial one (`tail`).
 struct Mine {
-  int64_t first;
+  int64_t base;
   int count;
   bool tail;
 };
 __device__ __forceinline__ Mine my_vectors(const NormArgs& a, int64_t chunk, int64_t size, int vec) {
-  const int64_t full = a.R / vec, lo = chunk * size + threadIdx.x;
-  Mine m{lo, 0, false};
+  const int64_t full = a.R / vec, lo = chunk * size;
+  Mine m{lo * vec, 0, false};
   if ((int)threadIdx.x >= a.A) return m;
-  const int64_t end = chunk * size + size < full ? chunk * size + size : full;
-  if (lo < end) m.count = (int)((end - lo + a.A - 1) / a.A);
-  const int64_t next = lo + (int64_t)m.count * a.A;
-  m.tail = a.R % vec != 0 && next == full && next < chunk * size + size;
+  const int here = (int)(lo + size < full ? size : full > lo ? full - lo : 0);
+  if ((int)threadIdx.x < here) m.count = (here - (int)threadIdx.x + a.A - 1) / a.A;
+  const int next = (int)threadIdx.x + m.count * a.A;
+  m.tail = a.R % vec != 0 && lo + next == full && next < size;
   return m;
+}
+// The element of the chunk where this thread's vector k starts (past its last:
+// its last).  Chunks hold less than 2^31 elements.
+__device__ __forceinline__ uint32_t my_at(const NormArgs& a, const Mine& m, int k, int vec) {
+  return (uint32_t)(((int)threadIdx.x + (k < m.count ? k : m.count - 1) * a.A) * vec);
 }
 
 // The channel of element j of thread t's vectors.
@@ -232,10 +238,10 @@ __device__ __forceinline__ int my_channel(const NormArgs& a, int j, int vec) {
 // UNI: a vector's channels are of one group (and C is a multiple of a vector).
 template <typename T, bool UNI>
 __device__ __forceinline__ void flat_stats(const NormArgs& a, int64_t unit, Sums* lds) {  // [A][E]
-  constexpr int V = kVec<T>, UN = 4, E = UNI ? 1 : V;
+  constexpr int V = kVec<T>, UN = 8, E = UNI ? 1 : V;
   const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
-  const T* x = static_cast<const T*>(a.x) + b * a.R;
   const Mine m = my_vectors(a, chunk, a.v1, V);
+  const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
   Sums acc[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) acc[j] = Sums{0.0, 0.0};
@@ -243,7 +249,7 @@ __device__ __forceinline__ void flat_stats(const NormArgs& a, int64_t unit, Sums
     Vec<T, V> v[UN];
 #pragma unroll
     for (int u = 0; u < UN; ++u)
-      v[u] = load_vec<T, V>(x + (m.first + (int64_t)(k + u < m.count ? k + u : m.count - 1) * a.A) * V);
+      v[u] = load_vec<T, V>(x + my_at(a, m, k + u, V));
 #pragma unroll
     for (int u = 0; u < UN; ++u)
       if (k + u < m.count)
@@ -254,9 +260,9 @@ __device__ __forceinline__ void flat_stats(const NormArgs& a, int64_t unit, Sums
 #pragma unroll
     for (int j = 0; j < E; ++j) {
       if (m.tail) {
-        const int64_t at = (m.first + (int64_t)m.count * a.A) * V;
+        const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
         for (int i = UNI ? 0 : j; i < (UNI ? V : j + 1); ++i)
-          if (at + i < a.R) add_value(&acc[j], (float)x[at + i]);
+          if (m.base + at + i < a.R) add_value(&acc[j], (float)x[at + i]);
       }
       lds[threadIdx.x * E + j] = acc[j];
     }
@@ -275,12 +281,13 @@ __global__ __launch_bounds__(NT) void flat_stats_kernel(NormArgs a) {
   }
 }
 
-// The sample's group sums into LDS.
-__device__ __forceinline__ void load_groups(const NormArgs& a, int64_t b, Sums* lds) {
+// Each of a sample's groups joined, f(group, sum) into LDS.
+template <typename V2, typename F>
+__device__ __forceinline__ void load_groups(const NormArgs& a, int64_t b, V2* lds, F f) {
   const Sums* p = a.collapse ? a.joined + b * a.G : a.part + b * a.G * a.n;
   const int n = a.collapse ? 1 : a.n;
   group_sums(a.G, n, [&](int g, int i) { return p[(int64_t)g * n + i]; },
-             [&](int g, const Sums& t) { lds[g] = t; });
+             [&](int g, const Sums& t) { lds[g] = f(g, t); });
   __syncthreads();
 }
 
@@ -290,44 +297,45 @@ struct Line {
   float mu, k, be;
 };
 __device__ __forceinline__ Line line_of(const NormArgs& a, const Stat& st, int c) {
-  return Line{(float)st.mean, (float)(st.rstd * (a.gamma ? (double)a.gamma[c] : 1.0)),
-              a.beta ? a.beta[c] : 0.0f};
+  return Line{st.mean, a.gamma ? st.rstd * a.gamma[c] : st.rstd, a.beta ? a.beta[c] : 0.0f};
 }
 __device__ __forceinline__ float on_line(const Line& l, float x) {
   return __builtin_fmaf(x - l.mu, l.k, l.be);
 }
 
 __device__ __forceinline__ void write_stat(const NormArgs& a, int64_t bg, const Stat& st) {
-  a.stats[2 * bg] = (float)st.mean;
-  a.stats[2 * bg + 1] = (float)st.rstd;
+  a.stats[2 * bg] = st.mean;
+  a.stats[2 * bg + 1] = st.rstd;
 }
 
 template <typename T, int ACT, bool UNI>
-__device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Sums* lds) {  // [G]
+__device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* lds) {  // [G]
   constexpr int V = kVec<T>, UN = 4;
   const int64_t b = unit / a.n2, chunk = unit - b * a.n2;
-  load_groups(a, b, lds);
-  if (chunk == 0 && a.stats)
-    for (int g = threadIdx.x; g < a.G; g += NT) write_stat(a, b * a.G + g, stat_of(a, lds[g]));
+  load_groups(a, b, lds, [&](int g, const Sums& t) {
+    const Stat st = stat_of(a, t);
+    if (chunk == 0 && a.stats) write_stat(a, b * a.G + g, st);
+    return st;
+  });
   const bool res = a.res != nullptr;
-  const T* x = static_cast<const T*>(a.x) + b * a.R;
-  const T* r = static_cast<const T*>(a.res) + (res ? b * a.R : 0);
-  T* out = static_cast<T*>(a.out) + b * a.R;
   const Mine m = my_vectors(a, chunk, a.v2, V);
+  const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
+  const T* r = res ? static_cast<const T*>(a.res) + b * a.R + m.base : nullptr;
+  T* out = static_cast<T*>(a.out) + b * a.R + m.base;
   if (!m.count && !m.tail) return;
   Line l[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const int c = my_channel(a, j, V);
-    l[j] = line_of(a, stat_of(a, lds[c / a.Cg]), c);
+    l[j] = line_of(a, lds[c / a.Cg], c);
     if (UNI && j) l[j].mu = l[0].mu;
   }
   for (int k = 0; k < m.count; k += UN) {
     Vec<T, V> v[UN], rv[UN];
-    int64_t at[UN];
+    uint32_t at[UN];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      at[u] = (m.first + (int64_t)(k + u < m.count ? k + u : m.count - 1) * a.A) * V;
+      at[u] = my_at(a, m, k + u, V);
       v[u] = load_vec<T, V>(x + at[u]);
     }
     if (res)
@@ -349,10 +357,10 @@ __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Sums* 
       }
   }
   if (m.tail) {
-    const int64_t at = (m.first + (int64_t)m.count * a.A) * V;
+    const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (at + j < a.R) {
+      if (m.base + at + j < a.R) {
         float y = act_f<ACT>(on_line(l[j], (float)x[at + j]));
         if (res) y += (float)r[at + j];
         out[at + j] = (T)y;
@@ -363,7 +371,7 @@ template <typename T, int ACT, bool UNI>
 __global__ __launch_bounds__(NT) void flat_fwd_kernel(NormArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += gridDim.x) {
-    flat_fwd<T, ACT, UNI>(a, u, reinterpret_cast<Sums*>(smem));
+    flat_fwd<T, ACT, UNI>(a, u, reinterpret_cast<Stat*>(smem));
     __syncthreads();
   }
 }
@@ -376,11 +384,16 @@ __device__ __forceinline__ Coef bwd_coef(const NormArgs& a, int64_t b, int c) {
   const float* st = a.stats_in + 2 * (b * a.G + c / a.Cg);
   return Coef{st[0], st[1], a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f};
 }
+// (Both passes form h alike: in a group whose values hardly differ gx is the
+// small difference of large terms, and would show any difference of the two.)
 template <int ACT>
 __device__ __forceinline__ void bwd_terms(const Coef& k, float x, float g, float* h, float* xh) {
   *xh = (x - k.mu) * k.rs;
   *h = g * act_grad_f<ACT>(__builtin_fmaf(*xh, k.ga, k.be));
 }
+// A sum of h where the statistics are not finite: not a number (h itself may
+// be finite there).
+__device__ __forceinline__ float poisoned(const Coef& k, float s) { return __builtin_fmaf(0.0f, k.rs, s); }
 // gx = rs (ga h - a - xh d).
 struct Means {
   float a, d;
@@ -398,9 +411,9 @@ template <typename T, int ACT, bool UNI>
 __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float2* lds, Sums* ch) {
   constexpr int V = kVec<T>, UN = 2;
   const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
-  const T* x = static_cast<const T*>(a.x) + b * a.R;
-  const T* g = static_cast<const T*>(a.gout) + b * a.R;
   const Mine m = my_vectors(a, chunk, a.v1, V);
+  const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
+  const T* g = static_cast<const T*>(a.gout) + b * a.R + m.base;
   if ((int)threadIdx.x < a.A) {
     Coef k[V];
     float s[V], q[V];
@@ -417,7 +430,7 @@ __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float
       Vec<T, V> xv[UN], gv[UN];
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
-        const int64_t at = (m.first + (int64_t)(i + u < m.count ? i + u : m.count - 1) * a.A) * V;
+        const uint32_t at = my_at(a, m, i + u, V);
         xv[u] = load_vec<T, V>(x + at);
         gv[u] = load_vec<T, V>(g + at);
       }
@@ -433,10 +446,10 @@ __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float
           }
     }
     if (m.tail) {
-      const int64_t at = (m.first + (int64_t)m.count * a.A) * V;
+      const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (at + j < a.R) {
+        if (m.base + at + j < a.R) {
           float h, xh;
           bwd_terms<ACT>(k[j], (float)x[at + j], (float)g[at + j], &h, &xh);
           s[j] += h;
@@ -444,7 +457,7 @@ __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float
         }
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) lds[threadIdx.x * V + j] = make_float2(s[j], q[j]);
+    for (int j = 0; j < V; ++j) lds[threadIdx.x * V + j] = make_float2(poisoned(k[j], s[j]), q[j]);
   }
   __syncthreads();
   // element f = V t + j of the threads is channel f mod C's
@@ -484,14 +497,14 @@ __device__ __forceinline__ void param_grads(const NormArgs& a, int c) {
 }
 
 template <typename T, int ACT, bool UNI>
-__device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Sums* lds) {  // [G]
+__device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means* lds) {  // [G]
   constexpr int V = kVec<T>, UN = 2;
   const int64_t b = unit / a.n2, chunk = unit - b * a.n2;
-  load_groups(a, b, lds);
-  const T* x = static_cast<const T*>(a.x) + b * a.R;
-  const T* g = static_cast<const T*>(a.gout) + b * a.R;
-  T* out = static_cast<T*>(a.out) + b * a.R;
+  load_groups(a, b, lds, [&](int, const Sums& t) { return means_of(a, t); });
   const Mine m = my_vectors(a, chunk, a.v2, V);
+  const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
+  const T* g = static_cast<const T*>(a.gout) + b * a.R + m.base;
+  T* out = static_cast<T*>(a.out) + b * a.R + m.base;
   if (!m.count && !m.tail) return;
   Coef k[V];
   Means mn[V];
@@ -499,7 +512,7 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Sums* 
   for (int j = 0; j < V; ++j) {
     const int c = my_channel(a, j, V);
     k[j] = bwd_coef(a, b, c);
-    mn[j] = means_of(a, lds[c / a.Cg]);
+    mn[j] = lds[c / a.Cg];
     if (UNI && j) {
       k[j].mu = k[0].mu;
       k[j].rs = k[0].rs;
@@ -508,10 +521,10 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Sums* 
   }
   for (int i = 0; i < m.count; i += UN) {
     Vec<T, V> xv[UN], gv[UN];
-    int64_t at[UN];
+    uint32_t at[UN];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      at[u] = (m.first + (int64_t)(i + u < m.count ? i + u : m.count - 1) * a.A) * V;
+      at[u] = my_at(a, m, i + u, V);
       xv[u] = load_vec<T, V>(x + at[u]);
       gv[u] = load_vec<T, V>(g + at[u]);
     }
@@ -529,10 +542,10 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Sums* 
       }
   }
   if (m.tail) {
-    const int64_t at = (m.first + (int64_t)m.count * a.A) * V;
+    const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (at + j < a.R) {
+      if (m.base + at + j < a.R) {
         float h, xh;
         bwd_terms<ACT>(k[j], (float)x[at + j], (float)g[at + j], &h, &xh);
         out[at + j] = (T)bwd_gx(k[j], mn[j], h, xh);
@@ -545,7 +558,7 @@ __global__ __launch_bounds__(NT) void flat_bwd_kernel(NormArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   if ((int)blockIdx.x >= a.main) return param_grads(a, (int)blockIdx.x - a.main);
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += a.main) {
-    flat_bwd<T, ACT, UNI>(a, u, reinterpret_cast<Sums*>(smem));
+    flat_bwd<T, ACT, UNI>(a, u, reinterpret_cast<Means*>(smem));
     __syncthreads();
   }
 }
@@ -680,8 +693,9 @@ __global__ __launch_bounds__(NT) void wide_sums_kernel(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const int64_t at = (w.b * a.C + w.c + j) * a.n1 + w.chunk;
-      a.chan[at] = Sums{s[j], q[j]};
-      a.part[at] = Sums{(double)k[j].ga * s[j], (double)k[j].ga * q[j]};
+      const double sj = poisoned(k[j], s[j]);
+      a.chan[at] = Sums{sj, q[j]};
+      a.part[at] = Sums{(double)k[j].ga * sj, (double)k[j].ga * q[j]};
     }
   }
 }
@@ -846,7 +860,7 @@ __global__ __launch_bounds__(NT) void first_sums_kernel(NormArgs a) {
           for (int j = 0; j < V; ++j) one((float)xv.e[j], (float)gv.e[j]);
         },
         [&](int e) { one((float)x[e], (float)g[e]); });
-    const Sums t = team_sum<TEAM>(Sums{sh, sx});
+    const Sums t = team_sum<TEAM>(Sums{poisoned(k, sh), sx});
     if ((threadIdx.x & (TEAM - 1)) == 0) {
       a.chan[u] = t;
       a.part[u] = Sums{(double)k.ga * t.s, (double)k.ga * t.q};
@@ -954,8 +968,8 @@ NormPlan plan_of(const fno_norm_desc& d) {
     a.A = (int)(NT / L * L);
     p.uni = a.C % V == 0 && a.Cg % V == 0;
     const int64_t nv = cdiv(a.R, V), room = std::max<int64_t>(1, nv / ((int64_t)a.A * 4));
-    const int64_t want = std::max<int64_t>(1, kFill / a.B);
-    a.v1 = a.v2 = rup(cdiv(nv, std::min(want, room)), a.A);
+    const int64_t want = std::max<int64_t>(std::max<int64_t>(1, kFill / a.B), cdiv(nv, (int64_t)1 << 26));
+    a.v1 = a.v2 = rup(cdiv(nv, std::min(want, room)), a.A);  // room: four vectors a thread
     a.n1 = a.n2 = (int)cdiv(nv, a.v1);
     a.n = a.nc = a.n1;
     a.collapse = (int64_t)a.n * a.G > 2048;
@@ -1032,7 +1046,7 @@ void launch_fwd_t(NormLaunch& L) {
   a.u1 = L.p.units2;
   if (L.p.route == FLAT) {
     auto k = L.p.uni ? flat_fwd_kernel<T, ACT, true> : flat_fwd_kernel<T, ACT, false>;
-    hipLaunchKernelGGL(k, dim3(grid_of(a.u1)), dim3(NT), a.G * sizeof(Sums), L.s, a);
+    hipLaunchKernelGGL(k, dim3(grid_of(a.u1)), dim3(NT), a.G * sizeof(Stat), L.s, a);
   } else if (L.p.route == WIDE) {
     auto k = L.p.vec == 1 ? wide_fwd_kernel<T, 1> : wide_fwd_kernel<T, kVec<T>>;
     hipLaunchKernelGGL(k, dim3(grid_of(a.u1)), dim3(NT), 0, L.s, a);
@@ -1057,7 +1071,7 @@ void launch_bwd_t(NormLaunch& L) {
     a.u1 = L.p.units2;
     a.main = (int)grid_of(a.u1);
     auto k2 = L.p.uni ? flat_bwd_kernel<T, ACT, true> : flat_bwd_kernel<T, ACT, false>;
-    hipLaunchKernelGGL(k2, dim3(a.main + extra), dim3(NT), a.G * sizeof(Sums), L.s, a);
+    hipLaunchKernelGGL(k2, dim3(a.main + extra), dim3(NT), a.G * sizeof(Stat), L.s, a);
   } else if (L.p.route == WIDE) {
     auto k1 = L.p.vec == 1 ? wide_sums_kernel<T, 1> : wide_sums_kernel<T, kVec<T>>;
     hipLaunchKernelGGL(k1, dim3(grid_of(a.u1)), dim3(NT), 0, L.s, a);
