@@ -19,7 +19,8 @@ namespace {
 constexpr int kBatch = FNO_ADAMW_LAUNCH_TENSORS;
 constexpr int kBlk = FNO_ADAMW_BLOCK;
 constexpr int64_t kChunk = 2048;             // elements of a work-group of the step
-constexpr int64_t kNormChunk = 16384;        // elements of a work-group of the norm
+constexpr int64_t kNormChunk = 8192;         // elements of a work-group of the norm
+constexpr int64_t kMomentChunk = 4096;       // elements of a work-group that reads moments out
 constexpr int64_t kMaxN = (int64_t)1 << 34;  // elements of a tensor
 constexpr int64_t kMaxGrid = (int64_t)1 << 23;  // work-groups of a launch
 
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a, AdamHyper h,
   }
 }
 
-// 8-bit moments read out, four elements per thread at a time.
+// 8-bit moments read out.
 struct MomentArgs {
   AdamArgs a;
   void* mo[kBatch];
@@ -429,32 +430,51 @@ struct MomentArgs {
   int32_t dt;
 };
 
+// Eight elements of a thread at a time, so that a 16-bit result is stored in
+// whole 16-byte pieces; all of a chunk's loads in flight at once.
 template <typename T>
 __device__ __forceinline__ void moments_chunk(const AdamTensor& t, int64_t base, T* mo, T* vo) {
-  constexpr int U = (int)kChunk / 1024;
-  using V = typename Vec4<T>::type;
+  constexpr int U = (int)kMomentChunk / 2048;
+  typedef T V __attribute__((ext_vector_type(8)));
+  typedef int8_t C __attribute__((ext_vector_type(8)));
+  typedef uint8_t D __attribute__((ext_vector_type(8)));
+  const int8_t* pm = static_cast<const int8_t*>(t.m);
+  const uint8_t* pv = static_cast<const uint8_t*>(t.v);
+  if (base + kMomentChunk > t.n) {
+    for (int64_t e = base + threadIdx.x; e < t.n; e += 256) {
+      mo[e] = rounded<T>(decode_m(t.ms[e / kBlk], pm[e]));
+      vo[e] = rounded<T>(decode_v(t.vs[e / kBlk], pv[e]));
+    }
+    return;
+  }
+  const int64_t e0 = base + 8 * threadIdx.x;
+  C qm[U];
+  D qv[U];
+  float a[U], b[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t e = base + 1024 * u + 4 * threadIdx.x;
-    if (e >= t.n) return;
-    const c4 qm = load4<c4>(static_cast<int8_t*>(t.m), e, t.n);
-    const u4 qv = load4<u4>(static_cast<uint8_t*>(t.v), e, t.n);
-    const float a = t.ms[e / kBlk], b = t.vs[e / kBlk];
+    qm[u] = *reinterpret_cast<const C*>(pm + e0 + 2048 * u);
+    qv[u] = *reinterpret_cast<const D*>(pv + e0 + 2048 * u);
+    a[u] = t.ms[(e0 + 2048 * u) / kBlk];
+    b[u] = t.vs[(e0 + 2048 * u) / kBlk];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
     V m, v;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      m[j] = rounded<T>(decode_m(a, qm[j]));
-      v[j] = rounded<T>(decode_v(b, qv[j]));
+    for (int j = 0; j < 8; ++j) {
+      m[j] = rounded<T>(decode_m(a[u], qm[u][j]));
+      v[j] = rounded<T>(decode_v(b[u], qv[u][j]));
     }
-    store4(mo, e, t.n, m);
-    store4(vo, e, t.n, v);
+    *reinterpret_cast<V*>(mo + e0 + 2048 * u) = m;
+    *reinterpret_cast<V*>(vo + e0 + 2048 * u) = v;
   }
 }
 
 __global__ __launch_bounds__(256) void moments_kernel(MomentArgs a) {
   const int i = find_tensor(a.a.first, a.a.count, (int)blockIdx.x);
   const AdamTensor& t = a.a.t[i];
-  const int64_t base = (int64_t)((int)blockIdx.x - a.a.first[i]) * kChunk;
+  const int64_t base = (int64_t)((int)blockIdx.x - a.a.first[i]) * kMomentChunk;
   if (a.dt == FNO_DTYPE_F32)
     moments_chunk(t, base, static_cast<float*>(a.mo[i]), static_cast<float*>(a.vo[i]));
   else if (a.dt == FNO_DTYPE_F16)
@@ -463,14 +483,18 @@ __global__ __launch_bounds__(256) void moments_kernel(MomentArgs a) {
     moments_chunk(t, base, static_cast<__bf16*>(a.mo[i]), static_cast<__bf16*>(a.vo[i]));
 }
 
-// v summed over the work-group's 256 threads in a fixed order.
+// v summed over the work-group's THREADS threads in a fixed order.
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v) {
-  __shared__ double red[4];
+  __shared__ double red[THREADS / 64];
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v += __shfl_down(v, d);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) s += red[i];
+  return s;
 }
 
 // Sum of squares of each chunk of the gradients, in double: no fp32 gradient
@@ -507,16 +531,17 @@ __global__ __launch_bounds__(256) void grad_sq_kernel(AdamArgs a, double* part) 
   if (t.gdt == FNO_DTYPE_F32) s = square_sum(static_cast<const float*>(t.g), base, t.n);
   else if (t.gdt == FNO_DTYPE_F16) s = square_sum(static_cast<const _Float16*>(t.g), base, t.n);
   else s = square_sum(static_cast<const __bf16*>(t.g), base, t.n);
-  s = block_sum(s);
+  s = block_sum<256>(s);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int64_t n, double b1,
+__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* part, int64_t n, double b1,
                                                         double b2, double max_norm,
                                                         double inv_scale, fno_adamw_control* ctl) {
   double s = 0.0;
-  for (int64_t e = threadIdx.x; e < n; e += 256) s += part[e];
-  const double sum = block_sum(s);
+#pragma unroll 8
+  for (int64_t e = threadIdx.x; e < n; e += 1024) s += part[e];
+  const double sum = block_sum<1024>(s);
   if (threadIdx.x != 0) return;
   const double norm = sqrt(sum) * inv_scale;
   const bool ok = sum <= 1.7976931348623157e308;  // false for inf and NaN
@@ -642,7 +667,7 @@ hipError_t launch_norm(void* ctx) {
         at += chunks;
       });
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, L.s, L.part, at, L.b1, L.b2,
+  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, L.s, L.part, at, L.b1, L.b2,
                      L.max_norm, L.inv_scale, L.ctl);
   return hipGetLastError();
 }
@@ -660,7 +685,7 @@ hipError_t launch_moments(void* ctx) {
   const MomentLaunch& L = *static_cast<MomentLaunch*>(ctx);
   MomentArgs ma;
   ma.dt = L.dt;
-  return over_batches(L.t, L.count, kChunk, [&](const AdamArgs& a, int64_t chunks, int64_t from) {
+  return over_batches(L.t, L.count, kMomentChunk, [&](const AdamArgs& a, int64_t chunks, int64_t from) {
     ma.a = a;
     for (int64_t i = from, j = 0; j < a.count; ++i) {
       if (L.t[i].n == 0) continue;

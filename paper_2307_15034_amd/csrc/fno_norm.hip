@@ -63,29 +63,35 @@ __device__ __forceinline__ void store_vec(T* p, const Vec<T, W>& v) {
 // --------------------------------------------------------------------------
 // Activations
 // --------------------------------------------------------------------------
-// Half of erfc(|z| / sqrt 2) by Abramowitz & Stegun 7.1.26 (absolute error at
-// most 0.75e-7), and exp(-z^2 / 2).
-__device__ __forceinline__ float half_erfc(float z, float* e) {
+// GELU z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt 2) / 2, with half of erfc by
+// Abramowitz & Stegun 7.1.26 (absolute error at most 0.75e-7).
+__device__ __forceinline__ float gelu_of(float z) {
   const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.23164189f, 1.0f));
   float p = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);
   p = __builtin_fmaf(t, p, 0.7107068705f);
   p = __builtin_fmaf(t, p, -0.142248368f);
   p = __builtin_fmaf(t, p, 0.127414796f);
-  *e = __builtin_amdgcn_exp2f(z * (z * -0.72134752044448f));
-  return p * t * *e;
+  const float e = __builtin_amdgcn_exp2f(z * (z * -0.72134752044448f));
+  return __builtin_fmaf(-__builtin_fabsf(z), p * t * e, __builtin_fmaxf(z, 0.0f));
 }
-// z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt 2) / 2.
-__device__ __forceinline__ float gelu_of(float z) {
-  float e;
-  const float h = half_erfc(z, &e);
-  return __builtin_fmaf(-__builtin_fabsf(z), h, __builtin_fmaxf(z, 0.0f));
-}
-// Phi(z) + z phi(z), Phi = 1/2 + sign(z) (1/2 - erfc / 2).
+// Its derivative Phi(z) + z phi(z) as 1/2 + z P(z^2) / Q(z^2) for |z| <= 5.6,
+// constant beyond: a rational fit of degrees (5, 5) to the definition (least
+// squares, reweighted to near the minimax of 1.1e-7), within 3.3e-7 of it
+// everywhere in float.  One reciprocal and no exponential: 18 operations' time
+// against 22 through erfc and exp(-z^2 / 2), where the passes are bound by it.
 __device__ __forceinline__ float gelu_grad_of(float z) {
-  float e;
-  const float h = half_erfc(z, &e);
-  const float phi = 0.5f + __builtin_copysignf(0.5f - h, z);
-  return __builtin_fmaf(z * 0.39894228040143268f, e, phi);
+  const float c = __builtin_amdgcn_fmed3f(z, -5.6f, 5.6f), t = c * c;
+  float p = __builtin_fmaf(t, 1.921672664e-07f, 3.589928644e-05f);
+  p = __builtin_fmaf(t, p, 1.975132363e-05f);
+  p = __builtin_fmaf(t, p, 1.422606847e-02f);
+  p = __builtin_fmaf(t, p, -3.097535923e-02f);
+  p = __builtin_fmaf(t, p, 7.978853454e-01f);
+  float q = __builtin_fmaf(t, 8.928170334e-06f, 1.920517995e-04f);
+  q = __builtin_fmaf(t, q, 3.522637464e-03f);
+  q = __builtin_fmaf(t, q, 4.098374084e-02f);
+  q = __builtin_fmaf(t, q, 2.945195774e-01f);
+  q = __builtin_fmaf(t, q, 1.0f);
+  return __builtin_fmaf(c * p, __builtin_amdgcn_rcpf(q), 0.5f);
 }
 
 template <int ACT>
@@ -116,10 +122,9 @@ struct NormArgs {
   int collapse;          // part is joined by a launch of its own
   int act;
   float eps;
-  // flat: L, A as above; vectors of a chunk (a multiple of A) and chunks of a
-  // sample, in the first and in the second pass
-  int L, A, n1, n2;
-  int64_t v1, v2;
+  // flat: L, A as above; vectors of a chunk (a multiple of A), chunks of a sample
+  int L, A, n1;
+  int64_t v1;
   // wide: rows of a chunk, column blocks, chunks (n1)
   // first: elements of a segment, segments of a plane (n1)
   int64_t rows;
@@ -203,6 +208,53 @@ __device__ __forceinline__ void add_value(Sums* t, float x) {
   t->q = __builtin_fma(d, d, t->q);
 }
 
+// A thread's items 0 .. count - 1, loaded ahead of their use: the first UN when
+// the stream is made (before what the use needs is worked out), then the next
+// UN while UN are used.  The loads stand outside every condition but that there
+// are items; inside one the compiler moves them next to their use.  An item is
+// loaded before any item from it on is used, so results may overwrite what was
+// loaded.
+template <int UN, typename Load>
+struct Stream {
+  int count;
+  Load load;
+  decltype(load(0)) cur[UN];
+  __device__ __forceinline__ Stream(int n, Load l) : count(n), load(l) {
+    if (count > 0)
+#pragma unroll
+      for (int u = 0; u < UN; ++u) cur[u] = load(u < count ? u : count - 1);
+  }
+  // use(item k, k) for each
+  template <typename Use>
+  __device__ __forceinline__ void run(Use use) {
+    if (count <= 0) return;
+    decltype(load(0)) next[UN];
+    int k = 0;
+#pragma unroll 2
+    for (; k + UN <= count; k += UN) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u) next[u] = load(k + UN + u < count ? k + UN + u : count - 1);
+#pragma unroll
+      for (int u = 0; u < UN; ++u) use(cur[u], k + u);
+#pragma unroll
+      for (int u = 0; u < UN; ++u) cur[u] = next[u];
+    }
+#pragma unroll
+    for (int u = 0; u < UN - 1; ++u)
+      if (k + u < count) use(cur[u], k + u);
+  }
+};
+template <int UN, typename Load>
+__device__ __forceinline__ Stream<UN, Load> stream(int count, Load load) {
+  return Stream<UN, Load>(count, load);
+}
+
+// Vectors of x and of a second tensor.
+template <typename T, int W>
+struct Pair {
+  Vec<T, W> x, y;
+};
+
 // --------------------------------------------------------------------------
 // Channels last, flat
 // --------------------------------------------------------------------------
@@ -224,38 +276,44 @@ __device__ __forceinline__ Mine my_vectors(const NormArgs& a, int64_t chunk, int
   m.tail = a.R % vec != 0 && lo + next == full && next < size;
   return m;
 }
-// The element of the chunk where this thread's vector k starts (past its last:
-// its last).  Chunks hold less than 2^31 elements.
-__device__ __forceinline__ uint32_t my_at(const NormArgs& a, const Mine& m, int k, int vec) {
-  return (uint32_t)(((int)threadIdx.x + (k < m.count ? k : m.count - 1) * a.A) * vec);
+// The element of the chunk where this thread's vector k starts.  Chunks hold
+// less than 2^31 elements.
+__device__ __forceinline__ uint32_t my_at(const NormArgs& a, int k, int vec) {
+  return (uint32_t)(((int)threadIdx.x + k * a.A) * vec);
 }
 
-// The channel of element j of thread t's vectors.
-__device__ __forceinline__ int my_channel(const NormArgs& a, int j, int vec) {
-  return (vec * ((int)threadIdx.x % a.L) + j) % a.C;
+// f(j, channel, group) for the elements of this thread's vectors.
+template <int V, bool UNI, typename F>
+__device__ __forceinline__ void my_channels(const NormArgs& a, F f) {
+  int c = V * ((int)threadIdx.x % a.L);
+  if (!UNI) c %= a.C;
+  int g = c / a.Cg, left = (g + 1) * a.Cg - c;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    f(j, c, g);
+    ++c;
+    if (!UNI && --left == 0) {
+      left = a.Cg;
+      if (++g == a.G) g = c = 0;
+    }
+  }
 }
 
 // UNI: a vector's channels are of one group (and C is a multiple of a vector).
 template <typename T, bool UNI>
 __device__ __forceinline__ void flat_stats(const NormArgs& a, int64_t unit, Sums* lds) {  // [A][E]
-  constexpr int V = kVec<T>, UN = 8, E = UNI ? 1 : V;
+  constexpr int V = kVec<T>, UN = 4, E = UNI ? 1 : V;
   const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
   const Mine m = my_vectors(a, chunk, a.v1, V);
   const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
   Sums acc[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) acc[j] = Sums{0.0, 0.0};
-  for (int k = 0; k < m.count; k += UN) {
-    Vec<T, V> v[UN];
+  stream<UN>(m.count, [&](int k) { return load_vec<T, V>(x + my_at(a, k, V)); })
+      .run([&](const Vec<T, V>& v, int) {
 #pragma unroll
-    for (int u = 0; u < UN; ++u)
-      v[u] = load_vec<T, V>(x + my_at(a, m, k + u, V));
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-      if (k + u < m.count)
-#pragma unroll
-        for (int j = 0; j < V; ++j) add_value(&acc[UNI ? 0 : j], (float)v[u].e[j]);
-  }
+        for (int j = 0; j < V; ++j) add_value(&acc[UNI ? 0 : j], (float)v.e[j]);
+      });
   if ((int)threadIdx.x < a.A) {
 #pragma unroll
     for (int j = 0; j < E; ++j) {
@@ -291,6 +349,16 @@ __device__ __forceinline__ void load_groups(const NormArgs& a, int64_t b, V2* ld
   __syncthreads();
 }
 
+// x - mu.  The factor is one; it is hidden from the compiler so that the fp16
+// conversion folds into the multiply-add.
+__device__ __forceinline__ float less(float x, float mu) { return x - mu; }
+__device__ __forceinline__ float less(_Float16 x, float mu) {
+  float one = 1.0f;
+  asm("" : "+s"(one));
+  return __builtin_fmaf((float)x, one, -mu);
+}
+__device__ __forceinline__ float less(__bf16 x, float mu) { return (float)x - mu; }
+
 // z = (x - mu) k + beta, k = r gamma.  (Not x k + (beta - mu k): where a
 // group's spread is nothing beside its mean, that has mu k 2^-24 of error.)
 struct Line {
@@ -299,8 +367,9 @@ struct Line {
 __device__ __forceinline__ Line line_of(const NormArgs& a, const Stat& st, int c) {
   return Line{st.mean, a.gamma ? st.rstd * a.gamma[c] : st.rstd, a.beta ? a.beta[c] : 0.0f};
 }
-__device__ __forceinline__ float on_line(const Line& l, float x) {
-  return __builtin_fmaf(x - l.mu, l.k, l.be);
+template <typename T>
+__device__ __forceinline__ float on_line(const Line& l, T x) {
+  return __builtin_fmaf(less(x, l.mu), l.k, l.be);
 }
 
 __device__ __forceinline__ void write_stat(const NormArgs& a, int64_t bg, const Stat& st) {
@@ -310,65 +379,56 @@ __device__ __forceinline__ void write_stat(const NormArgs& a, int64_t bg, const 
 
 template <typename T, int ACT, bool UNI>
 __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* lds) {  // [G]
-  constexpr int V = kVec<T>, UN = 4;
-  const int64_t b = unit / a.n2, chunk = unit - b * a.n2;
+  constexpr int V = kVec<T>, UN = UNI ? 2 : 1;
+  const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
+  const bool res = a.res != nullptr;
+  const Mine m = my_vectors(a, chunk, a.v1, V);
+  const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
+  const T* r = res ? static_cast<const T*>(a.res) + b * a.R + m.base : nullptr;
+  T* out = static_cast<T*>(a.out) + b * a.R + m.base;
+  auto data = stream<UN>(m.count, [&](int k) {
+    Pair<T, V> p;
+    p.x = load_vec<T, V>(x + my_at(a, k, V));
+    if (res) p.y = load_vec<T, V>(r + my_at(a, k, V));
+    return p;
+  });
   load_groups(a, b, lds, [&](int g, const Sums& t) {
     const Stat st = stat_of(a, t);
     if (chunk == 0 && a.stats) write_stat(a, b * a.G + g, st);
     return st;
   });
-  const bool res = a.res != nullptr;
-  const Mine m = my_vectors(a, chunk, a.v2, V);
-  const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
-  const T* r = res ? static_cast<const T*>(a.res) + b * a.R + m.base : nullptr;
-  T* out = static_cast<T*>(a.out) + b * a.R + m.base;
   if (!m.count && !m.tail) return;
   Line l[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int c = my_channel(a, j, V);
-    l[j] = line_of(a, lds[c / a.Cg], c);
+  my_channels<V, UNI>(a, [&](int j, int c, int g) {
+    l[j] = line_of(a, lds[g], c);
     if (UNI && j) l[j].mu = l[0].mu;
-  }
-  for (int k = 0; k < m.count; k += UN) {
-    Vec<T, V> v[UN], rv[UN];
-    uint32_t at[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      at[u] = my_at(a, m, k + u, V);
-      v[u] = load_vec<T, V>(x + at[u]);
-    }
-    if (res)
-#pragma unroll
-      for (int u = 0; u < UN; ++u) rv[u] = load_vec<T, V>(r + at[u]);
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-      if (k + u < m.count) {
+  });
+  data.run(
+      [&](const Pair<T, V>& p, int k) {
         float y[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) y[j] = act_f<ACT>(on_line(l[j], (float)v[u].e[j]));
+        for (int j = 0; j < V; ++j) y[j] = act_f<ACT>(on_line(l[j], p.x.e[j]));
         if (res)
 #pragma unroll
-          for (int j = 0; j < V; ++j) y[j] += (float)rv[u].e[j];
+          for (int j = 0; j < V; ++j) y[j] += (float)p.y.e[j];
         Vec<T, V> o;
 #pragma unroll
         for (int j = 0; j < V; ++j) o.e[j] = (T)y[j];
-        store_vec<T, V>(out + at[u], o);
-      }
-  }
+        store_vec<T, V>(out + my_at(a, k, V), o);
+      });
   if (m.tail) {
     const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (m.base + at + j < a.R) {
-        float y = act_f<ACT>(on_line(l[j], (float)x[at + j]));
+        float y = act_f<ACT>(on_line(l[j], x[at + j]));
         if (res) y += (float)r[at + j];
         out[at + j] = (T)y;
       }
   }
 }
 template <typename T, int ACT, bool UNI>
-__global__ __launch_bounds__(NT) void flat_fwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT, 4) void flat_fwd_kernel(NormArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += gridDim.x) {
     flat_fwd<T, ACT, UNI>(a, u, reinterpret_cast<Stat*>(smem));
@@ -376,30 +436,40 @@ __global__ __launch_bounds__(NT) void flat_fwd_kernel(NormArgs a) {
   }
 }
 
-// What the backward needs of a channel: xh = (x - mu) rs, z = xh ga + be.
+// What the backward needs of a channel: d = x - mu, z = d k + beta (k = r gamma),
+// h = g_out act'(z); the sums of h and, with r put to it at the end, of h d.
 struct Coef {
-  float mu, rs, ga, be;
+  float mu, rs, k, ga, be;
 };
-__device__ __forceinline__ Coef bwd_coef(const NormArgs& a, int64_t b, int c) {
-  const float* st = a.stats_in + 2 * (b * a.G + c / a.Cg);
-  return Coef{st[0], st[1], a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f};
+__device__ __forceinline__ Coef bwd_coef(const NormArgs& a, int64_t bg, int c) {
+  const float* st = a.stats_in + 2 * bg;
+  const float ga = a.gamma ? a.gamma[c] : 1.0f;
+  return Coef{st[0], st[1], st[1] * ga, ga, a.beta ? a.beta[c] : 0.0f};
 }
 // (Both passes form h alike: in a group whose values hardly differ gx is the
 // small difference of large terms, and would show any difference of the two.)
-template <int ACT>
-__device__ __forceinline__ void bwd_terms(const Coef& k, float x, float g, float* h, float* xh) {
-  *xh = (x - k.mu) * k.rs;
-  *h = g * act_grad_f<ACT>(__builtin_fmaf(*xh, k.ga, k.be));
+template <int ACT, typename T>
+__device__ __forceinline__ void bwd_terms(const Coef& k, T x, T g, float* h, float* d) {
+  *d = less(x, k.mu);
+  *h = (float)g * act_grad_f<ACT>(__builtin_fmaf(*d, k.k, k.be));
 }
-// A sum of h where the statistics are not finite: not a number (h itself may
-// be finite there).
-__device__ __forceinline__ float poisoned(const Coef& k, float s) { return __builtin_fmaf(0.0f, k.rs, s); }
-// gx = rs (ga h - a - xh d).
+// The sums of h and h xh; where the statistics are not finite, not numbers (h
+// itself may be finite there).
+__device__ __forceinline__ float2 bwd_sums(const Coef& k, float s, float q) {
+  return make_float2(__builtin_fmaf(0.0f, k.rs, s), q * k.rs);
+}
+// gx = r (gamma h - a - xh d) with xh = r (x - mu).
 struct Means {
   float a, d;
 };
-__device__ __forceinline__ float bwd_gx(const Coef& k, const Means& m, float h, float xh) {
-  return k.rs * __builtin_fmaf(k.ga, h, __builtin_fmaf(xh, -m.d, -m.a));
+struct Gx {
+  float c0, c1;
+};
+__device__ __forceinline__ Gx gx_coef(const Coef& k, const Means& m) {
+  return Gx{-k.rs * m.a, -(k.rs * m.d) * k.rs};
+}
+__device__ __forceinline__ float bwd_gx(const Coef& k, const Gx& m, float h, float d) {
+  return __builtin_fmaf(k.k, h, __builtin_fmaf(d, m.c1, m.c0));
 }
 __device__ __forceinline__ Means means_of(const NormArgs& a, const Sums& t) {
   const double m = (double)a.P * a.Cg;
@@ -409,55 +479,48 @@ __device__ __forceinline__ Means means_of(const NormArgs& a, const Sums& t) {
 // lds [A][V]: by thread and element; ch [C]: gamma times the channel's sums.
 template <typename T, int ACT, bool UNI>
 __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float2* lds, Sums* ch) {
-  constexpr int V = kVec<T>, UN = 2;
+  constexpr int V = kVec<T>, UN = UNI ? 2 : 1;
   const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
   const Mine m = my_vectors(a, chunk, a.v1, V);
   const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
   const T* g = static_cast<const T*>(a.gout) + b * a.R + m.base;
+  auto data = stream<UN>(m.count, [&](int i) {
+    return Pair<T, V>{load_vec<T, V>(x + my_at(a, i, V)), load_vec<T, V>(g + my_at(a, i, V))};
+  });
   if ((int)threadIdx.x < a.A) {
     Coef k[V];
     float s[V], q[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      k[j] = bwd_coef(a, b, my_channel(a, j, V));
+    my_channels<V, UNI>(a, [&](int j, int c, int gr) {
+      k[j] = bwd_coef(a, b * a.G + gr, c);
       if (UNI && j) {
         k[j].mu = k[0].mu;
         k[j].rs = k[0].rs;
       }
       s[j] = q[j] = 0.0f;
-    }
-    for (int i = 0; i < m.count; i += UN) {
-      Vec<T, V> xv[UN], gv[UN];
-#pragma unroll
-      for (int u = 0; u < UN; ++u) {
-        const uint32_t at = my_at(a, m, i + u, V);
-        xv[u] = load_vec<T, V>(x + at);
-        gv[u] = load_vec<T, V>(g + at);
-      }
-#pragma unroll
-      for (int u = 0; u < UN; ++u)
-        if (i + u < m.count)
+    });
+    data.run(
+        [&](const Pair<T, V>& p, int) {
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            float h, xh;
-            bwd_terms<ACT>(k[j], (float)xv[u].e[j], (float)gv[u].e[j], &h, &xh);
+            float h, d;
+            bwd_terms<ACT>(k[j], p.x.e[j], p.y.e[j], &h, &d);
             s[j] += h;
-            q[j] = __builtin_fmaf(h, xh, q[j]);
+            q[j] = __builtin_fmaf(h, d, q[j]);
           }
-    }
+        });
     if (m.tail) {
       const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
 #pragma unroll
       for (int j = 0; j < V; ++j)
         if (m.base + at + j < a.R) {
-          float h, xh;
-          bwd_terms<ACT>(k[j], (float)x[at + j], (float)g[at + j], &h, &xh);
+          float h, d;
+          bwd_terms<ACT>(k[j], x[at + j], g[at + j], &h, &d);
           s[j] += h;
-          q[j] = __builtin_fmaf(h, xh, q[j]);
+          q[j] = __builtin_fmaf(h, d, q[j]);
         }
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) lds[threadIdx.x * V + j] = make_float2(poisoned(k[j], s[j]), q[j]);
+    for (int j = 0; j < V; ++j) lds[threadIdx.x * V + j] = bwd_sums(k[j], s[j], q[j]);
   }
   __syncthreads();
   // element f = V t + j of the threads is channel f mod C's
@@ -473,7 +536,7 @@ __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float
              [&](int gr, const Sums& t) { a.part[(b * a.G + gr) * a.n + chunk] = t; });
 }
 template <typename T, int ACT, bool UNI>
-__global__ __launch_bounds__(NT) void flat_sums_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT, UNI ? 4 : 3) void flat_sums_kernel(NormArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   float2* lds = reinterpret_cast<float2*>(smem);
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += gridDim.x) {
@@ -498,63 +561,52 @@ __device__ __forceinline__ void param_grads(const NormArgs& a, int c) {
 
 template <typename T, int ACT, bool UNI>
 __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means* lds) {  // [G]
-  constexpr int V = kVec<T>, UN = 2;
-  const int64_t b = unit / a.n2, chunk = unit - b * a.n2;
-  load_groups(a, b, lds, [&](int, const Sums& t) { return means_of(a, t); });
-  const Mine m = my_vectors(a, chunk, a.v2, V);
+  constexpr int V = kVec<T>, UN = UNI ? 2 : 1;
+  const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
+  const Mine m = my_vectors(a, chunk, a.v1, V);
   const T* x = static_cast<const T*>(a.x) + b * a.R + m.base;
   const T* g = static_cast<const T*>(a.gout) + b * a.R + m.base;
   T* out = static_cast<T*>(a.out) + b * a.R + m.base;
+  auto data = stream<UN>(m.count, [&](int i) {
+    return Pair<T, V>{load_vec<T, V>(x + my_at(a, i, V)), load_vec<T, V>(g + my_at(a, i, V))};
+  });
+  load_groups(a, b, lds, [&](int, const Sums& t) { return means_of(a, t); });
   if (!m.count && !m.tail) return;
   Coef k[V];
-  Means mn[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int c = my_channel(a, j, V);
-    k[j] = bwd_coef(a, b, c);
-    mn[j] = lds[c / a.Cg];
+  Gx gk[V];
+  my_channels<V, UNI>(a, [&](int j, int c, int gr) {
+    k[j] = bwd_coef(a, b * a.G + gr, c);
+    gk[j] = gx_coef(k[j], lds[gr]);
     if (UNI && j) {
       k[j].mu = k[0].mu;
-      k[j].rs = k[0].rs;
-      mn[j] = mn[0];
+      gk[j] = gk[0];
     }
-  }
-  for (int i = 0; i < m.count; i += UN) {
-    Vec<T, V> xv[UN], gv[UN];
-    uint32_t at[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      at[u] = my_at(a, m, i + u, V);
-      xv[u] = load_vec<T, V>(x + at[u]);
-      gv[u] = load_vec<T, V>(g + at[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-      if (i + u < m.count) {
+  });
+  data.run(
+      [&](const Pair<T, V>& p, int i) {
         Vec<T, V> o;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          float h, xh;
-          bwd_terms<ACT>(k[j], (float)xv[u].e[j], (float)gv[u].e[j], &h, &xh);
-          o.e[j] = (T)bwd_gx(k[j], mn[j], h, xh);
+          float h, d;
+          bwd_terms<ACT>(k[j], p.x.e[j], p.y.e[j], &h, &d);
+          o.e[j] = (T)bwd_gx(k[j], gk[j], h, d);
         }
-        store_vec<T, V>(out + at[u], o);
-      }
-  }
+        store_vec<T, V>(out + my_at(a, i, V), o);
+      });
   if (m.tail) {
     const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (m.base + at + j < a.R) {
-        float h, xh;
-        bwd_terms<ACT>(k[j], (float)x[at + j], (float)g[at + j], &h, &xh);
-        out[at + j] = (T)bwd_gx(k[j], mn[j], h, xh);
+        float h, d;
+        bwd_terms<ACT>(k[j], x[at + j], g[at + j], &h, &d);
+        out[at + j] = (T)bwd_gx(k[j], gk[j], h, d);
       }
   }
 }
 
 template <typename T, int ACT, bool UNI>
-__global__ __launch_bounds__(NT) void flat_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT, UNI ? 4 : 3) void flat_bwd_kernel(NormArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   if ((int)blockIdx.x >= a.main) return param_grads(a, (int)blockIdx.x - a.main);
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += a.main) {
@@ -601,23 +653,15 @@ __device__ __forceinline__ float act_grad_any(float z, int act) {
   return act == FNO_NORM_ACT_GELU ? gelu_grad_of(z) : act == FNO_NORM_ACT_SILU ? silu_grad_f(z) : 1.0f;
 }
 
-// f(row, vector of x, vector of the second tensor) for the thread's rows,
-// four rows' loads in flight.
+// f(row, vector of x, vector of the second tensor) for the thread's rows.
 template <typename T, int W, typename F>
 __device__ __forceinline__ void over_rows(const NormArgs& a, const Wide& w, const T* x, const T* y, F f) {
-  constexpr int UN = 4;
-  for (int64_t i = 0; i < w.rows; i += UN) {
-    Vec<T, W> xv[UN], yv[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int64_t at = w.at + (i + u < w.rows ? i + u : w.rows - 1) * a.C;
-      xv[u] = load_vec<T, W>(x + at);
-      if (y) yv[u] = load_vec<T, W>(y + at);
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-      if (i + u < w.rows) f(i + u, xv[u], yv[u]);
-  }
+  stream<4>((int)w.rows, [&](int i) {
+    Pair<T, W> p;
+    p.x = load_vec<T, W>(x + w.at + (int64_t)i * a.C);
+    if (y) p.y = load_vec<T, W>(y + w.at + (int64_t)i * a.C);
+    return p;
+  }).run([&](const Pair<T, W>& p, int i) { f((int64_t)i, p.x, p.y); });
 }
 
 template <typename T, int W>
@@ -658,7 +702,7 @@ __global__ __launch_bounds__(NT) void wide_fwd_kernel(NormArgs a) {
                       Vec<T, W> o;
 #pragma unroll
                       for (int j = 0; j < W; ++j) {
-                        float y = act_any(on_line(l[j], (float)v.e[j]), a.act);
+                        float y = act_any(on_line(l[j], v.e[j]), a.act);
                         if (a.res) y += (float)r.e[j];
                         o.e[j] = (T)y;
                       }
@@ -676,26 +720,26 @@ __global__ __launch_bounds__(NT) void wide_sums_kernel(NormArgs a) {
     float s[W], q[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      k[j] = bwd_coef(a, w.b, w.c + j);
+      k[j] = bwd_coef(a, w.b * a.G + (w.c + j) / a.Cg, w.c + j);
       s[j] = q[j] = 0.0f;
     }
     over_rows<T, W>(a, w, static_cast<const T*>(a.x), static_cast<const T*>(a.gout),
                     [&](int64_t, const Vec<T, W>& x, const Vec<T, W>& g) {
 #pragma unroll
                       for (int j = 0; j < W; ++j) {
-                        const float xh = ((float)x.e[j] - k[j].mu) * k[j].rs;
+                        const float d = (float)x.e[j] - k[j].mu;
                         const float h = (float)g.e[j] *
-                                        act_grad_any(__builtin_fmaf(xh, k[j].ga, k[j].be), a.act);
+                                        act_grad_any(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
                         s[j] += h;
-                        q[j] = __builtin_fmaf(h, xh, q[j]);
+                        q[j] = __builtin_fmaf(h, d, q[j]);
                       }
                     });
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const int64_t at = (w.b * a.C + w.c + j) * a.n1 + w.chunk;
-      const double sj = poisoned(k[j], s[j]);
-      a.chan[at] = Sums{sj, q[j]};
-      a.part[at] = Sums{(double)k[j].ga * sj, (double)k[j].ga * q[j]};
+      const float2 t = bwd_sums(k[j], s[j], q[j]);
+      a.chan[at] = Sums{t.x, t.y};
+      a.part[at] = Sums{(double)k[j].ga * t.x, (double)k[j].ga * t.y};
     }
   }
 }
@@ -707,11 +751,12 @@ __global__ __launch_bounds__(NT) void wide_bwd_kernel(NormArgs a) {
     const Wide w = my_wide<W>(a, u);
     if (!w.rows) continue;
     Coef k[W];
-    Means mn[W];
+    Gx gk[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      k[j] = bwd_coef(a, w.b, w.c + j);
-      mn[j] = means_of(a, a.joined[w.b * a.G + (w.c + j) / a.Cg]);
+      const int64_t bg = w.b * a.G + (w.c + j) / a.Cg;
+      k[j] = bwd_coef(a, bg, w.c + j);
+      gk[j] = gx_coef(k[j], means_of(a, a.joined[bg]));
     }
     T* out = static_cast<T*>(a.out) + w.at;
     over_rows<T, W>(a, w, static_cast<const T*>(a.x), static_cast<const T*>(a.gout),
@@ -719,10 +764,10 @@ __global__ __launch_bounds__(NT) void wide_bwd_kernel(NormArgs a) {
                       Vec<T, W> o;
 #pragma unroll
                       for (int j = 0; j < W; ++j) {
-                        const float xh = ((float)x.e[j] - k[j].mu) * k[j].rs;
+                        const float d = (float)x.e[j] - k[j].mu;
                         const float h = (float)g.e[j] *
-                                        act_grad_any(__builtin_fmaf(xh, k[j].ga, k[j].be), a.act);
-                        o.e[j] = (T)bwd_gx(k[j], mn[j], h, xh);
+                                        act_grad_any(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
+                        o.e[j] = (T)bwd_gx(k[j], gk[j], h, d);
                       }
                       store_vec<T, W>(out + i * a.C, o);
                     });
@@ -750,25 +795,25 @@ __device__ __forceinline__ Seg seg_of(const NormArgs& a, int64_t unit) {
   return s;
 }
 
-// f(element, vector of x, vector of y) for this thread's full vectors of a
-// segment, UN of them in flight, then f1(element) for at most one element of
-// its last partial vector.
-template <typename T, int TEAM, int UN, typename F, typename F1>
-__device__ __forceinline__ void over_segment(const T* x, const T* y, int len, F f, F1 f1) {
+// This thread's full vectors of a segment, of x and (y not null) of y.
+template <typename T, int TEAM, int UN>
+__device__ __forceinline__ auto segment(const T* x, const T* y, int len) {
   constexpr int V = kVec<T>;
   const int lane = threadIdx.x & (TEAM - 1), full = len / V;
-  for (int i = lane; i < full; i += TEAM * UN) {
-    Vec<T, V> xv[UN], yv[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int at = (i + u * TEAM < full ? i + u * TEAM : i) * V;
-      xv[u] = load_vec<T, V>(x + at);
-      if (y) yv[u] = load_vec<T, V>(y + at);
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-      if (i + u * TEAM < full) f((i + u * TEAM) * V, xv[u], yv[u]);
-  }
+  return stream<UN>(lane < full ? (full - lane + TEAM - 1) / TEAM : 0, [=](int k) {
+    Pair<T, V> p;
+    p.x = load_vec<T, V>(x + (uint32_t)((lane + k * TEAM) * V));
+    if (y) p.y = load_vec<T, V>(y + (uint32_t)((lane + k * TEAM) * V));
+    return p;
+  });
+}
+// f(element, vector of x, vector of y) for them, then f1(element) for at most
+// one element of the segment's last, partial vector.
+template <typename T, int TEAM, typename S, typename F, typename F1>
+__device__ __forceinline__ void over_segment(S& data, int len, F f, F1 f1) {
+  constexpr int V = kVec<T>;
+  const int lane = threadIdx.x & (TEAM - 1), full = len / V;
+  data.run([&](const Pair<T, V>& p, int k) { f((lane + k * TEAM) * V, p.x, p.y); });
   if (lane < len - full * V) f1(full * V + lane);
 }
 
@@ -784,8 +829,9 @@ __global__ __launch_bounds__(NT) void first_stats_kernel(NormArgs a) {
     const Seg s = seg_of(a, u);
     const T* x = static_cast<const T*>(a.x) + s.at;
     Sums t{0.0, 0.0}, t1{0.0, 0.0};
-    over_segment<T, TEAM, 4>(
-        x, (const T*)nullptr, s.len,
+    auto data = segment<T, TEAM, 4>(x, (const T*)nullptr, s.len);
+    over_segment<T, TEAM>(
+        data, s.len,
         [&](int, const Vec<T, V>& v, const Vec<T, V>&) {
 #pragma unroll
           for (int j = 0; j < V; ++j) add_value(j & 1 ? &t1 : &t, (float)v.e[j]);
@@ -810,18 +856,19 @@ __global__ __launch_bounds__(NT) void first_fwd_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
   for (int64_t u = first_unit<TEAM>(a); u < a.u1; u += (int64_t)gridDim.x * (NT / TEAM)) {
     const Seg s = seg_of(a, u);
+    const T* x = static_cast<const T*>(a.x) + s.at;
+    const T* r = a.res ? static_cast<const T*>(a.res) + s.at : nullptr;
+    auto data = segment<T, TEAM, 2>(x, r, s.len);
     const Stat st = stat_of(a, group_of<TEAM>(a, s.bg));
     if (a.stats && s.seg == 0 && s.c % a.Cg == 0 && (threadIdx.x & (TEAM - 1)) == 0) write_stat(a, s.bg, st);
     const Line l = line_of(a, st, s.c);
-    const T* x = static_cast<const T*>(a.x) + s.at;
-    const T* r = a.res ? static_cast<const T*>(a.res) + s.at : nullptr;
     T* out = static_cast<T*>(a.out) + s.at;
-    over_segment<T, TEAM, 4>(
-        x, r, s.len,
+    over_segment<T, TEAM>(
+        data, s.len,
         [&](int e, const Vec<T, V>& v, const Vec<T, V>& rv) {
           float y[V];
 #pragma unroll
-          for (int j = 0; j < V; ++j) y[j] = act_f<ACT>(on_line(l, (float)v.e[j]));
+          for (int j = 0; j < V; ++j) y[j] = act_f<ACT>(on_line(l, v.e[j]));
           if (r)
 #pragma unroll
             for (int j = 0; j < V; ++j) y[j] += (float)rv.e[j];
@@ -831,7 +878,7 @@ __global__ __launch_bounds__(NT) void first_fwd_kernel(NormArgs a) {
           store_vec<T, V>(out + e, o);
         },
         [&](int e) {
-          float y = act_f<ACT>(on_line(l, (float)x[e]));
+          float y = act_f<ACT>(on_line(l, x[e]));
           if (r) y += (float)r[e];
           out[e] = (T)y;
         });
@@ -843,24 +890,26 @@ __global__ __launch_bounds__(NT) void first_sums_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
   for (int64_t u = first_unit<TEAM>(a); u < a.u1; u += (int64_t)gridDim.x * (NT / TEAM)) {
     const Seg s = seg_of(a, u);
-    const Coef k = bwd_coef(a, s.bc / a.C, s.c);
     const T* x = static_cast<const T*>(a.x) + s.at;
     const T* g = static_cast<const T*>(a.gout) + s.at;
+    auto data = segment<T, TEAM, 2>(x, g, s.len);
+    const Coef k = bwd_coef(a, s.bg, s.c);
     float sh = 0.0f, sx = 0.0f;
-    auto one = [&](float xv, float gv) {
-      float h, xh;
-      bwd_terms<ACT>(k, xv, gv, &h, &xh);
+    auto one = [&](T xv, T gv) {
+      float h, d;
+      bwd_terms<ACT>(k, xv, gv, &h, &d);
       sh += h;
-      sx = __builtin_fmaf(h, xh, sx);
+      sx = __builtin_fmaf(h, d, sx);
     };
-    over_segment<T, TEAM, 2>(
-        x, g, s.len,
+    over_segment<T, TEAM>(
+        data, s.len,
         [&](int, const Vec<T, V>& xv, const Vec<T, V>& gv) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) one((float)xv.e[j], (float)gv.e[j]);
+          for (int j = 0; j < V; ++j) one(xv.e[j], gv.e[j]);
         },
-        [&](int e) { one((float)x[e], (float)g[e]); });
-    const Sums t = team_sum<TEAM>(Sums{poisoned(k, sh), sx});
+        [&](int e) { one(x[e], g[e]); });
+    const float2 mine = bwd_sums(k, sh, sx);
+    const Sums t = team_sum<TEAM>(Sums{mine.x, mine.y});
     if ((threadIdx.x & (TEAM - 1)) == 0) {
       a.chan[u] = t;
       a.part[u] = Sums{(double)k.ga * t.s, (double)k.ga * t.q};
@@ -874,25 +923,26 @@ __global__ __launch_bounds__(NT) void first_bwd_kernel(NormArgs a) {
   if ((int)blockIdx.x >= a.main) return param_grads(a, (int)blockIdx.x - a.main);
   for (int64_t u = first_unit<TEAM>(a); u < a.u1; u += (int64_t)a.main * (NT / TEAM)) {
     const Seg s = seg_of(a, u);
-    const Coef k = bwd_coef(a, s.bc / a.C, s.c);
-    const Means mn = means_of(a, group_of<TEAM>(a, s.bg));
     const T* x = static_cast<const T*>(a.x) + s.at;
     const T* g = static_cast<const T*>(a.gout) + s.at;
+    auto data = segment<T, TEAM, 2>(x, g, s.len);
+    const Coef k = bwd_coef(a, s.bg, s.c);
+    const Gx gk = gx_coef(k, means_of(a, group_of<TEAM>(a, s.bg)));
     T* out = static_cast<T*>(a.out) + s.at;
-    auto one = [&](float xv, float gv) {
-      float h, xh;
-      bwd_terms<ACT>(k, xv, gv, &h, &xh);
-      return bwd_gx(k, mn, h, xh);
+    auto one = [&](T xv, T gv) {
+      float h, d;
+      bwd_terms<ACT>(k, xv, gv, &h, &d);
+      return bwd_gx(k, gk, h, d);
     };
-    over_segment<T, TEAM, 2>(
-        x, g, s.len,
+    over_segment<T, TEAM>(
+        data, s.len,
         [&](int e, const Vec<T, V>& xv, const Vec<T, V>& gv) {
           Vec<T, V> o;
 #pragma unroll
-          for (int j = 0; j < V; ++j) o.e[j] = (T)one((float)xv.e[j], (float)gv.e[j]);
+          for (int j = 0; j < V; ++j) o.e[j] = (T)one(xv.e[j], gv.e[j]);
           store_vec<T, V>(out + e, o);
         },
-        [&](int e) { out[e] = (T)one((float)x[e], (float)g[e]); });
+        [&](int e) { out[e] = (T)one(x[e], g[e]); });
   }
 }
 
@@ -920,7 +970,7 @@ fno_status check_desc(const fno_norm_desc* d) {
 }
 
 enum Route { FLAT, WIDE, FIRST };
-constexpr int kFill = 2048;        // work-groups that fill the chip (eight per compute unit)
+constexpr int kFill = 1024;        // work-groups that fill the chip (four per compute unit)
 constexpr int kMaxGrid = 1 << 20;  // work-groups of a launch; more work is looped over
 
 struct NormPlan {
@@ -929,7 +979,7 @@ struct NormPlan {
   int vec;     // elements of a vector (wide: of a thread)
   bool uni;    // flat: a vector's channels are of one group
   int team;    // first
-  int64_t units1, units2;  // work items of the passes
+  int64_t units;  // work items of each pass
 };
 
 NormPlan plan_of(const fno_norm_desc& d) {
@@ -946,35 +996,46 @@ NormPlan plan_of(const fno_norm_desc& d) {
   a.eps = d.eps;
   p.vec = V;
   if (d.layout == FNO_LAYOUT_CHANNELS_FIRST) {
-    // a wave per plane up to 16 vectors a lane, else work-groups on segments
-    // of at least four vectors a thread, enough of them to fill the chip
+    // A wave per plane up to 16 vectors a lane, else work-groups on segments
+    // of at least eight vectors a thread, up to eight times what fills the
+    // chip: the memory keeps busiest while work-groups start and end at
+    // different times (backward of 16 x 128 planes of 256^2, bf16: 277 us with
+    // 2048 segments, 264 with 4096, 251 with 8192).
     p.route = FIRST;
     p.team = a.P <= 64 * V * 16 ? 64 : NT;
     a.n1 = 1;
     if (p.team == NT)
-      a.n1 = (int)std::max<int64_t>({1, std::min(cdiv(2 * kFill, a.B * a.C), cdiv(a.P, NT * V * 4)), cdiv(a.P, (int64_t)1 << 30)});
+      a.n1 = (int)std::max<int64_t>(
+          {1, std::min(cdiv(8 * kFill, a.B * a.C), a.P / (NT * V * 8)), cdiv(a.P, (int64_t)1 << 30)});
     a.rows = rup(cdiv(a.P, a.n1), (int64_t)NT * V);
     a.n1 = (int)cdiv(a.P, a.rows);
     a.n = a.Cg * a.n1;
     a.nc = a.n1;
     a.collapse = a.n > (p.team == NT ? 1024 : 256);
-    p.units1 = p.units2 = a.B * a.C * a.n1;
+    p.units = a.B * a.C * a.n1;
     return p;
   }
   const int64_t L = a.C / std::gcd(a.C, V);
   if (L <= NT) {
+    // Chunks of 16 vectors a thread (fp32, whose vectors take half the
+    // operations: 8), between one and four times the work-groups that fill
+    // the chip, but at least four vectors a thread.  A work-group's start and
+    // end (its channels' coefficients, its sums joined) cost as much as five
+    // vectors (33.5 M fp16 elements: forward 44 us with 1024 work-groups, 48
+    // with 2048, 62 with 4096; as many fp32: 83, 81 and 76).
     p.route = FLAT;
     a.L = (int)L;
     a.A = (int)(NT / L * L);
     p.uni = a.C % V == 0 && a.Cg % V == 0;
-    const int64_t nv = cdiv(a.R, V), room = std::max<int64_t>(1, nv / ((int64_t)a.A * 4));
-    const int64_t want = std::max<int64_t>(std::max<int64_t>(1, kFill / a.B), cdiv(nv, (int64_t)1 << 26));
-    a.v1 = a.v2 = rup(cdiv(nv, std::min(want, room)), a.A);  // room: four vectors a thread
-    a.n1 = a.n2 = (int)cdiv(nv, a.v1);
+    const int64_t nv = cdiv(a.R, V), per = (int64_t)a.A * (V == 4 ? 8 : 16);
+    const int64_t want = std::clamp<int64_t>(a.B * nv / per, kFill, 4 * kFill) / a.B;
+    const int64_t room = std::max<int64_t>(1, nv / ((int64_t)a.A * 4));
+    const int64_t n = std::max(std::clamp<int64_t>(want, 1, room), cdiv(nv, (int64_t)1 << 26));
+    a.v1 = rup(cdiv(nv, n), a.A);
+    a.n1 = (int)cdiv(nv, a.v1);
     a.n = a.nc = a.n1;
     a.collapse = (int64_t)a.n * a.G > 2048;
-    p.units1 = a.B * a.n1;
-    p.units2 = a.B * a.n2;
+    p.units = a.B * a.n1;
     return p;
   }
   p.route = WIDE;
@@ -986,7 +1047,7 @@ NormPlan plan_of(const fno_norm_desc& d) {
   a.n = a.Cg * a.n1;
   a.nc = a.n1;
   a.collapse = 1;
-  p.units1 = p.units2 = a.B * a.n1 * a.cols;
+  p.units = a.B * a.n1 * a.cols;
   return p;
 }
 
@@ -1014,7 +1075,6 @@ unsigned grid_of(int64_t units) { return (unsigned)std::min<int64_t>(units, kMax
 void launch_join(NormLaunch& L) {
   NormArgs& a = L.p.a;
   if (!a.collapse) return;
-  a.u0 = 0;
   a.u1 = a.B * a.G;
   hipLaunchKernelGGL(join_kernel, dim3(grid_of(cdiv(a.u1, 4))), dim3(NT), 0, L.s, a);
 }
@@ -1022,89 +1082,91 @@ void launch_join(NormLaunch& L) {
 template <typename T>
 void launch_stats(NormLaunch& L) {
   NormArgs& a = L.p.a;
-  a.u0 = 0;
-  a.u1 = L.p.units1;
+  const int64_t units = a.u1 - a.u0;
   if (L.p.route == FLAT) {
     const size_t lds = (size_t)a.A * (L.p.uni ? 1 : kVec<T>) * sizeof(Sums);
     auto k = L.p.uni ? flat_stats_kernel<T, true> : flat_stats_kernel<T, false>;
-    hipLaunchKernelGGL(k, dim3(grid_of(a.u1)), dim3(NT), lds, L.s, a);
+    hipLaunchKernelGGL(k, dim3(grid_of(units)), dim3(NT), lds, L.s, a);
   } else if (L.p.route == WIDE) {
     auto k = L.p.vec == 1 ? wide_stats_kernel<T, 1> : wide_stats_kernel<T, kVec<T>>;
-    hipLaunchKernelGGL(k, dim3(grid_of(a.u1)), dim3(NT), 0, L.s, a);
+    hipLaunchKernelGGL(k, dim3(grid_of(units)), dim3(NT), 0, L.s, a);
   } else {
     auto k = L.p.team == 64 ? first_stats_kernel<T, 64> : first_stats_kernel<T, NT>;
-    hipLaunchKernelGGL(k, dim3(grid_of(cdiv(a.u1, NT / L.p.team))), dim3(NT), 0, L.s, a);
+    hipLaunchKernelGGL(k, dim3(grid_of(cdiv(units, NT / L.p.team))), dim3(NT), 0, L.s, a);
   }
 }
 
 template <typename T, int ACT>
-void launch_fwd_t(NormLaunch& L) {
+void launch_fwd2(NormLaunch& L) {
   NormArgs& a = L.p.a;
-  launch_stats<T>(L);
-  launch_join(L);
-  a.u0 = 0;
-  a.u1 = L.p.units2;
+  const int64_t units = a.u1 - a.u0;
   if (L.p.route == FLAT) {
     auto k = L.p.uni ? flat_fwd_kernel<T, ACT, true> : flat_fwd_kernel<T, ACT, false>;
-    hipLaunchKernelGGL(k, dim3(grid_of(a.u1)), dim3(NT), a.G * sizeof(Stat), L.s, a);
+    hipLaunchKernelGGL(k, dim3(grid_of(units)), dim3(NT), a.G * sizeof(Stat), L.s, a);
   } else if (L.p.route == WIDE) {
     auto k = L.p.vec == 1 ? wide_fwd_kernel<T, 1> : wide_fwd_kernel<T, kVec<T>>;
-    hipLaunchKernelGGL(k, dim3(grid_of(a.u1)), dim3(NT), 0, L.s, a);
+    hipLaunchKernelGGL(k, dim3(grid_of(units)), dim3(NT), 0, L.s, a);
   } else {
     auto k = L.p.team == 64 ? first_fwd_kernel<T, 64, ACT> : first_fwd_kernel<T, NT, ACT>;
-    hipLaunchKernelGGL(k, dim3(grid_of(cdiv(a.u1, NT / L.p.team))), dim3(NT), 0, L.s, a);
+    hipLaunchKernelGGL(k, dim3(grid_of(cdiv(units, NT / L.p.team))), dim3(NT), 0, L.s, a);
   }
 }
 
 template <typename T, int ACT>
-void launch_bwd_t(NormLaunch& L) {
+void launch_sums(NormLaunch& L) {
   NormArgs& a = L.p.a;
-  const int extra = a.ggamma || a.gbeta ? a.C : 0;
-  a.u0 = 0;
-  a.u1 = L.p.units1;
+  const int64_t units = a.u1 - a.u0;
   if (L.p.route == FLAT) {
     const size_t lds = (size_t)NT * kVec<T> * sizeof(float2) + a.C * sizeof(Sums);
-    auto k1 = L.p.uni ? flat_sums_kernel<T, ACT, true> : flat_sums_kernel<T, ACT, false>;
-    hipLaunchKernelGGL(k1, dim3(grid_of(a.u1)), dim3(NT), lds, L.s, a);
-    launch_join(L);
-    a.u0 = 0;
-    a.u1 = L.p.units2;
-    a.main = (int)grid_of(a.u1);
-    auto k2 = L.p.uni ? flat_bwd_kernel<T, ACT, true> : flat_bwd_kernel<T, ACT, false>;
-    hipLaunchKernelGGL(k2, dim3(a.main + extra), dim3(NT), a.G * sizeof(Stat), L.s, a);
+    auto k = L.p.uni ? flat_sums_kernel<T, ACT, true> : flat_sums_kernel<T, ACT, false>;
+    hipLaunchKernelGGL(k, dim3(grid_of(units)), dim3(NT), lds, L.s, a);
   } else if (L.p.route == WIDE) {
-    auto k1 = L.p.vec == 1 ? wide_sums_kernel<T, 1> : wide_sums_kernel<T, kVec<T>>;
-    hipLaunchKernelGGL(k1, dim3(grid_of(a.u1)), dim3(NT), 0, L.s, a);
-    launch_join(L);
-    a.u0 = 0;
-    a.u1 = L.p.units2;
-    a.main = (int)grid_of(a.u1);
-    auto k2 = L.p.vec == 1 ? wide_bwd_kernel<T, 1> : wide_bwd_kernel<T, kVec<T>>;
-    hipLaunchKernelGGL(k2, dim3(a.main + extra), dim3(NT), 0, L.s, a);
+    auto k = L.p.vec == 1 ? wide_sums_kernel<T, 1> : wide_sums_kernel<T, kVec<T>>;
+    hipLaunchKernelGGL(k, dim3(grid_of(units)), dim3(NT), 0, L.s, a);
   } else {
-    const int64_t per = NT / L.p.team;
-    auto k1 = L.p.team == 64 ? first_sums_kernel<T, 64, ACT> : first_sums_kernel<T, NT, ACT>;
-    hipLaunchKernelGGL(k1, dim3(grid_of(cdiv(a.u1, per))), dim3(NT), 0, L.s, a);
-    launch_join(L);
-    a.u0 = 0;
-    a.u1 = L.p.units2;
-    a.main = (int)grid_of(cdiv(a.u1, per));
-    auto k2 = L.p.team == 64 ? first_bwd_kernel<T, 64, ACT> : first_bwd_kernel<T, NT, ACT>;
-    hipLaunchKernelGGL(k2, dim3(a.main + extra), dim3(NT), 0, L.s, a);
+    auto k = L.p.team == 64 ? first_sums_kernel<T, 64, ACT> : first_sums_kernel<T, NT, ACT>;
+    hipLaunchKernelGGL(k, dim3(grid_of(cdiv(units, NT / L.p.team))), dim3(NT), 0, L.s, a);
   }
+}
+
+// extra: work-groups beyond the slab's for the parameter gradients
+template <typename T, int ACT>
+void launch_bwd2(NormLaunch& L, int extra) {
+  NormArgs& a = L.p.a;
+  const int64_t units = a.u1 - a.u0;
+  if (L.p.route == FLAT) {
+    a.main = (int)grid_of(units);
+    auto k = L.p.uni ? flat_bwd_kernel<T, ACT, true> : flat_bwd_kernel<T, ACT, false>;
+    hipLaunchKernelGGL(k, dim3(a.main + extra), dim3(NT), a.G * sizeof(Stat), L.s, a);
+  } else if (L.p.route == WIDE) {
+    a.main = (int)grid_of(units);
+    auto k = L.p.vec == 1 ? wide_bwd_kernel<T, 1> : wide_bwd_kernel<T, kVec<T>>;
+    hipLaunchKernelGGL(k, dim3(a.main + extra), dim3(NT), 0, L.s, a);
+  } else {
+    a.main = (int)grid_of(cdiv(units, NT / L.p.team));
+    auto k = L.p.team == 64 ? first_bwd_kernel<T, 64, ACT> : first_bwd_kernel<T, NT, ACT>;
+    hipLaunchKernelGGL(k, dim3(a.main + extra), dim3(NT), 0, L.s, a);
+  }
+}
+
+template <typename T, int ACT>
+void launch_both(NormLaunch& L, bool bwd) {
+  NormArgs& a = L.p.a;
+  a.u0 = 0;
+  a.u1 = L.p.units;
+  bwd ? launch_sums<T, ACT>(L) : launch_stats<T>(L);
+  launch_join(L);
+  a.u1 = L.p.units;
+  if (bwd) launch_bwd2<T, ACT>(L, a.ggamma || a.gbeta ? a.C : 0);
+  else launch_fwd2<T, ACT>(L);
 }
 
 template <typename T>
 hipError_t by_act(NormLaunch& L, bool bwd) {
   switch (L.p.a.act) {
-    case FNO_NORM_ACT_GELU:
-      bwd ? launch_bwd_t<T, FNO_NORM_ACT_GELU>(L) : launch_fwd_t<T, FNO_NORM_ACT_GELU>(L);
-      break;
-    case FNO_NORM_ACT_SILU:
-      bwd ? launch_bwd_t<T, FNO_NORM_ACT_SILU>(L) : launch_fwd_t<T, FNO_NORM_ACT_SILU>(L);
-      break;
-    default:
-      bwd ? launch_bwd_t<T, FNO_NORM_ACT_NONE>(L) : launch_fwd_t<T, FNO_NORM_ACT_NONE>(L);
+    case FNO_NORM_ACT_GELU: launch_both<T, FNO_NORM_ACT_GELU>(L, bwd); break;
+    case FNO_NORM_ACT_SILU: launch_both<T, FNO_NORM_ACT_SILU>(L, bwd); break;
+    default: launch_both<T, FNO_NORM_ACT_NONE>(L, bwd);
   }
   return hipGetLastError();
 }
