@@ -27,233 +27,11 @@
 #include <numeric>
 
 #include "../../include/fno_spectral_conv.h"
-#include "fno_act.h"
 #include "fno_host.h"
+#include "fno_norm.h"
 
 namespace fno {
 namespace {
-
-constexpr int NT = 256;  // threads of a work-group
-
-inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t rup(int64_t a, int64_t b) { return cdiv(a, b) * b; }
-
-struct Sums {  // of x and x^2, or of h and h xh
-  double s, q;
-};
-
-template <typename T>
-constexpr int kVec = 16 / (int)sizeof(T);
-template <typename T, int W = kVec<T>>
-struct Vec {
-  T e[W];
-};
-// W consecutive elements at any element address, in one access.
-template <typename T, int W>
-__device__ __forceinline__ Vec<T, W> load_vec(const T* p) {
-  Vec<T, W> v;
-  __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), sizeof(v));
-  return v;
-}
-template <typename T, int W>
-__device__ __forceinline__ void store_vec(T* p, const Vec<T, W>& v) {
-  __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T)), &v, sizeof(v));
-}
-
-// --------------------------------------------------------------------------
-// Activations
-// --------------------------------------------------------------------------
-// GELU z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt 2) / 2, with half of erfc by
-// Abramowitz & Stegun 7.1.26 (absolute error at most 0.75e-7).
-__device__ __forceinline__ float gelu_of(float z) {
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.23164189f, 1.0f));
-  float p = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);
-  p = __builtin_fmaf(t, p, 0.7107068705f);
-  p = __builtin_fmaf(t, p, -0.142248368f);
-  p = __builtin_fmaf(t, p, 0.127414796f);
-  const float e = __builtin_amdgcn_exp2f(z * (z * -0.72134752044448f));
-  return __builtin_fmaf(-__builtin_fabsf(z), p * t * e, __builtin_fmaxf(z, 0.0f));
-}
-// Its derivative Phi(z) + z phi(z) as 1/2 + z P(z^2) / Q(z^2) for |z| <= 5.6,
-// constant beyond: a rational fit of degrees (5, 5) to the definition (least
-// squares, reweighted to near the minimax of 1.1e-7), within 3.3e-7 of it
-// everywhere in float.  One reciprocal and no exponential: 18 operations' time
-// against 22 through erfc and exp(-z^2 / 2), where the passes are bound by it.
-__device__ __forceinline__ float gelu_grad_of(float z) {
-  const float c = __builtin_amdgcn_fmed3f(z, -5.6f, 5.6f), t = c * c;
-  float p = __builtin_fmaf(t, 1.921672664e-07f, 3.589928644e-05f);
-  p = __builtin_fmaf(t, p, 1.975132363e-05f);
-  p = __builtin_fmaf(t, p, 1.422606847e-02f);
-  p = __builtin_fmaf(t, p, -3.097535923e-02f);
-  p = __builtin_fmaf(t, p, 7.978853454e-01f);
-  float q = __builtin_fmaf(t, 8.928170334e-06f, 1.920517995e-04f);
-  q = __builtin_fmaf(t, q, 3.522637464e-03f);
-  q = __builtin_fmaf(t, q, 4.098374084e-02f);
-  q = __builtin_fmaf(t, q, 2.945195774e-01f);
-  q = __builtin_fmaf(t, q, 1.0f);
-  return __builtin_fmaf(c * p, __builtin_amdgcn_rcpf(q), 0.5f);
-}
-
-template <int ACT>
-__device__ __forceinline__ float act_f(float z) {
-  return ACT == FNO_NORM_ACT_GELU ? gelu_of(z) : ACT == FNO_NORM_ACT_SILU ? silu_f(z) : z;
-}
-template <int ACT>
-__device__ __forceinline__ float act_grad_f(float z) {
-  return ACT == FNO_NORM_ACT_GELU ? gelu_grad_of(z) : ACT == FNO_NORM_ACT_SILU ? silu_grad_f(z) : 1.0f;
-}
-
-// --------------------------------------------------------------------------
-// Arguments
-// --------------------------------------------------------------------------
-struct NormArgs {
-  const void *x, *res, *gout;
-  const float *gamma, *beta;
-  void* out;             // out or gx
-  const float* stats_in; // backward: [B][G][2]
-  float* stats;          // forward: [B][G][2] or null
-  Sums* part;            // [B][G][n]: the first pass's sums of each group
-  Sums* joined;          // [B][G], where `collapse`
-  Sums* chan;            // [B][C][nc]: the backward's sums of each channel
-  float *ggamma, *gbeta;
-  int64_t B, P, R;       // R = P C elements of a sample
-  int C, G, Cg;
-  int n, nc;             // entries of a group in part, of a channel in chan
-  int collapse;          // part is joined by a launch of its own
-  int act;
-  float eps;
-  // flat: L, A as above; vectors of a chunk (a multiple of A), chunks of a sample
-  int L, A, n1;
-  int64_t v1;
-  // wide: rows of a chunk, column blocks, chunks (n1)
-  // first: elements of a segment, segments of a plane (n1)
-  int64_t rows;
-  int cols;
-  // this launch's work items and the work-groups that share them (further
-  // ones, one per channel, form the parameter gradients)
-  int64_t u0, u1;
-  int main;
-};
-
-// A group's statistics from its sums.
-struct Stat {
-  float mean, rstd;
-};
-__device__ __forceinline__ Stat stat_of(const NormArgs& a, const Sums& t) {
-  const double m = (double)a.P * a.Cg;
-  const double mean = t.s / m, var = __builtin_fmax(t.q / m - mean * mean, 0.0);
-  // a value that is not finite makes the sum of squares so
-  const bool ok = t.q <= 1.7976931348623157e308;
-  const float nan = __builtin_nanf("");
-  return Stat{ok ? (float)mean : nan, ok ? (float)(1.0 / sqrt(var + (double)a.eps)) : nan};
-}
-
-__device__ __forceinline__ Sums add(const Sums& a, const Sums& b) { return Sums{a.s + b.s, a.q + b.q}; }
-
-// Sums over the TEAM consecutive threads of a team (a power of two; a whole
-// work-group for 256), for all of them.
-template <int TEAM>
-__device__ __forceinline__ Sums team_sum(Sums v) {
-#pragma unroll
-  for (int d = (TEAM < 64 ? TEAM : 64) / 2; d > 0; d >>= 1)
-    v = add(v, Sums{__shfl_xor(v.s, d), __shfl_xor(v.q, d)});
-  if (TEAM > 64) {
-    __shared__ Sums red[NT / 64];
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = add(add(red[0], red[1]), add(red[2], red[3]));
-  }
-  return v;
-}
-
-// For each of `groups` groups the sum of its `n` entries entry(g, i), handed
-// to put(g, sum) by one thread; all threads of the work-group take part.
-template <typename Entry, typename Put>
-__device__ __forceinline__ void group_sums(int groups, int n, Entry entry, Put put) {
-  __shared__ Sums red[NT / 64];
-  if (groups > NT / 64) {
-    // a power of two of threads (at most a wave) per group
-    int sub = 1;
-    while (sub < 64 && sub * 2 * groups <= NT) sub *= 2;
-    const int s = threadIdx.x & (sub - 1);
-    for (int g0 = 0; g0 < groups; g0 += NT / sub) {
-      const int g = g0 + (int)threadIdx.x / sub;
-      Sums v{0.0, 0.0};
-      if (g < groups)
-        for (int i = s; i < n; i += sub) v = add(v, entry(g, i));
-      for (int d = sub / 2; d > 0; d >>= 1) v = add(v, Sums{__shfl_xor(v.s, d), __shfl_xor(v.q, d)});
-      if (g < groups && s == 0) put(g, v);
-    }
-    return;
-  }
-  for (int g = 0; g < groups; ++g) {
-    Sums v{0.0, 0.0};
-    for (int i = threadIdx.x; i < n; i += NT) v = add(v, entry(g, i));
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = add(v, Sums{__shfl_xor(v.s, d), __shfl_xor(v.q, d)});
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    if (threadIdx.x == 0) put(g, add(add(red[0], red[1]), add(red[2], red[3])));
-  }
-}
-
-// x and x^2 added in double: nothing cancels however far a group's mean or a
-// few of its values lie from the rest, and the unit's double additions run at
-// the rate of float ones.
-__device__ __forceinline__ void add_value(Sums* t, float x) {
-  const double d = (double)x;
-  t->s += d;
-  t->q = __builtin_fma(d, d, t->q);
-}
-
-// A thread's items 0 .. count - 1, loaded ahead of their use: the first UN when
-// the stream is made (before what the use needs is worked out), then the next
-// UN while UN are used.  The loads stand outside every condition but that there
-// are items; inside one the compiler moves them next to their use.  An item is
-// loaded before any item from it on is used, so results may overwrite what was
-// loaded.
-template <int UN, typename Load>
-struct Stream {
-  int count;
-  Load load;
-  decltype(load(0)) cur[UN];
-  __device__ __forceinline__ Stream(int n, Load l) : count(n), load(l) {
-    if (count > 0)
-#pragma unroll
-      for (int u = 0; u < UN; ++u) cur[u] = load(u < count ? u : count - 1);
-  }
-  // use(item k, k) for each
-  template <typename Use>
-  __device__ __forceinline__ void run(Use use) {
-    if (count <= 0) return;
-    decltype(load(0)) next[UN];
-    int k = 0;
-#pragma unroll 2
-    for (; k + UN <= count; k += UN) {
-#pragma unroll
-      for (int u = 0; u < UN; ++u) next[u] = load(k + UN + u < count ? k + UN + u : count - 1);
-#pragma unroll
-      for (int u = 0; u < UN; ++u) use(cur[u], k + u);
-#pragma unroll
-      for (int u = 0; u < UN; ++u) cur[u] = next[u];
-    }
-#pragma unroll
-    for (int u = 0; u < UN - 1; ++u)
-      if (k + u < count) use(cur[u], k + u);
-  }
-};
-template <int UN, typename Load>
-__device__ __forceinline__ Stream<UN, Load> stream(int count, Load load) {
-  return Stream<UN, Load>(count, load);
-}
-
-// Vectors of x and of a second tensor.
-template <typename T, int W>
-struct Pair {
-  Vec<T, W> x, y;
-};
 
 // --------------------------------------------------------------------------
 // Channels last, flat
@@ -349,34 +127,6 @@ __device__ __forceinline__ void load_groups(const NormArgs& a, int64_t b, V2* ld
   __syncthreads();
 }
 
-// x - mu.  The factor is one; it is hidden from the compiler so that the fp16
-// conversion folds into the multiply-add.
-__device__ __forceinline__ float less(float x, float mu) { return x - mu; }
-__device__ __forceinline__ float less(_Float16 x, float mu) {
-  float one = 1.0f;
-  asm("" : "+s"(one));
-  return __builtin_fmaf((float)x, one, -mu);
-}
-__device__ __forceinline__ float less(__bf16 x, float mu) { return (float)x - mu; }
-
-// z = (x - mu) k + beta, k = r gamma.  (Not x k + (beta - mu k): where a
-// group's spread is nothing beside its mean, that has mu k 2^-24 of error.)
-struct Line {
-  float mu, k, be;
-};
-__device__ __forceinline__ Line line_of(const NormArgs& a, const Stat& st, int c) {
-  return Line{st.mean, a.gamma ? st.rstd * a.gamma[c] : st.rstd, a.beta ? a.beta[c] : 0.0f};
-}
-template <typename T>
-__device__ __forceinline__ float on_line(const Line& l, T x) {
-  return __builtin_fmaf(less(x, l.mu), l.k, l.be);
-}
-
-__device__ __forceinline__ void write_stat(const NormArgs& a, int64_t bg, const Stat& st) {
-  a.stats[2 * bg] = st.mean;
-  a.stats[2 * bg + 1] = st.rstd;
-}
-
 template <typename T, int ACT, bool UNI>
 __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* lds) {  // [G]
   constexpr int V = kVec<T>, UN = UNI ? 2 : 1;
@@ -434,46 +184,6 @@ __global__ __launch_bounds__(NT, 4) void flat_fwd_kernel(NormArgs a) {
     flat_fwd<T, ACT, UNI>(a, u, reinterpret_cast<Stat*>(smem));
     __syncthreads();
   }
-}
-
-// What the backward needs of a channel: d = x - mu, z = d k + beta (k = r gamma),
-// h = g_out act'(z); the sums of h and, with r put to it at the end, of h d.
-struct Coef {
-  float mu, rs, k, ga, be;
-};
-__device__ __forceinline__ Coef bwd_coef(const NormArgs& a, int64_t bg, int c) {
-  const float* st = a.stats_in + 2 * bg;
-  const float ga = a.gamma ? a.gamma[c] : 1.0f;
-  return Coef{st[0], st[1], st[1] * ga, ga, a.beta ? a.beta[c] : 0.0f};
-}
-// (Both passes form h alike: in a group whose values hardly differ gx is the
-// small difference of large terms, and would show any difference of the two.)
-template <int ACT, typename T>
-__device__ __forceinline__ void bwd_terms(const Coef& k, T x, T g, float* h, float* d) {
-  *d = less(x, k.mu);
-  *h = (float)g * act_grad_f<ACT>(__builtin_fmaf(*d, k.k, k.be));
-}
-// The sums of h and h xh; where the statistics are not finite, not numbers (h
-// itself may be finite there).
-__device__ __forceinline__ float2 bwd_sums(const Coef& k, float s, float q) {
-  return make_float2(__builtin_fmaf(0.0f, k.rs, s), q * k.rs);
-}
-// gx = r (gamma h - a - xh d) with xh = r (x - mu).
-struct Means {
-  float a, d;
-};
-struct Gx {
-  float c0, c1;
-};
-__device__ __forceinline__ Gx gx_coef(const Coef& k, const Means& m) {
-  return Gx{-k.rs * m.a, -(k.rs * m.d) * k.rs};
-}
-__device__ __forceinline__ float bwd_gx(const Coef& k, const Gx& m, float h, float d) {
-  return __builtin_fmaf(k.k, h, __builtin_fmaf(d, m.c1, m.c0));
-}
-__device__ __forceinline__ Means means_of(const NormArgs& a, const Sums& t) {
-  const double m = (double)a.P * a.Cg;
-  return Means{(float)(t.s / m), (float)(t.q / m)};
 }
 
 // lds [A][V]: by thread and element; ch [C]: gamma times the channel's sums.
@@ -542,20 +252,6 @@ __global__ __launch_bounds__(NT, UNI ? 4 : 3) void flat_sums_kernel(NormArgs a) 
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += gridDim.x) {
     flat_sums<T, ACT, UNI>(a, u, lds, reinterpret_cast<Sums*>(lds + (size_t)NT * kVec<T>));
     __syncthreads();
-  }
-}
-
-// One channel's parameter gradients: the sum over samples and chunks.
-__device__ __forceinline__ void param_grads(const NormArgs& a, int c) {
-  Sums v{0.0, 0.0};
-  for (int64_t i = threadIdx.x; i < a.B * a.nc; i += NT) {
-    const int64_t b = i / a.nc;
-    v = add(v, a.chan[(b * a.C + c) * a.nc + (i - b * a.nc)]);
-  }
-  v = team_sum<NT>(v);
-  if (threadIdx.x == 0) {
-    if (a.gbeta) a.gbeta[c] = (float)v.s;
-    if (a.ggamma) a.ggamma[c] = (float)v.q;
   }
 }
 
@@ -969,7 +665,7 @@ fno_status check_desc(const fno_norm_desc* d) {
   return FNO_OK;
 }
 
-enum Route { FLAT, WIDE, FIRST };
+enum Route { FLAT, WIDE, FIRST, RESIDENT };
 constexpr int kFill = 1024;        // work-groups that fill the chip (four per compute unit)
 constexpr int kMaxGrid = 1 << 20;  // work-groups of a launch; more work is looped over
 
@@ -980,6 +676,7 @@ struct NormPlan {
   bool uni;    // flat: a vector's channels are of one group
   int team;    // first
   int64_t units;  // work items of each pass
+  bool first;     // channels first
 };
 
 NormPlan plan_of(const fno_norm_desc& d) {
@@ -995,7 +692,13 @@ NormPlan plan_of(const fno_norm_desc& d) {
   a.act = d.activation;
   a.eps = d.eps;
   p.vec = V;
-  if (d.layout == FNO_LAYOUT_CHANNELS_FIRST) {
+  p.first = d.layout == FNO_LAYOUT_CHANNELS_FIRST;
+  if (norm_resident_fits(a, d.dtype, p.first)) {
+    p.route = RESIDENT;
+    a.nc = 1;
+    return p;
+  }
+  if (p.first) {
     // A wave per plane up to 16 vectors a lane, else work-groups on segments
     // of at least eight vectors a thread, up to eight times what fills the
     // chip: the memory keeps busiest while work-groups start and end at
@@ -1058,7 +761,7 @@ struct WsLayout {
 WsLayout ws_of(const NormPlan& p, bool bwd) {
   const NormArgs& a = p.a;
   WsLayout w;
-  w.joined = rup(a.B * a.G * a.n * (int64_t)sizeof(Sums), 256);
+  w.joined = rup(std::max<int64_t>(1, a.B * a.G * a.n) * (int64_t)sizeof(Sums), 256);
   w.chan = w.joined + rup(a.B * a.G * (int64_t)sizeof(Sums), 256);
   w.bytes = w.chan + (bwd ? rup(a.B * a.C * a.nc * (int64_t)sizeof(Sums), 256) : 0);
   return w;
@@ -1172,6 +875,7 @@ hipError_t by_act(NormLaunch& L, bool bwd) {
 }
 
 hipError_t by_type(NormLaunch& L, bool bwd) {
+  if (L.p.route == RESIDENT) return norm_resident_launch(L.p.a, L.dt, L.p.first, bwd, L.s);
   return L.dt == FNO_DTYPE_F32   ? by_act<float>(L, bwd)
          : L.dt == FNO_DTYPE_F16 ? by_act<_Float16>(L, bwd)
                                  : by_act<__bf16>(L, bwd);
