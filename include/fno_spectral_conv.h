@@ -494,10 +494,11 @@ typedef struct {
 } fno_adamw_desc;
 
 /* What steps of one optimizer share on the device, for training without a
- * host read between backward and update, and under HIP graph capture: 48
- * bytes of device memory, zeroed by the caller before first use except for
- * lr_factor = 1 (and step, to go on from a checkpoint).  fno_grad_norm writes
- * all but lr_factor. */
+ * host read between backward and update, and under HIP graph capture: 64
+ * bytes of device memory, zeroed by the caller before first use (and after a
+ * call that failed) except for lr_factor = 1 and, to go on from a checkpoint,
+ * step.  fno_grad_norm writes all but lr_factor; its calls with one block
+ * belong on one stream. */
 typedef struct {
   int64_t step;       /* steps taken */
   int64_t skipped;    /* steps left out for non-finite gradients */
@@ -507,6 +508,8 @@ typedef struct {
   float grad_scale;   /* what the step multiplies gradients with */
   int32_t skip;       /* 1: the last gradients were not finite */
   float lr_factor;    /* multiplies lr (the caller's: a schedule under replay) */
+  int32_t arrived;    /* the library's own; 0 between calls */
+  int32_t reserved[3];
 } fno_adamw_control;
 
 /* The global gradient norm with clip, loss-scale removal and non-finite check:

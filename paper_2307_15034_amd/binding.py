@@ -147,6 +147,8 @@ class FnoAdamwControl(ctypes.Structure):
         ("grad_scale", ctypes.c_float),
         ("skip", ctypes.c_int32),
         ("lr_factor", ctypes.c_float),
+        ("arrived", ctypes.c_int32),
+        ("reserved", ctypes.c_int32 * 3),
     ]
 
 

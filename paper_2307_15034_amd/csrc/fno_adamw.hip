@@ -17,6 +17,7 @@ namespace fno {
 namespace {
 
 constexpr int kBatch = FNO_ADAMW_LAUNCH_TENSORS;
+constexpr int kNormBatch = 128;              // tensors of a launch of the norm
 constexpr int kBlk = FNO_ADAMW_BLOCK;
 constexpr int64_t kChunk = 2048;             // elements of a work-group of the step
 constexpr int64_t kNormChunk = 8192;         // elements of a work-group of the norm
@@ -110,13 +111,18 @@ __device__ __forceinline__ T rounded(float x) {
   return (T)x;
 }
 
-// The tensor of chunk c: the last i with first[i] <= c.  Every lane looks at
-// one entry (kBatch <= 64), all in one load.
-__device__ __forceinline__ int find_tensor(const int32_t* first, int count, int c) {
-  static_assert(kBatch <= 64, "one entry per lane");
-  const int lane = threadIdx.x & 63;
-  const uint64_t below = __ballot(lane < count && first[lane < count ? lane : 0] <= c);
-  return 63 - __builtin_clzll(below);
+// The tensor of chunk c: the last i with first[i] <= c.  Every lane looks at an
+// entry (of N <= 128: at two), all in one or two loads.
+template <int N>
+__device__ __forceinline__ int find_tensor(const int32_t (&first)[N], int count, int c) {
+  static_assert(N <= 129, "two entries per lane");
+  const int lane = threadIdx.x & 63, last = count - 1;
+  int i = __builtin_popcountll(__ballot(lane <= last && first[lane <= last ? lane : last] <= c));
+  if (N > 65) {
+    const int l2 = lane + 64;
+    i += __builtin_popcountll(__ballot(l2 <= last && first[l2 <= last ? l2 : last] <= c));
+  }
+  return i - 1;
 }
 
 struct Consts {  // an element's step in floats
@@ -166,18 +172,19 @@ __device__ inline float decode_v(float b, int q) {
   const float s = (b * (1.0f / 65025.0f)) * (float)(q * q);
   return s * s;
 }
-// Four elements of an array of any type as floats, all loads before the first use.
-__device__ __forceinline__ void load_any(const void* p, int dt, const int64_t (&at)[4], float (&x)[4]) {
-  uint32_t raw[4];
+// Elements of an array of any type as floats, all loads before the first use.
+template <int N>
+__device__ __forceinline__ void load_any(const void* p, int dt, const int64_t (&at)[N], float (&x)[N]) {
+  uint32_t raw[N];
   if (dt == FNO_DTYPE_F32) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) raw[j] = static_cast<const uint32_t*>(p)[at[j]];
+    for (int j = 0; j < N; ++j) raw[j] = static_cast<const uint32_t*>(p)[at[j]];
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) raw[j] = static_cast<const uint16_t*>(p)[at[j]];
+    for (int j = 0; j < N; ++j) raw[j] = static_cast<const uint16_t*>(p)[at[j]];
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < N; ++j)
     x[j] = dt == FNO_DTYPE_F32   ? __uint_as_float(raw[j])
            : dt == FNO_DTYPE_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)raw[j])
                                  : __uint_as_float(raw[j] << 16);
@@ -311,77 +318,86 @@ __device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, co
 }
 
 // A tensor's last chunk, of any types: elements lie across the lanes, 64 of a
-// block at a time; loads past the end read the last element and are dropped.
+// block at a time; loads past the end read the last element (block) and are
+// dropped, so that here too all of them are in flight at once.
 template <int BITS>
 __device__ __forceinline__ void last_chunk(const AdamTensor& t, int64_t base, const Consts& k) {
-  constexpr int U = (int)kChunk / 1024;
+  constexpr int U = (int)kChunk / 1024, N = 4 * U;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll 1
+  float p[N], g[N], m[N], v[N], w[N], as[U], bs[U];
+  int64_t at[N];
+  bool in[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int64_t e = base + (4 * (i / 4) + wave) * kBlk + 64 * (i % 4) + lane;
+    in[i] = e < t.n;
+    at[i] = in[i] ? e : t.n - 1;
+  }
+  load_any(t.master ? t.master : t.p, t.master ? FNO_DTYPE_F32 : t.pdt, at, p);
+  load_any(t.g, t.gdt, at, g);
+  if (BITS == 32) {
+    load_any(t.m, FNO_DTYPE_F32, at, m);
+    load_any(t.v, FNO_DTYPE_F32, at, v);
+  } else {
+    int qm[N], qv[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      qm[i] = static_cast<const int8_t*>(t.m)[at[i]];
+      qv[i] = static_cast<const uint8_t*>(t.v)[at[i]];
+      if (i % 4 == 0) {
+        as[i / 4] = t.ms[at[i] / kBlk];
+        bs[i / 4] = t.vs[at[i] / kBlk];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      m[i] = decode_m(as[i / 4], qm[i]);
+      v[i] = decode_v(bs[i / 4], qv[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    p[i] = adam_element(k, p[i], g[i], &m[i], &v[i], &w[i]);
+    if (!in[i]) continue;
+    if (t.master) t.master[at[i]] = p[i];
+    if (t.pdt == FNO_DTYPE_F32) static_cast<float*>(t.p)[at[i]] = p[i];
+    else if (t.pdt == FNO_DTYPE_F16) static_cast<_Float16*>(t.p)[at[i]] = rounded<_Float16>(p[i]);
+    else static_cast<__bf16*>(t.p)[at[i]] = rounded<__bf16>(p[i]);
+    if (BITS == 32) {
+      static_cast<float*>(t.m)[at[i]] = m[i];
+      static_cast<float*>(t.v)[at[i]] = v[i];
+    }
+  }
+  if (BITS == 32) return;
+#pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t b = base / kBlk + 4 * u + wave;
-    if (b * kBlk >= t.n) break;
-    float p[4], g[4], m[4], v[4];
-    int64_t at[4];
-    f4 w, am;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t e = b * kBlk + 64 * j + lane;
-      at[j] = e < t.n ? e : t.n - 1;
-    }
-    load_any(t.master ? t.master : t.p, t.master ? FNO_DTYPE_F32 : t.pdt, at, p);
-    load_any(t.g, t.gdt, at, g);
-    if (BITS == 32) {
-      load_any(t.m, FNO_DTYPE_F32, at, m);
-      load_any(t.v, FNO_DTYPE_F32, at, v);
-    } else {
-      int qm[4], qv[4];
-      const float as = t.ms[b], bs = t.vs[b];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        qm[j] = static_cast<const int8_t*>(t.m)[at[j]];
-        qv[j] = static_cast<const uint8_t*>(t.v)[at[j]];
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m[j] = decode_m(as, qm[j]);
-        v[j] = decode_v(bs, qv[j]);
-      }
-    }
+    if (b * kBlk >= t.n) break;  // the same for the wave's lanes
     uint32_t ma = 0, mb = 0;
+    f4 am, wm, cm, cv;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool in = b * kBlk + 64 * j + lane < t.n;
-      float wj;
-      p[j] = adam_element(k, p[j], g[j], &m[j], &v[j], &wj);
-      w[j] = wj;
-      am[j] = __builtin_fabsf(m[j]);
-      ma = max(ma, abs_bits(m[j]));  // past the end: the last element's own, once more
-      mb = max(mb, abs_bits(wj));
-      if (!in) continue;
-      if (t.master) t.master[at[j]] = p[j];
-      if (t.pdt == FNO_DTYPE_F32) static_cast<float*>(t.p)[at[j]] = p[j];
-      else if (t.pdt == FNO_DTYPE_F16) static_cast<_Float16*>(t.p)[at[j]] = rounded<_Float16>(p[j]);
-      else static_cast<__bf16*>(t.p)[at[j]] = rounded<__bf16>(p[j]);
-      if (BITS == 32) {
-        static_cast<float*>(t.m)[at[j]] = m[j];
-        static_cast<float*>(t.v)[at[j]] = v[j];
+      const int i = 4 * u + j;
+      am[j] = __builtin_fabsf(m[i]);
+      wm[j] = w[i];
+      if (in[i]) {
+        ma = max(ma, abs_bits(m[i]));
+        mb = max(mb, abs_bits(w[i]));
       }
     }
-    if (BITS == 8) {
-      const float A = __uint_as_float(wave_max(ma)), Bt = __uint_as_float(wave_max(mb));
-      f4 cm, cv;
-      codes4(am, A, 127.0f, &cm);
-      codes4(w, Bt, 255.0f, &cv);
+    const float A = __uint_as_float(wave_max(ma)), Bt = __uint_as_float(wave_max(mb));
+    codes4(am, A, 127.0f, &cm);
+    codes4(wm, Bt, 255.0f, &cv);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (b * kBlk + 64 * j + lane >= t.n) continue;
-        static_cast<int8_t*>(t.m)[at[j]] = signed_code(cm[j], m[j]);
-        static_cast<uint8_t*>(t.v)[at[j]] = unsigned_code(cv[j], w[j]);
-      }
-      if (lane == 0) {
-        t.ms[b] = A;
-        t.vs[b] = Bt;
-      }
+    for (int j = 0; j < 4; ++j) {
+      const int i = 4 * u + j;
+      if (!in[i]) continue;
+      static_cast<int8_t*>(t.m)[at[i]] = signed_code(cm[j], m[i]);
+      static_cast<uint8_t*>(t.v)[at[i]] = unsigned_code(cv[j], w[i]);
+    }
+    if (lane == 0) {
+      t.ms[b] = A;
+      t.vs[b] = Bt;
     }
   }
 }
@@ -523,30 +539,39 @@ __device__ __forceinline__ double square_sum(const G* g, int64_t base, int64_t n
   return s;
 }
 
-__global__ __launch_bounds__(256) void grad_sq_kernel(AdamArgs a, double* part) {
-  const int i = find_tensor(a.first, a.count, (int)blockIdx.x);
-  const AdamTensor& t = a.t[i];
-  const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * kNormChunk;
-  double s;
-  if (t.gdt == FNO_DTYPE_F32) s = square_sum(static_cast<const float*>(t.g), base, t.n);
-  else if (t.gdt == FNO_DTYPE_F16) s = square_sum(static_cast<const _Float16*>(t.g), base, t.n);
-  else s = square_sum(static_cast<const __bf16*>(t.g), base, t.n);
-  s = block_sum<256>(s);
-  if (threadIdx.x == 0) part[blockIdx.x] = s;
-}
+// A batch's gradients alone.
+struct NormTensor {
+  const void* g;
+  int64_t n;
+};
+struct NormArgs {
+  NormTensor t[kNormBatch];
+  int32_t first[kNormBatch + 1];
+  int8_t dt[kNormBatch];
+  int32_t count;
+};
 
-__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* part, int64_t n, double b1,
-                                                        double b2, double max_norm,
-                                                        double inv_scale, fno_adamw_control* ctl) {
+struct NormOut {
+  double* part;  // the whole list's sums, by chunk
+  int64_t chunks;
+  double b1, b2, max_norm, inv_scale;
+  fno_adamw_control* ctl;
+};
+
+// The control block from the chunks' sums, by the THREADS threads of a
+// work-group; `load` reads a sum.
+template <int THREADS, typename Load>
+__device__ __forceinline__ void finish_norm(const NormOut& o, Load load) {
   double s = 0.0;
 #pragma unroll 8
-  for (int64_t e = threadIdx.x; e < n; e += 1024) s += part[e];
-  const double sum = block_sum<1024>(s);
+  for (int64_t e = threadIdx.x; e < o.chunks; e += THREADS) s += load(o.part + e);
+  const double sum = block_sum<THREADS>(s);
   if (threadIdx.x != 0) return;
-  const double norm = sqrt(sum) * inv_scale;
+  fno_adamw_control* ctl = o.ctl;
+  const double norm = sqrt(sum) * o.inv_scale;
   const bool ok = sum <= 1.7976931348623157e308;  // false for inf and NaN
   ctl->grad_norm = (float)norm;
-  ctl->grad_scale = (float)(norm > max_norm ? inv_scale * (max_norm / norm) : inv_scale);
+  ctl->grad_scale = (float)(norm > o.max_norm ? o.inv_scale * (o.max_norm / norm) : o.inv_scale);
   ctl->skip = ok ? 0 : 1;
   if (!ok) {
     ctl->skipped += 1;
@@ -554,8 +579,45 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* part, int
   }
   const int64_t t = ctl->step + 1;
   ctl->step = t;
-  ctl->bias1 = 1.0 / (1.0 - int_pow(b1, t));
-  ctl->bias2 = 1.0 / sqrt(1.0 - int_pow(b2, t));
+  ctl->bias1 = 1.0 / (1.0 - int_pow(o.b1, t));
+  ctl->bias2 = 1.0 / sqrt(1.0 - int_pow(o.b2, t));
+}
+
+// JOIN: the work-group that ends last forms the norm.  Its sum was made
+// visible to the device before it counted itself (release), and it reads the
+// others' after it saw that all had (acquire); it leaves the count at zero.
+template <bool JOIN>
+__global__ __launch_bounds__(256) void grad_sq_kernel(NormArgs a, NormOut o, int64_t at) {
+  const int i = find_tensor(a.first, a.count, (int)blockIdx.x);
+  const NormTensor t = a.t[i];
+  const int dt = a.dt[i];
+  const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * kNormChunk;
+  double s;
+  if (dt == FNO_DTYPE_F32) s = square_sum(static_cast<const float*>(t.g), base, t.n);
+  else if (dt == FNO_DTYPE_F16) s = square_sum(static_cast<const _Float16*>(t.g), base, t.n);
+  else s = square_sum(static_cast<const __bf16*>(t.g), base, t.n);
+  s = block_sum<256>(s);
+  if (!JOIN) {
+    if (threadIdx.x == 0) o.part[at + blockIdx.x] = s;
+    return;
+  }
+  __shared__ bool last;
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(o.part + at + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int32_t before = __hip_atomic_fetch_add(&o.ctl->arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    last = before == (int32_t)o.chunks - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  finish_norm<256>(o, [](const double* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  });
+  if (threadIdx.x == 0) o.ctl->arrived = 0;
+}
+
+__global__ __launch_bounds__(1024) void grad_norm_kernel(NormOut o) {
+  finish_norm<1024>(o, [](const double* p) { return *p; });
 }
 
 // --------------------------------------------------------------------------
@@ -594,18 +656,28 @@ bool check_tensor(const fno_adamw_tensor& t) {
   return t.n == 0 || (ok16(t.param) && (!t.master || ok16(t.master)));
 }
 
+void put(AdamArgs* a, const fno_adamw_tensor& x) {
+  a->t[a->count] = AdamTensor{x.param, x.master, x.grad, x.exp_avg, x.exp_avg_sq,
+                              x.exp_avg_scale, x.exp_avg_sq_scale, x.n, x.param_dtype,
+                              x.grad_dtype, x.state_bits, x.weight_decay};
+}
+void put(NormArgs* a, const fno_adamw_tensor& x) {
+  a->t[a->count] = NormTensor{x.grad, x.n};
+  a->dt[a->count] = (int8_t)x.grad_dtype;
+}
+
 // The next launch's tensors from list position *i on; returns its chunks.
-int64_t next_batch(const fno_adamw_tensor* t, int64_t count, int64_t chunk, int64_t* i, AdamArgs* a) {
+template <typename Args>
+int64_t next_batch(const fno_adamw_tensor* t, int64_t count, int64_t chunk, int64_t* i, Args* a) {
+  constexpr int most = (int)(sizeof(a->t) / sizeof(a->t[0]));
   int64_t chunks = 0;
   a->count = 0;
-  for (; *i < count && a->count < kBatch; ++*i) {
+  for (; *i < count && a->count < most; ++*i) {
     const fno_adamw_tensor& x = t[*i];
     if (x.n == 0) continue;
     const int64_t c = cdiv(x.n, chunk);
     if (a->count && chunks + c > kMaxGrid) break;
-    a->t[a->count] = AdamTensor{x.param, x.master, x.grad, x.exp_avg, x.exp_avg_sq,
-                                x.exp_avg_scale, x.exp_avg_sq_scale, x.n, x.param_dtype,
-                                x.grad_dtype, x.state_bits, x.weight_decay};
+    put(a, x);
     a->first[a->count++] = (int32_t)chunks;
     chunks += c;
   }
@@ -620,9 +692,9 @@ int64_t norm_chunks(const fno_adamw_tensor* t, int64_t count) {
 }
 
 // Runs `launch(args, chunks, list index of the first tensor)` over the batches of a list.
-template <typename F>
+template <typename Args, typename F>
 hipError_t over_batches(const fno_adamw_tensor* t, int64_t count, int64_t chunk, F launch) {
-  AdamArgs a;
+  Args a;
   for (int64_t i = 0; i < count;) {
     const int64_t from = i;
     const int64_t chunks = next_batch(t, count, chunk, &i, &a);
@@ -644,7 +716,7 @@ struct StepLaunch {
 
 hipError_t launch_step(void* ctx) {
   const StepLaunch& L = *static_cast<StepLaunch*>(ctx);
-  return over_batches(L.t, L.count, kChunk, [&](const AdamArgs& a, int64_t chunks, int64_t) {
+  return over_batches<AdamArgs>(L.t, L.count, kChunk, [&](const AdamArgs& a, int64_t chunks, int64_t) {
     hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)chunks), dim3(256), 0, L.s, a, L.h, L.ctl);
   });
 }
@@ -652,23 +724,27 @@ hipError_t launch_step(void* ctx) {
 struct NormLaunch {
   const fno_adamw_tensor* t;
   int64_t count;
-  double b1, b2, max_norm, inv_scale;
-  fno_adamw_control* ctl;
-  double* part;
+  NormOut o;
   hipStream_t s;
 };
 
+// Up to kJoin chunks the last work-group of the sums forms the norm too (the
+// launch that it saves is a third of a small model's step); beyond, counting
+// every work-group would cost more than a launch of its own.
+constexpr int64_t kJoin = 512;
+
 hipError_t launch_norm(void* ctx) {
   const NormLaunch& L = *static_cast<NormLaunch*>(ctx);
+  const bool join = L.o.chunks > 0 && L.o.chunks <= kJoin;
   int64_t at = 0;
   const hipError_t e =
-      over_batches(L.t, L.count, kNormChunk, [&](const AdamArgs& a, int64_t chunks, int64_t) {
-        hipLaunchKernelGGL(grad_sq_kernel, dim3((unsigned)chunks), dim3(256), 0, L.s, a, L.part + at);
+      over_batches<NormArgs>(L.t, L.count, kNormChunk, [&](const NormArgs& a, int64_t chunks, int64_t) {
+        hipLaunchKernelGGL(join ? grad_sq_kernel<true> : grad_sq_kernel<false>, dim3((unsigned)chunks),
+                           dim3(256), 0, L.s, a, L.o, at);
         at += chunks;
       });
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, L.s, L.part, at, L.b1, L.b2,
-                     L.max_norm, L.inv_scale, L.ctl);
+  if (e != hipSuccess || join) return e;
+  hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, L.s, L.o);
   return hipGetLastError();
 }
 
@@ -685,7 +761,7 @@ hipError_t launch_moments(void* ctx) {
   const MomentLaunch& L = *static_cast<MomentLaunch*>(ctx);
   MomentArgs ma;
   ma.dt = L.dt;
-  return over_batches(L.t, L.count, kMomentChunk, [&](const AdamArgs& a, int64_t chunks, int64_t from) {
+  return over_batches<AdamArgs>(L.t, L.count, kMomentChunk, [&](const AdamArgs& a, int64_t chunks, int64_t from) {
     ma.a = a;
     for (int64_t i = from, j = 0; j < a.count; ++i) {
       if (L.t[i].n == 0) continue;
@@ -729,8 +805,10 @@ extern "C" fno_status fno_grad_norm(const fno_adamw_desc* d, const fno_adamw_ten
   if (st != FNO_OK) return st;
   if (ws_len < need) return FNO_ERR_WORKSPACE_TOO_SMALL;
   if (!ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
-  NormLaunch L{t, count, d->beta1, d->beta2, max_norm, inv_loss_scale, control,
-               static_cast<double*>(ws), stream};
+  NormLaunch L{t, count,
+               NormOut{static_cast<double*>(ws), norm_chunks(t, count), d->beta1, d->beta2, max_norm,
+                       inv_loss_scale, control},
+               stream};
   return timed_status("grad_norm", stream, launch_norm, &L);
 }
 

@@ -321,10 +321,10 @@ def _stream_of(device: torch.device, stream: Optional[int]) -> int:
     """The stream a call runs on: `stream`, or torch's current one on
     `device`, which has to be the current device (the library launches
     there)."""
-    if device.index is not None and device.index != torch.cuda.current_device():
-        raise ValueError(f"the current device is cuda:{torch.cuda.current_device()}, the tensors "
-                         f"live on {device}")
-    return torch.cuda.current_stream().cuda_stream if stream is None else stream
+    current = torch.cuda.current_device()
+    if device.index != current:
+        raise ValueError(f"the current device is cuda:{current}, the tensors live on {device}")
+    return torch.cuda.current_stream(current).cuda_stream if stream is None else stream
 
 
 class GroupNormAct:
@@ -369,23 +369,26 @@ class GroupNormAct:
     def _workspace(self, device):
         if self._ws is None or self._ws.device != device:
             self._ws = torch.empty(max(self.ws_bytes.values()), dtype=torch.uint8, device=device)
-        return self._ws
+        return self._ws.data_ptr(), self._ws.numel()
 
     def _t(self, t, name, device):
-        return _addr(t, self.shape, self.dtype, name, device)
+        return 0 if t is None else _addr(t, self.shape, self.dtype, name, device)
 
     def _c(self, t, name, device):
-        return _addr(t, (self.channels,), torch.float32, name, device)
+        return 0 if t is None else _addr(t, (self.channels,), torch.float32, name, device)
 
     def _s(self, t, device):
-        return _addr(t, (self.batch, self.groups, 2), torch.float32, "stats", device)
+        return 0 if t is None else _addr(t, (self.batch, self.groups, 2), torch.float32, "stats",
+                                         device)
 
-    def _new(self, t, shape, dtype, stream, name):
-        if t is not None:
-            return t
+    @staticmethod
+    def _given(stream, name):
         if stream is not None:
             raise ValueError(f"{name} is required where a stream is given")
-        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _new(self, like, stream, name):
+        self._given(stream, name)
+        return torch.empty_like(like)
 
     def fwd(self, x, gamma=None, beta=None, residual=None, out=None, stats=None,
             keep_stats: bool = True, stream: Optional[int] = None):
@@ -396,16 +399,16 @@ class GroupNormAct:
         ax, dev = self._t(x, "x", self.device), x.device
         ar = self._t(residual, "residual", dev)
         ag, ab = self._c(gamma, "gamma", dev), self._c(beta, "beta", dev)
-        self._t(out, "out", dev)
-        self._s(stats, dev)
+        ao, ast = self._t(out, "out", dev), self._s(stats, dev)
         s = _stream_of(dev, stream)
-        out = self._new(out, self.shape, self.dtype, stream, "out")
-        if keep_stats:
-            stats = self._new(stats, (self.batch, self.groups, 2), torch.float32, stream, "stats")
-        ws = self._workspace(dev)
-        B.fno_group_norm_act_fwd(self.desc, ax, ag, ab, ar, out.data_ptr(),
-                                 stats.data_ptr() if stats is not None else 0, ws.data_ptr(),
-                                 ws.numel(), s)
+        if out is None:
+            out = self._new(x, stream, "out")
+            ao = out.data_ptr()
+        if stats is None and keep_stats:
+            self._given(stream, "stats")
+            stats = torch.empty((self.batch, self.groups, 2), dtype=torch.float32, device=dev)
+            ast = stats.data_ptr()
+        B.fno_group_norm_act_fwd(self.desc, ax, ag, ab, ar, ao, ast, *self._workspace(dev), s)
         return out, stats
 
     def bwd(self, x, g_out, stats, gamma=None, beta=None, gx=None, g_gamma=None, g_beta=None,
@@ -418,15 +421,20 @@ class GroupNormAct:
         ax, dev = self._t(x, "x", self.device), x.device
         ago, ast = self._t(g_out, "g_out", dev), self._s(stats, dev)
         ag, ab = self._c(gamma, "gamma", dev), self._c(beta, "beta", dev)
-        self._t(gx, "gx", dev)
-        self._c(g_gamma, "g_gamma", dev)
-        self._c(g_beta, "g_beta", dev)
+        agx = self._t(gx, "gx", dev)
+        agg, agb = self._c(g_gamma, "g_gamma", dev), self._c(g_beta, "g_beta", dev)
         s = _stream_of(dev, stream)
-        gx = self._new(gx, self.shape, self.dtype, stream, "gx")
-        g_gamma = self._new(g_gamma, (self.channels,), torch.float32, stream, "g_gamma")
-        g_beta = self._new(g_beta, (self.channels,), torch.float32, stream, "g_beta")
-        ws = self._workspace(dev)
-        B.fno_group_norm_act_bwd(self.desc, ax, ag, ab, ast, ago, gx.data_ptr(),
-                                 g_gamma.data_ptr(), g_beta.data_ptr(), ws.data_ptr(),
-                                 ws.numel(), s)
+        if gx is None:
+            gx = self._new(x, stream, "gx")
+            agx = gx.data_ptr()
+        if g_gamma is None:
+            self._given(stream, "g_gamma")
+            g_gamma = torch.empty(self.channels, dtype=torch.float32, device=dev)
+            agg = g_gamma.data_ptr()
+        if g_beta is None:
+            self._given(stream, "g_beta")
+            g_beta = torch.empty(self.channels, dtype=torch.float32, device=dev)
+            agb = g_beta.data_ptr()
+        B.fno_group_norm_act_bwd(self.desc, ax, ag, ab, ast, ago, agx, agg, agb,
+                                 *self._workspace(dev), s)
         return gx, g_gamma, g_beta

@@ -199,7 +199,7 @@ class AdamW:
         if self.control is None:
             raise ValueError("read_control needs device_control=True")
         c = B.FnoAdamwControl.from_buffer_copy(bytes(self.control.cpu().numpy()))
-        return {k: getattr(c, k) for k, _ in c._fields_}
+        return {k: getattr(c, k) for k, _ in c._fields_ if k not in ("arrived", "reserved")}
 
     def moments(self, exp_avg: Optional[Sequence[torch.Tensor]] = None,
                 exp_avg_sq: Optional[Sequence[torch.Tensor]] = None,
