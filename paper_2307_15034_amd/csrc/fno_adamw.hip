@@ -19,7 +19,8 @@ namespace {
 constexpr int kBatch = FNO_ADAMW_LAUNCH_TENSORS;
 constexpr int kNormBatch = 128;              // tensors of a launch of the norm
 constexpr int kBlk = FNO_ADAMW_BLOCK;
-constexpr int64_t kChunk = 2048;             // elements of a work-group of the step
+constexpr int64_t kPiece = 1024;             // elements that a work-group of the step loads at once:
+                                             // a block of the 8-bit states per wave
 constexpr int64_t kNormChunk = 8192;         // elements of a work-group of the norm
 constexpr int64_t kMomentChunk = 4096;       // elements of a work-group that reads moments out
 constexpr int64_t kMaxN = (int64_t)1 << 34;  // elements of a tensor
@@ -174,7 +175,7 @@ __device__ inline float decode_v(float b, int q) {
 }
 // Elements of an array of any type as floats, all loads before the first use.
 template <int N>
-__device__ __forceinline__ void load_any(const void* p, int dt, const int64_t (&at)[N], float (&x)[N]) {
+__device__ __forceinline__ void load_any(const void* p, int dt, const uint32_t (&at)[N], float (&x)[N]) {
   uint32_t raw[N];
   if (dt == FNO_DTYPE_F32) {
 #pragma unroll
@@ -214,7 +215,7 @@ __device__ __forceinline__ float code_exact(float x, float top, float levels) {
 // the nearest integer is the same unless a half lies that near.  Where one of
 // the wave's values is (about one wave in nine), all take the divisions and
 // rounded roots.  (These cost 60 operations an element for both moments: the
-// step of 2^28 fp32 parameters took @SLOW@ us with them everywhere, @FAST@ us so.)
+// step of 268 M fp32 parameters takes 987 us with them everywhere, 827 so.)
 __device__ __forceinline__ void codes4(const f4& x, float top, float levels, f4* q) {
   const float r = __builtin_amdgcn_rcpf(top > 0.0f ? top : 1.0f);
   bool near = false;
@@ -233,9 +234,8 @@ __device__ __forceinline__ void codes4(const f4& x, float top, float levels, f4*
 // A chunk that lies inside its tensor: each thread takes four consecutive
 // elements at a time, so that a wave covers 256, a block of the 8-bit states;
 // all loads of the chunk are in flight before the first element's step.
-template <typename P, typename G, bool MASTER, int BITS>
+template <typename P, typename G, bool MASTER, int BITS, int U>
 __device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, const Consts& k) {
-  constexpr int U = (int)kChunk / 1024;
   using PV = typename Vec4<P>::type;
   using GV = typename Vec4<G>::type;
   const int64_t e0 = base + 4 * threadIdx.x;
@@ -317,124 +317,124 @@ __device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, co
   }
 }
 
-// A tensor's last chunk, of any types: elements lie across the lanes, 64 of a
-// block at a time; loads past the end read the last element (block) and are
-// dropped, so that here too all of them are in flight at once.
+// The last piece of a tensor, of any types: elements lie across the lanes, 64 of
+// a block at a time; loads past the end read the last element and are dropped,
+// so that here too all of them are in flight at once.
 template <int BITS>
-__device__ __forceinline__ void last_chunk(const AdamTensor& t, int64_t base, const Consts& k) {
-  constexpr int U = (int)kChunk / 1024, N = 4 * U;
+__device__ __forceinline__ void last_piece(const AdamTensor& t, int64_t base, const Consts& k) {
+  constexpr int N = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float p[N], g[N], m[N], v[N], w[N], as[U], bs[U];
-  int64_t at[N];
-  bool in[N];
+  const int left = (int)(t.n - base < kPiece ? t.n - base : kPiece);  // elements of the piece
+  const int first = wave * kBlk + lane;
+  float p[N], g[N], m[N], v[N];
+  uint32_t at[N];  // from `base` on
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int64_t e = base + (4 * (i / 4) + wave) * kBlk + 64 * (i % 4) + lane;
-    in[i] = e < t.n;
-    at[i] = in[i] ? e : t.n - 1;
+    const int e = first + 64 * i;
+    at[i] = (uint32_t)(e < left ? e : left - 1);
   }
-  load_any(t.master ? t.master : t.p, t.master ? FNO_DTYPE_F32 : t.pdt, at, p);
-  load_any(t.g, t.gdt, at, g);
+  const int ps = t.master || t.pdt == FNO_DTYPE_F32 ? 4 : 2, gs = t.gdt == FNO_DTYPE_F32 ? 4 : 2;
+  load_any(static_cast<const char*>(t.master ? t.master : t.p) + base * ps, t.master ? FNO_DTYPE_F32 : t.pdt, at, p);
+  load_any(static_cast<const char*>(t.g) + base * gs, t.gdt, at, g);
+  float *m32 = static_cast<float*>(t.m) + base, *v32 = static_cast<float*>(t.v) + base;
+  int8_t* m8 = static_cast<int8_t*>(t.m) + base;
+  uint8_t* v8 = static_cast<uint8_t*>(t.v) + base;
+  float *ms = t.ms + base / kBlk, *vs = t.vs + base / kBlk;
   if (BITS == 32) {
-    load_any(t.m, FNO_DTYPE_F32, at, m);
-    load_any(t.v, FNO_DTYPE_F32, at, v);
+    load_any(m32, FNO_DTYPE_F32, at, m);
+    load_any(v32, FNO_DTYPE_F32, at, v);
   } else {
     int qm[N], qv[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      qm[i] = static_cast<const int8_t*>(t.m)[at[i]];
-      qv[i] = static_cast<const uint8_t*>(t.v)[at[i]];
-      if (i % 4 == 0) {
-        as[i / 4] = t.ms[at[i] / kBlk];
-        bs[i / 4] = t.vs[at[i] / kBlk];
-      }
+      qm[i] = m8[at[i]];
+      qv[i] = v8[at[i]];
     }
+    const float as = ms[at[0] / kBlk], bs = vs[at[0] / kBlk];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      m[i] = decode_m(as[i / 4], qm[i]);
-      v[i] = decode_v(bs[i / 4], qv[i]);
+      m[i] = decode_m(as, qm[i]);
+      v[i] = decode_v(bs, qv[i]);
     }
   }
+  if (wave * kBlk >= left) return;  // the same for the wave's lanes
+  uint32_t ma = 0, mb = 0;
+  f4 am, wm;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    p[i] = adam_element(k, p[i], g[i], &m[i], &v[i], &w[i]);
-    if (!in[i]) continue;
-    if (t.master) t.master[at[i]] = p[i];
-    if (t.pdt == FNO_DTYPE_F32) static_cast<float*>(t.p)[at[i]] = p[i];
-    else if (t.pdt == FNO_DTYPE_F16) static_cast<_Float16*>(t.p)[at[i]] = rounded<_Float16>(p[i]);
-    else static_cast<__bf16*>(t.p)[at[i]] = rounded<__bf16>(p[i]);
+    float w;
+    p[i] = adam_element(k, p[i], g[i], &m[i], &v[i], &w);
+    am[i] = __builtin_fabsf(m[i]);
+    wm[i] = w;
+    if (first + 64 * i >= left) continue;
+    ma = max(ma, abs_bits(m[i]));
+    mb = max(mb, abs_bits(w));
+    if (t.master) (t.master + base)[at[i]] = p[i];
+    if (t.pdt == FNO_DTYPE_F32) (static_cast<float*>(t.p) + base)[at[i]] = p[i];
+    else if (t.pdt == FNO_DTYPE_F16) (static_cast<_Float16*>(t.p) + base)[at[i]] = rounded<_Float16>(p[i]);
+    else (static_cast<__bf16*>(t.p) + base)[at[i]] = rounded<__bf16>(p[i]);
     if (BITS == 32) {
-      static_cast<float*>(t.m)[at[i]] = m[i];
-      static_cast<float*>(t.v)[at[i]] = v[i];
+      m32[at[i]] = m[i];
+      v32[at[i]] = v[i];
     }
   }
   if (BITS == 32) return;
+  const float A = __uint_as_float(wave_max(ma)), Bt = __uint_as_float(wave_max(mb));
+  f4 cm, cv;
+  codes4(am, A, 127.0f, &cm);
+  codes4(wm, Bt, 255.0f, &cv);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t b = base / kBlk + 4 * u + wave;
-    if (b * kBlk >= t.n) break;  // the same for the wave's lanes
-    uint32_t ma = 0, mb = 0;
-    f4 am, wm, cm, cv;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = 4 * u + j;
-      am[j] = __builtin_fabsf(m[i]);
-      wm[j] = w[i];
-      if (in[i]) {
-        ma = max(ma, abs_bits(m[i]));
-        mb = max(mb, abs_bits(w[i]));
-      }
-    }
-    const float A = __uint_as_float(wave_max(ma)), Bt = __uint_as_float(wave_max(mb));
-    codes4(am, A, 127.0f, &cm);
-    codes4(wm, Bt, 255.0f, &cv);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = 4 * u + j;
-      if (!in[i]) continue;
-      static_cast<int8_t*>(t.m)[at[i]] = signed_code(cm[j], m[i]);
-      static_cast<uint8_t*>(t.v)[at[i]] = unsigned_code(cv[j], w[i]);
-    }
-    if (lane == 0) {
-      t.ms[b] = A;
-      t.vs[b] = Bt;
-    }
+  for (int i = 0; i < N; ++i) {
+    if (first + 64 * i >= left) continue;
+    m8[at[i]] = signed_code(cm[i], m[i]);
+    v8[at[i]] = unsigned_code(cv[i], wm[i]);
+  }
+  if (lane == 0) {
+    ms[wave] = A;
+    vs[wave] = Bt;
   }
 }
 
-template <typename P, typename G, bool MASTER>
+template <typename P, typename G, bool MASTER, int U>
 __device__ __forceinline__ void full_of(const AdamTensor& t, int64_t base, const Consts& k) {
-  if (t.bits == 32) full_chunk<P, G, MASTER, 32>(t, base, k);
-  else full_chunk<P, G, MASTER, 8>(t, base, k);
+  if (t.bits == 32) full_chunk<P, G, MASTER, 32, U>(t, base, k);
+  else full_chunk<P, G, MASTER, 8, U>(t, base, k);
 }
 
-template <typename P>
+template <typename P, int U>
 __device__ __forceinline__ void full_half(const AdamTensor& t, int64_t base, const Consts& k) {
   if (t.gdt == FNO_DTYPE_F32) {
-    if (t.master) full_of<P, float, true>(t, base, k);
-    else full_of<P, float, false>(t, base, k);
+    if (t.master) full_of<P, float, true, U>(t, base, k);
+    else full_of<P, float, false, U>(t, base, k);
   } else {
-    if (t.master) full_of<P, P, true>(t, base, k);
-    else full_of<P, P, false>(t, base, k);
+    if (t.master) full_of<P, P, true, U>(t, base, k);
+    else full_of<P, P, false, U>(t, base, k);
   }
 }
 
+// A work-group takes a chunk of U pieces.  Two per work-group stream a large
+// list 3% faster (67 M fp16 weights with masters: step and norm 432 us, 445
+// with one), one keeps small lists' chains of loads short (24 tensors of 262 K
+// elements in all: 10.9 us, 12.3 with two).
+template <int U>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a, AdamHyper h,
                                                     const fno_adamw_control* ctl) {
   if (ctl && ctl->skip) return;
   const int i = find_tensor(a.first, a.count, (int)blockIdx.x);
   const AdamTensor& t = a.t[i];
-  const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * kChunk;
+  const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * (U * kPiece);
   const Consts k = consts_of(h, ctl, t.wd);
-  if (base + kChunk > t.n) {
-    if (t.bits == 32) last_chunk<32>(t, base, k);
-    else last_chunk<8>(t, base, k);
+  if (base + U * kPiece > t.n) {
+#pragma unroll 1
+    for (int64_t b = base; b < base + U * kPiece && b < t.n; b += kPiece)
+      if (t.bits == 32) last_piece<32>(t, b, k);
+      else last_piece<8>(t, b, k);
   } else if (t.pdt == FNO_DTYPE_F32) {
-    full_of<float, float, false>(t, base, k);
+    full_of<float, float, false, U>(t, base, k);
   } else if (t.pdt == FNO_DTYPE_F16) {
-    full_half<_Float16>(t, base, k);
+    full_half<_Float16, U>(t, base, k);
   } else {
-    full_half<__bf16>(t, base, k);
+    full_half<__bf16, U>(t, base, k);
   }
 }
 
@@ -714,11 +714,18 @@ struct StepLaunch {
   hipStream_t s;
 };
 
+template <int U>
+hipError_t launch_step_of(const StepLaunch& L) {
+  return over_batches<AdamArgs>(L.t, L.count, U * kPiece, [&](const AdamArgs& a, int64_t chunks, int64_t) {
+    hipLaunchKernelGGL(adamw_kernel<U>, dim3((unsigned)chunks), dim3(256), 0, L.s, a, L.h, L.ctl);
+  });
+}
+
 hipError_t launch_step(void* ctx) {
   const StepLaunch& L = *static_cast<StepLaunch*>(ctx);
-  return over_batches<AdamArgs>(L.t, L.count, kChunk, [&](const AdamArgs& a, int64_t chunks, int64_t) {
-    hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)chunks), dim3(256), 0, L.s, a, L.h, L.ctl);
-  });
+  int64_t n = 0;
+  for (int64_t i = 0; i < L.count; ++i) n += L.t[i].n;
+  return n < ((int64_t)1 << 22) ? launch_step_of<1>(L) : launch_step_of<2>(L);
 }
 
 struct NormLaunch {
