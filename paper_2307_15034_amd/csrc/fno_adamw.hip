@@ -231,6 +231,16 @@ __device__ __forceinline__ void codes4(const f4& x, float top, float levels, f4*
   }
 }
 
+// Masters, moments and 16-bit parameters of large lists (U 2) are stored past
+// the memory-side cache, so that the step's reads push nothing back to memory
+// (67 M fp16 weights with masters: 436 -> 432 us, with 8-bit states 298 -> 295;
+// fp32 parameters stored so cost 2% of 268 M weights' step).
+template <int U, typename V>
+__device__ __forceinline__ void put_result(V* p, const V& v) {
+  if (U == 1) *p = v;
+  else __builtin_nontemporal_store(v, p);
+}
+
 // A chunk that lies inside its tensor: each thread takes four consecutive
 // elements at a time, so that a wave covers 256, a block of the 8-bit states;
 // all loads of the chunk are in flight before the first element's step.
@@ -282,14 +292,14 @@ __device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, co
       v[u][j] = vj;
       w[j] = wj;
     }
-    if (MASTER) *reinterpret_cast<f4*>(master + 1024 * u) = p;
+    if (MASTER) put_result<U>(reinterpret_cast<f4*>(master + 1024 * u), p);
     PV pr;
 #pragma unroll
     for (int j = 0; j < 4; ++j) pr[j] = rounded<P>(p[j]);
-    *reinterpret_cast<PV*>(pp + 1024 * u) = pr;
+    put_result<sizeof(P) == 2 ? U : 1>(reinterpret_cast<PV*>(pp + 1024 * u), pr);
     if (BITS == 32) {
-      *reinterpret_cast<f4*>(m32 + 1024 * u) = m[u];
-      *reinterpret_cast<f4*>(v32 + 1024 * u) = v[u];
+      put_result<U>(reinterpret_cast<f4*>(m32 + 1024 * u), m[u]);
+      put_result<U>(reinterpret_cast<f4*>(v32 + 1024 * u), v[u]);
     } else {
       f4 am, cm, cv;
       uint32_t ma = 0, mb = 0;
@@ -307,8 +317,8 @@ __device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, co
         qm[u][j] = signed_code(cm[j], m[u][j]);
         qv[u][j] = unsigned_code(cv[j], w[j]);
       }
-      *reinterpret_cast<c4*>(m8 + 1024 * u) = qm[u];
-      *reinterpret_cast<u4*>(v8 + 1024 * u) = qv[u];
+      put_result<U>(reinterpret_cast<c4*>(m8 + 1024 * u), qm[u]);
+      put_result<U>(reinterpret_cast<u4*>(v8 + 1024 * u), qv[u]);
       if ((threadIdx.x & 63) == 0) {
         t.ms[b0 + 4 * u] = A;
         t.vs[b0 + 4 * u] = Bt;

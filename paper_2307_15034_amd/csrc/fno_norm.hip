@@ -78,6 +78,8 @@ __device__ __forceinline__ void my_channels(const NormArgs& a, F f) {
 }
 
 // UNI: a vector's channels are of one group (and C is a multiple of a vector).
+// The second pass also tells whether vectors are aligned, as they then are.
+enum { kAny = 0, kAligned = 1, kUni = 2 };
 template <typename T, bool UNI>
 __device__ __forceinline__ void flat_stats(const NormArgs& a, int64_t unit, Sums* lds) {  // [A][E]
   constexpr int V = kVec<T>, UN = 4, E = UNI ? 1 : V;
@@ -127,8 +129,9 @@ __device__ __forceinline__ void load_groups(const NormArgs& a, int64_t b, V2* ld
   __syncthreads();
 }
 
-template <typename T, int ACT, bool UNI>
+template <typename T, int ACT, int KIND>
 __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* lds) {  // [G]
+  constexpr bool UNI = KIND == kUni;
   constexpr int V = kVec<T>, UN = UNI ? 2 : 1;
   const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
   const bool res = a.res != nullptr;
@@ -164,7 +167,7 @@ __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* 
         Vec<T, V> o;
 #pragma unroll
         for (int j = 0; j < V; ++j) o.e[j] = (T)y[j];
-        store_vec<T, V>(out + my_at(a, k, V), o);
+        store_result<T, V>(out + my_at(a, k, V), o, KIND != kAny);
       });
   if (m.tail) {
     const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
@@ -177,11 +180,11 @@ __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* 
       }
   }
 }
-template <typename T, int ACT, bool UNI>
+template <typename T, int ACT, int KIND>
 __global__ __launch_bounds__(NT, 4) void flat_fwd_kernel(NormArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += gridDim.x) {
-    flat_fwd<T, ACT, UNI>(a, u, reinterpret_cast<Stat*>(smem));
+    flat_fwd<T, ACT, KIND>(a, u, reinterpret_cast<Stat*>(smem));
     __syncthreads();
   }
 }
@@ -255,8 +258,9 @@ __global__ __launch_bounds__(NT, UNI ? 4 : 3) void flat_sums_kernel(NormArgs a) 
   }
 }
 
-template <typename T, int ACT, bool UNI>
+template <typename T, int ACT, int KIND>
 __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means* lds) {  // [G]
+  constexpr bool UNI = KIND == kUni;
   constexpr int V = kVec<T>, UN = UNI ? 2 : 1;
   const int64_t b = unit / a.n1, chunk = unit - b * a.n1;
   const Mine m = my_vectors(a, chunk, a.v1, V);
@@ -287,7 +291,7 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means*
           bwd_terms<ACT>(k[j], p.x.e[j], p.y.e[j], &h, &d);
           o.e[j] = (T)bwd_gx(k[j], gk[j], h, d);
         }
-        store_vec<T, V>(out + my_at(a, i, V), o);
+        store_result<T, V>(out + my_at(a, i, V), o, KIND != kAny);
       });
   if (m.tail) {
     const int64_t at = ((int)threadIdx.x + m.count * a.A) * V;
@@ -301,12 +305,12 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means*
   }
 }
 
-template <typename T, int ACT, bool UNI>
-__global__ __launch_bounds__(NT, UNI ? 4 : 3) void flat_bwd_kernel(NormArgs a) {
+template <typename T, int ACT, int KIND>
+__global__ __launch_bounds__(NT, KIND == kUni ? 4 : 3) void flat_bwd_kernel(NormArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   if ((int)blockIdx.x >= a.main) return param_grads(a, (int)blockIdx.x - a.main);
   for (int64_t u = a.u0 + blockIdx.x; u < a.u1; u += a.main) {
-    flat_bwd<T, ACT, UNI>(a, u, reinterpret_cast<Means*>(smem));
+    flat_bwd<T, ACT, KIND>(a, u, reinterpret_cast<Means*>(smem));
     __syncthreads();
   }
 }
@@ -402,7 +406,7 @@ __global__ __launch_bounds__(NT) void wide_fwd_kernel(NormArgs a) {
                         if (a.res) y += (float)r.e[j];
                         o.e[j] = (T)y;
                       }
-                      store_vec<T, W>(out + i * a.C, o);
+                      store_result<T, W>(out + i * a.C, o, a.nt);
                     });
   }
 }
@@ -465,7 +469,7 @@ __global__ __launch_bounds__(NT) void wide_bwd_kernel(NormArgs a) {
                                         act_grad_any(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
                         o.e[j] = (T)bwd_gx(k[j], gk[j], h, d);
                       }
-                      store_vec<T, W>(out + i * a.C, o);
+                      store_result<T, W>(out + i * a.C, o, a.nt);
                     });
   }
 }
@@ -571,7 +575,7 @@ __global__ __launch_bounds__(NT) void first_fwd_kernel(NormArgs a) {
           Vec<T, V> o;
 #pragma unroll
           for (int j = 0; j < V; ++j) o.e[j] = (T)y[j];
-          store_vec<T, V>(out + e, o);
+          store_result<T, V>(out + e, o, a.nt);
         },
         [&](int e) {
           float y = act_f<ACT>(on_line(l, x[e]));
@@ -636,7 +640,7 @@ __global__ __launch_bounds__(NT) void first_bwd_kernel(NormArgs a) {
           Vec<T, V> o;
 #pragma unroll
           for (int j = 0; j < V; ++j) o.e[j] = (T)one(xv.e[j], gv.e[j]);
-          store_vec<T, V>(out + e, o);
+          store_result<T, V>(out + e, o, a.nt);
         },
         [&](int e) { out[e] = (T)one(x[e], g[e]); });
   }
@@ -667,6 +671,7 @@ fno_status check_desc(const fno_norm_desc* d) {
 
 enum Route { FLAT, WIDE, FIRST, RESIDENT };
 constexpr int kFill = 1024;        // work-groups that fill the chip (four per compute unit)
+constexpr int kFillFew = 768;      // three: the backward where groups cross vectors, by its registers
 constexpr int kMaxGrid = 1 << 20;  // work-groups of a launch; more work is looped over
 
 struct NormPlan {
@@ -679,7 +684,7 @@ struct NormPlan {
   bool first;     // channels first
 };
 
-NormPlan plan_of(const fno_norm_desc& d) {
+NormPlan plan_of(const fno_norm_desc& d, bool bwd) {
   NormPlan p{};
   NormArgs& a = p.a;
   const int V = d.dtype == FNO_DTYPE_F32 ? 4 : 8;
@@ -693,6 +698,7 @@ NormPlan plan_of(const fno_norm_desc& d) {
   a.eps = d.eps;
   p.vec = V;
   p.first = d.layout == FNO_LAYOUT_CHANNELS_FIRST;
+  a.nt = (p.first ? a.P : a.R) % V == 0;
   if (norm_resident_fits(a, d.dtype, p.first)) {
     p.route = RESIDENT;
     a.nc = 1;
@@ -731,7 +737,8 @@ NormPlan plan_of(const fno_norm_desc& d) {
     a.A = (int)(NT / L * L);
     p.uni = a.C % V == 0 && a.Cg % V == 0;
     const int64_t nv = cdiv(a.R, V), per = (int64_t)a.A * (V == 4 ? 8 : 16);
-    const int64_t want = std::clamp<int64_t>(a.B * nv / per, kFill, 4 * kFill) / a.B;
+    const int fill = bwd && !p.uni ? kFillFew : kFill;
+    const int64_t want = std::clamp<int64_t>(a.B * nv / per, fill, 4 * fill) / a.B;
     const int64_t room = std::max<int64_t>(1, nv / ((int64_t)a.A * 4));
     const int64_t n = std::max(std::clamp<int64_t>(want, 1, room), cdiv(nv, (int64_t)1 << 26));
     a.v1 = rup(cdiv(nv, n), a.A);
@@ -743,6 +750,7 @@ NormPlan plan_of(const fno_norm_desc& d) {
   }
   p.route = WIDE;
   p.vec = a.C % V == 0 ? V : 1;
+  a.nt = p.vec == V;
   a.cols = (int)cdiv(a.C, (int64_t)NT * p.vec);
   const int64_t want = std::max<int64_t>(1, kFill / (a.B * a.cols));
   a.rows = cdiv(a.P, std::min(want, std::max<int64_t>(1, a.P / 8)));
@@ -804,7 +812,7 @@ void launch_fwd2(NormLaunch& L) {
   NormArgs& a = L.p.a;
   const int64_t units = a.u1 - a.u0;
   if (L.p.route == FLAT) {
-    auto k = L.p.uni ? flat_fwd_kernel<T, ACT, true> : flat_fwd_kernel<T, ACT, false>;
+    auto k = L.p.uni ? flat_fwd_kernel<T, ACT, kUni> : a.nt ? flat_fwd_kernel<T, ACT, kAligned> : flat_fwd_kernel<T, ACT, kAny>;
     hipLaunchKernelGGL(k, dim3(grid_of(units)), dim3(NT), a.G * sizeof(Stat), L.s, a);
   } else if (L.p.route == WIDE) {
     auto k = L.p.vec == 1 ? wide_fwd_kernel<T, 1> : wide_fwd_kernel<T, kVec<T>>;
@@ -839,7 +847,7 @@ void launch_bwd2(NormLaunch& L, int extra) {
   const int64_t units = a.u1 - a.u0;
   if (L.p.route == FLAT) {
     a.main = (int)grid_of(units);
-    auto k = L.p.uni ? flat_bwd_kernel<T, ACT, true> : flat_bwd_kernel<T, ACT, false>;
+    auto k = L.p.uni ? flat_bwd_kernel<T, ACT, kUni> : a.nt ? flat_bwd_kernel<T, ACT, kAligned> : flat_bwd_kernel<T, ACT, kAny>;
     hipLaunchKernelGGL(k, dim3(a.main + extra), dim3(NT), a.G * sizeof(Stat), L.s, a);
   } else if (L.p.route == WIDE) {
     a.main = (int)grid_of(units);
@@ -900,7 +908,7 @@ extern "C" fno_status fno_group_norm_act_workspace_size(const fno_norm_desc* d, 
   const fno_status st = check_desc(d);
   if (st != FNO_OK) return st;
   if (!bytes || (op != FNO_OP_FWD && op != FNO_OP_BWD)) return FNO_ERR_INVALID_ARGUMENT;
-  *bytes = (size_t)ws_of(plan_of(*d), op == FNO_OP_BWD).bytes;
+  *bytes = (size_t)ws_of(plan_of(*d, op == FNO_OP_BWD), op == FNO_OP_BWD).bytes;
   return FNO_OK;
 }
 
@@ -913,7 +921,7 @@ extern "C" fno_status fno_group_norm_act_fwd(const fno_norm_desc* d, const void*
   if (!ok16(x) || !ok16(out) || !null_or16(gamma) || !null_or16(beta) || !null_or16(residual) ||
       !null_or16(stats))
     return FNO_ERR_INVALID_ARGUMENT;
-  NormLaunch L{plan_of(*d), d->dtype, stream};
+  NormLaunch L{plan_of(*d, false), d->dtype, stream};
   const WsLayout w = ws_of(L.p, false);
   if (ws_len < (size_t)w.bytes) return FNO_ERR_WORKSPACE_TOO_SMALL;
   if (!ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
@@ -939,7 +947,7 @@ extern "C" fno_status fno_group_norm_act_bwd(const fno_norm_desc* d, const void*
   if (!ok16(x) || !ok16(g_out) || !ok16(gx) || !ok16(stats) || !null_or16(gamma) ||
       !null_or16(beta) || !null_or16(g_gamma) || !null_or16(g_beta))
     return FNO_ERR_INVALID_ARGUMENT;
-  NormLaunch L{plan_of(*d), d->dtype, stream};
+  NormLaunch L{plan_of(*d, true), d->dtype, stream};
   const WsLayout w = ws_of(L.p, true);
   if (ws_len < (size_t)w.bytes) return FNO_ERR_WORKSPACE_TOO_SMALL;
   if (!ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
