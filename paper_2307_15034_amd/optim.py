@@ -6,12 +6,16 @@ PyTorch supplies memory and streams only; every step runs in the HIP kernels.
 from __future__ import annotations
 
 import ctypes
+from array import array
+from operator import attrgetter
 from typing import Dict, List, Optional, Sequence, Union
 
 import torch
 
 from . import binding as B
 from .layer import DTYPE_CODES, _addr, _stream_of
+
+_dtype_of = attrgetter("dtype")
 
 
 class AdamW:
@@ -85,6 +89,11 @@ class AdamW:
             if len(set(own)) != len(own) or seen & set(own):
                 raise ValueError(f"params[{i}]: a parameter, master or state is used twice")
             seen |= set(own)
+        # the tensors with 8-bit states, as `moments` reads them
+        self._eight = [i for i, b in enumerate(self.state_bits) if b == 8]
+        self._eight_sizes = [self.params[i].numel() for i in self._eight]
+        self._eight_list = (B.FnoAdamwTensor * max(1, len(self._eight)))(
+            *[self._list[i] for i in self._eight])
         self.set_grads(grads)
         self.control: Optional[torch.Tensor] = None
         if device_control:
@@ -201,6 +210,16 @@ class AdamW:
         c = B.FnoAdamwControl.from_buffer_copy(bytes(self.control.cpu().numpy()))
         return {k: getattr(c, k) for k, _ in c._fields_ if k not in ("arrived", "reserved")}
 
+    def _all_fit(self, tensors, dtype) -> bool:
+        """_addr's checks for the read-out's tensors, a check at a time over all
+        of them: with a hundred small tensors the call is as long as its checks."""
+        T = torch.Tensor
+        return (all(issubclass(c, T) for c in set(map(type, tensors))) and
+                list(map(T.numel, tensors)) == self._eight_sizes and
+                set(map(_dtype_of, tensors)) == {dtype} and
+                all(map(T.is_contiguous, tensors)) and
+                set(map(T.get_device, tensors)) == {self.device.index})
+
     def moments(self, exp_avg: Optional[Sequence[torch.Tensor]] = None,
                 exp_avg_sq: Optional[Sequence[torch.Tensor]] = None,
                 dtype: torch.dtype = torch.float32, stream: Optional[int] = None):
@@ -208,9 +227,9 @@ class AdamW:
         ones read out into tensors of the parameter's element count, made here
         in `dtype` or the caller's (then a full list of one type each; entries
         of 32-bit states stay as they are)."""
-        eight = [i for i, b in enumerate(self.state_bits) if b == 8]
+        eight = self._eight
         s = _stream_of(self.device, stream)
-        outs = []
+        outs, ptrs = [], []
         for k, given in (("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq)):
             if given is None:
                 if stream is not None:
@@ -218,22 +237,24 @@ class AdamW:
                 given = [torch.empty(self.params[i].numel(), dtype=dtype, device=self.device)
                          if b == 8 else self.states[i][k] for i, b in enumerate(self.state_bits)]
             given = self._per_tensor(given, k)
-            if eight:
-                dtype = given[eight[0]].dtype
-                if dtype not in DTYPE_CODES:
-                    raise ValueError(f"{k}: dtype {dtype}")
             outs.append(given)
+            if not eight:
+                continue
+            if not ptrs:
+                _addr(given[eight[0]], None, None, f"{k}[{eight[0]}]", self.device)
+                dtype = getattr(given[eight[0]], "dtype", None)
+                if dtype not in DTYPE_CODES:
+                    raise ValueError(f"{k}: dtype {dtype}, expected float32, float16 or bfloat16")
+            sub = [given[i] for i in eight]
+            if not self._all_fit(sub, dtype):
+                for i, n, t in zip(eight, self._eight_sizes, sub):
+                    _addr(t, None, dtype, f"{k}[{i}]", self.device)
+                    if t is None or t.numel() != n:
+                        raise ValueError(f"{k}[{i}]: a tensor of {n} elements is required")
+            addr = map(torch.Tensor.data_ptr, sub)
+            addr = array("Q", addr)      # a third of the time of a ctypes array's making
+            ptrs.append((ctypes.c_void_p * len(sub)).from_buffer(addr))
         if not eight:
             return outs[0], outs[1]
-        sub = (B.FnoAdamwTensor * len(eight))(*[self._list[i] for i in eight])
-        ptrs = []
-        for k, out in zip(("exp_avg", "exp_avg_sq"), outs):
-            a = (ctypes.c_void_p * len(eight))()
-            for j, i in enumerate(eight):
-                if out[i].numel() != self.params[i].numel():
-                    raise ValueError(f"{k}[{i}]: {out[i].numel()} elements, expected "
-                                     f"{self.params[i].numel()}")
-                a[j] = _addr(out[i], None, dtype, f"{k}[{i}]", self.device) or None
-            ptrs.append(a)
-        B.fno_adamw_moments(sub, len(eight), DTYPE_CODES[dtype], ptrs[0], ptrs[1], s)
+        B.fno_adamw_moments(self._eight_list, len(eight), DTYPE_CODES[dtype], ptrs[0], ptrs[1], s)
         return outs[0], outs[1]
