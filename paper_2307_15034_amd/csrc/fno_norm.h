@@ -34,6 +34,16 @@ __device__ __forceinline__ Vec<T, W> load_vec(const T* p) {
   __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), sizeof(v));
   return v;
 }
+// The same where the call reads them for the last time: past the memory-side
+// cache, which keeps what is still to be read.
+template <typename T, int W>
+__device__ __forceinline__ Vec<T, W> load_last(const T* p) {
+  if constexpr (sizeof(Vec<T, W>) == 16) {
+    typedef uint32_t U4 __attribute__((ext_vector_type(4), aligned(2)));
+    return __builtin_bit_cast(Vec<T, W>, __builtin_nontemporal_load(reinterpret_cast<const U4*>(p)));
+  }
+  return load_vec<T, W>(p);
+}
 template <typename T, int W>
 __device__ __forceinline__ void store_vec(T* p, const Vec<T, W>& v) {
   __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T)), &v, sizeof(v));
