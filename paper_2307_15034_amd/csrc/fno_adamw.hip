@@ -231,14 +231,22 @@ __device__ __forceinline__ void codes4(const f4& x, float top, float levels, f4*
   }
 }
 
-// Masters, moments and 16-bit parameters of large lists (U 2) are stored past
-// the memory-side cache, so that the step's reads push nothing back to memory
-// (67 M fp16 weights with masters: 436 -> 432 us, with 8-bit states 298 -> 295;
-// fp32 parameters stored so cost 2% of 268 M weights' step).
+// Large lists (U 2) go past the memory-side cache both ways: each operand is
+// read and written once, and through the cache the written lines would be
+// pushed out by later reads (67 M fp16 weights with masters, clipped: 436 us
+// through it, 430 with the results stored past it, 348 with the loads as well;
+// 268 M fp32 weights with 8-bit states, step and read-out: 1093, 1107 and,
+// with the parameters stored past it too, 1075).  Small lists stay in it from
+// one step to the next.
 template <int U, typename V>
 __device__ __forceinline__ void put_result(V* p, const V& v) {
   if (U == 1) *p = v;
   else __builtin_nontemporal_store(v, p);
+}
+template <int U, typename V>
+__device__ __forceinline__ V get_once(const V* p) {
+  if (U == 1) return *p;
+  return __builtin_nontemporal_load(p);
 }
 
 // A chunk that lies inside its tensor: each thread takes four consecutive
@@ -264,15 +272,15 @@ __device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, co
   float as[U], bs[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (MASTER) pm[u] = *reinterpret_cast<const f4*>(master + 1024 * u);
-    else pl[u] = *reinterpret_cast<const PV*>(pp + 1024 * u);
-    g[u] = *reinterpret_cast<const GV*>(gp + 1024 * u);
+    if (MASTER) pm[u] = get_once<U>(reinterpret_cast<const f4*>(master + 1024 * u));
+    else pl[u] = get_once<U>(reinterpret_cast<const PV*>(pp + 1024 * u));
+    g[u] = get_once<U>(reinterpret_cast<const GV*>(gp + 1024 * u));
     if (BITS == 32) {
-      m[u] = *reinterpret_cast<const f4*>(m32 + 1024 * u);
-      v[u] = *reinterpret_cast<const f4*>(v32 + 1024 * u);
+      m[u] = get_once<U>(reinterpret_cast<const f4*>(m32 + 1024 * u));
+      v[u] = get_once<U>(reinterpret_cast<const f4*>(v32 + 1024 * u));
     } else {
-      qm[u] = *reinterpret_cast<const c4*>(m8 + 1024 * u);
-      qv[u] = *reinterpret_cast<const u4*>(v8 + 1024 * u);
+      qm[u] = get_once<U>(reinterpret_cast<const c4*>(m8 + 1024 * u));
+      qv[u] = get_once<U>(reinterpret_cast<const u4*>(v8 + 1024 * u));
       as[u] = t.ms[b0 + 4 * u];
       bs[u] = t.vs[b0 + 4 * u];
     }
@@ -296,7 +304,7 @@ __device__ __forceinline__ void full_chunk(const AdamTensor& t, int64_t base, co
     PV pr;
 #pragma unroll
     for (int j = 0; j < 4; ++j) pr[j] = rounded<P>(p[j]);
-    put_result<sizeof(P) == 2 ? U : 1>(reinterpret_cast<PV*>(pp + 1024 * u), pr);
+    put_result<U>(reinterpret_cast<PV*>(pp + 1024 * u), pr);
     if (BITS == 32) {
       put_result<U>(reinterpret_cast<f4*>(m32 + 1024 * u), m[u]);
       put_result<U>(reinterpret_cast<f4*>(v32 + 1024 * u), v[u]);
@@ -423,16 +431,18 @@ __device__ __forceinline__ void full_half(const AdamTensor& t, int64_t base, con
 }
 
 // A work-group takes a chunk of U pieces.  Two per work-group stream a large
-// list 3% faster (67 M fp16 weights with masters: step and norm 432 us, 445
-// with one), one keeps small lists' chains of loads short (24 tensors of 262 K
-// elements in all: 10.9 us, 12.3 with two).
+// list faster (67 M fp16 weights with masters, clipped: 3%), one keeps small
+// lists' chains of loads short (24 tensors of 262 K elements in all: 10.9 us,
+// 12.3 with two).
 template <int U>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a, AdamHyper h,
                                                     const fno_adamw_control* ctl) {
   if (ctl && ctl->skip) return;
-  const int i = find_tensor(a.first, a.count, (int)blockIdx.x);
+  // From the last chunk on: the gradient norm has just read the last gradients.
+  const int blk = (int)gridDim.x - 1 - (int)blockIdx.x;
+  const int i = find_tensor(a.first, a.count, blk);
   const AdamTensor& t = a.t[i];
-  const int64_t base = (int64_t)((int)blockIdx.x - a.first[i]) * (U * kPiece);
+  const int64_t base = (int64_t)(blk - a.first[i]) * (U * kPiece);
   const Consts k = consts_of(h, ctl, t.wd);
   if (base + U * kPiece > t.n) {
 #pragma unroll 1
@@ -492,8 +502,9 @@ __device__ __forceinline__ void moments_chunk(const AdamTensor& t, int64_t base,
       m[j] = rounded<T>(decode_m(a[u], qm[u][j]));
       v[j] = rounded<T>(decode_v(b[u], qv[u][j]));
     }
-    *reinterpret_cast<V*>(mo + e0 + 2048 * u) = m;
-    *reinterpret_cast<V*>(vo + e0 + 2048 * u) = v;
+    // past the memory-side cache: 268 M weights 1059 us with the step, 1073 through it
+    __builtin_nontemporal_store(m, reinterpret_cast<V*>(mo + e0 + 2048 * u));
+    __builtin_nontemporal_store(v, reinterpret_cast<V*>(vo + e0 + 2048 * u));
   }
 }
 
