@@ -12,8 +12,8 @@
 // joins its group's and streams the tensors again.  The second pass takes the
 // work items in the opposite order, so that what the first read last is still
 // in the memory-side cache, and reads past that cache what is not needed again
-// (8 x 64 planes of 1024^2, fp16 with a residual: 809 us, 787 in the opposite
-// order, 756 with both).
+// (8 x 64 planes of 1024^2, fp16 with a residual: 787 us for 807 in the
+// opposite order, 756 with both).
 //
 // Every thread keeps to the same channels from its first vector to its last,
 // with their coefficients and sums in registers:
@@ -24,6 +24,12 @@
 //   channels last, "wide" (L beyond a work-group):  a thread takes one vector
 //     of channels (one channel where C is no multiple of a vector) down the rows;
 //   channels first:  a team of threads takes one plane or a segment of it.
+//
+// Bound by memory: 8 x 64 x 1024^2, fp16: sums 167 us (6.4 TB/s), results with a
+// residual 548 (6.1); the backward of 16 x 128 x 256^2, bf16: 102 and 138 (5.3
+// and 6.1).  Channels last 32 x 128^2 x 64, fp16: forward 13.6 + 27 us (5.0
+// TB/s), backward 34 + 36 (4.2 and 5.9), its sums as much by their arithmetic
+// (29% of a wave's time in vector operations, four waves to a unit).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -683,7 +689,8 @@ fno_status check_desc(const fno_norm_desc* d) {
 
 enum Route { FLAT, WIDE, FIRST, RESIDENT };
 constexpr int kFill = 1024;        // work-groups that fill the chip (four per compute unit)
-constexpr int kFillFew = 768;      // three: the backward where groups cross vectors, by its registers
+constexpr int kFillFew = 768;      // three: the backward where groups cross vectors, by its
+                                   // registers (16 x 241^2 x 20: 44.5 us, 50.7 with 1024)
 constexpr int kMaxGrid = 1 << 20;  // work-groups of a launch; more work is looped over
 
 struct NormPlan {
@@ -718,16 +725,16 @@ NormPlan plan_of(const fno_norm_desc& d, bool bwd) {
   }
   if (p.first) {
     // A wave per plane up to 16 vectors a lane, else work-groups on segments
-    // of at least eight vectors a thread, up to eight times what fills the
-    // chip: the memory keeps busiest while work-groups start and end at
-    // different times (backward of 16 x 128 planes of 256^2, bf16: 277 us with
-    // 2048 segments, 264 with 4096, 251 with 8192).
+    // of eight vectors a thread (no more than 8192 to a group, whose sums have
+    // to be joined): forward of 8 x 64 planes of 1024^2, fp16 with a residual,
+    // 703 us; 747 with sixteen vectors, 774 with six, 888 with four; backward of
+    // 16 x 128 planes of 256^2, bf16, 225, 232, 232 and 248.
     p.route = FIRST;
     p.team = a.P <= 64 * V * 16 ? 64 : NT;
     a.n1 = 1;
     if (p.team == NT)
       a.n1 = (int)std::max<int64_t>(
-          {1, std::min(cdiv(8 * kFill, a.B * a.C), a.P / (NT * V * 8)), cdiv(a.P, (int64_t)1 << 30)});
+          {1, std::min<int64_t>(8192 / a.Cg, a.P / (NT * V * 8)), cdiv(a.P, (int64_t)1 << 30)});
     a.rows = rup(cdiv(a.P, a.n1), (int64_t)NT * V);
     a.n1 = (int)cdiv(a.P, a.rows);
     a.n = a.Cg * a.n1;
@@ -742,8 +749,9 @@ NormPlan plan_of(const fno_norm_desc& d, bool bwd) {
     // operations: 8), between one and four times the work-groups that fill
     // the chip, but at least four vectors a thread.  A work-group's start and
     // end (its channels' coefficients, its sums joined) cost as much as five
-    // vectors (33.5 M fp16 elements: forward 44 us with 1024 work-groups, 48
-    // with 2048, 62 with 4096; as many fp32: 83, 81 and 76).
+    // vectors (33.5 M fp16 elements: forward 37.7 us with 1024 work-groups, 42.9
+    // with 2048, 57 with 4096, backward 67.4, 72.7 and 91; as many fp32: 68.5,
+    // 69 and 66).
     p.route = FLAT;
     a.L = (int)L;
     a.A = (int)(NT / L * L);

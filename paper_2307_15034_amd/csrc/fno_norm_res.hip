@@ -10,6 +10,10 @@
 //                  teams in turn, where there are more planes than waves);
 // channels last:   a thread keeps to one piece of W channels of the group's
 //                  part of a row and takes it from every so many-th row.
+//
+// Bound by latency at the sizes that fit (2 x 64^2 x 16, fp16, four groups:
+// 7.9 us on the device, eight work-groups in one chain of load, sum, result;
+// a call 15.4 us through the two passes, 12.3 so, 10.2 since calls are leaner).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
