@@ -329,14 +329,28 @@ __global__ __launch_bounds__(NT, KIND == kUni ? 4 : 3) void flat_bwd_kernel(Norm
   }
 }
 
-// Each group's entries joined: one wave per group.
+// Each group's entries joined by TEAM threads: a wave where a group has up to
+// 256, else a work-group; four loads of a thread in flight (8192 entries of one group,
+// 8 planes of 2^24: forward 136 us, 167 with a wave and one load).
+template <int TEAM>
 __global__ __launch_bounds__(NT) void join_kernel(NormArgs a) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t g = a.u0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); g < a.u1; g += (int64_t)gridDim.x * 4) {
-    Sums v{0.0, 0.0};
-    for (int i = lane; i < a.n; i += 64) v = add(v, a.part[g * a.n + i]);
-    v = team_sum<64>(v);
-    if (lane == 0) a.joined[g] = v;
+  const int lane = threadIdx.x & (TEAM - 1);
+  for (int64_t g0 = (int64_t)blockIdx.x * (NT / TEAM); g0 < a.u1; g0 += (int64_t)gridDim.x * (NT / TEAM)) {
+    const int64_t g = g0 + (int)threadIdx.x / TEAM;
+    Sums v[4] = {};
+    if (g < a.u1) {
+      const Sums* p = a.part + g * a.n;
+      for (int i = lane; i < a.n; i += 4 * TEAM) {
+        Sums t[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = p[i + k * TEAM < a.n ? i + k * TEAM : i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i + k * TEAM < a.n) v[k] = add(v[k], t[k]);
+      }
+    }
+    const Sums t = team_sum<TEAM>(add(add(v[0], v[1]), add(v[2], v[3])));
+    if (g < a.u1 && lane == 0) a.joined[g] = t;
   }
 }
 
@@ -725,16 +739,20 @@ NormPlan plan_of(const fno_norm_desc& d, bool bwd) {
   }
   if (p.first) {
     // A wave per plane up to 16 vectors a lane, else work-groups on segments
-    // of eight vectors a thread (no more than 8192 to a group, whose sums have
-    // to be joined): forward of 8 x 64 planes of 1024^2, fp16 with a residual,
-    // 703 us; 747 with sixteen vectors, 774 with six, 888 with four; backward of
-    // 16 x 128 planes of 256^2, bf16, 225, 232, 232 and 248.
+    // of eight vectors a thread: forward of 8 x 64 planes of 1024^2 in eight
+    // groups, fp16 with a residual, 703 us; 747 with sixteen vectors, 774 with
+    // six, 888 with four; backward of 16 x 128 planes of 256^2, bf16, 225, 232,
+    // 232 and 248.  Longer ones where a group would have more than the 1024
+    // entries that the second pass joins itself, unless work-groups are few
+    // (the same planes in one group: 603 us with sixteen segments a plane, 635
+    // with 64 and a launch that joins them).
     p.route = FIRST;
     p.team = a.P <= 64 * V * 16 ? 64 : NT;
     a.n1 = 1;
     if (p.team == NT)
       a.n1 = (int)std::max<int64_t>(
-          {1, std::min<int64_t>(8192 / a.Cg, a.P / (NT * V * 8)), cdiv(a.P, (int64_t)1 << 30)});
+          {1, std::min(std::max<int64_t>(1024 / a.Cg, cdiv(8 * kFill, a.B * a.C)), a.P / (NT * V * 8)),
+           cdiv(a.P, (int64_t)1 << 30)});
     a.rows = rup(cdiv(a.P, a.n1), (int64_t)NT * V);
     a.n1 = (int)cdiv(a.P, a.rows);
     a.n = a.Cg * a.n1;
@@ -807,7 +825,8 @@ void launch_join(NormLaunch& L) {
   NormArgs& a = L.p.a;
   if (!a.collapse) return;
   a.u1 = a.B * a.G;
-  hipLaunchKernelGGL(join_kernel, dim3(grid_of(cdiv(a.u1, 4))), dim3(NT), 0, L.s, a);
+  if (a.n <= 256) hipLaunchKernelGGL(join_kernel<64>, dim3(grid_of(cdiv(a.u1, 4))), dim3(NT), 0, L.s, a);
+  else hipLaunchKernelGGL(join_kernel<NT>, dim3(grid_of(a.u1)), dim3(NT), 0, L.s, a);
 }
 
 template <typename T>

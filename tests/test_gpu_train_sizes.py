@@ -57,6 +57,14 @@ def test_norm_sizes(case):
     _check((points,), b, c, g, dt, act, last, residual=case % 2 == 1, seed=200 + case)
 
 
+@pytest.mark.parametrize("points, channels, dt", [(300001, 48, "fp16"), (5000001, 4, "fp16"),
+                                                  (2500001, 4, "fp32")])
+def test_norm_of_many_segments(points, channels, dt):
+    """Channels first, one group: up to the segments that the second pass joins
+    itself, and more."""
+    _check((points,), 1, channels, 1, dt, "gelu", False, residual=True, seed=300)
+
+
 def _norm_of(grads):
     return np.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
 
