@@ -349,9 +349,9 @@ __device__ __forceinline__ void param_grads(const NormArgs& a, int c) {
 }
 
 // Group norm with each group held by one work-group (fno_norm_res.hip).  fits:
-// whether the kernels take this shape; launch: the whole call (forward with
-// bwd false), `dtype` the tensors' fno_dtype.
-bool norm_resident_fits(const NormArgs& a, int dtype, bool first);
+// whether the kernels take this shape in this direction; launch: the whole call
+// (forward with bwd false), `dtype` the tensors' fno_dtype.
+bool norm_resident_fits(const NormArgs& a, int dtype, bool first, bool bwd);
 hipError_t norm_resident_launch(const NormArgs& a, int dtype, bool first, bool bwd, hipStream_t s);
 
 }  // namespace fno

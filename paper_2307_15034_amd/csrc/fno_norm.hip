@@ -732,7 +732,7 @@ NormPlan plan_of(const fno_norm_desc& d, bool bwd) {
   p.vec = V;
   p.first = d.layout == FNO_LAYOUT_CHANNELS_FIRST;
   a.nt = (p.first ? a.P : a.R) % V == 0;
-  if (norm_resident_fits(a, d.dtype, p.first)) {
+  if (norm_resident_fits(a, d.dtype, p.first, bwd)) {
     p.route = RESIDENT;
     a.nc = 1;
     return p;

@@ -398,9 +398,17 @@ int piece_of(const NormArgs& a, int dtype) {
   const int V = vec_of(dtype);
   return a.Cg % V == 0 ? V : V == 8 && a.Cg % 4 == 0 ? 4 : 1;
 }
-bool last_fits(const NormArgs& a, int W, int threads) {
+// The backward's LDS of a call: sums by thread and by channel.
+size_t last_bwd_lds(const NormArgs& a, int W, int threads) {
+  return (size_t)threads * W * sizeof(float2) + (size_t)a.Cg * sizeof(Sums);
+}
+// Beside it the waves' sums of the two joins; 160 KiB in all (which one or two
+// rows of 6120 channels to a group pass, with pieces of eight).
+constexpr size_t kLdsMax = 160 * 1024;
+bool last_fits(const NormArgs& a, int W, int threads, bool bwd) {
   const int S = a.Cg / W;
-  return S <= threads && a.P <= (int64_t)(threads / S) * (each_of(threads, W) / W);
+  if (S > threads || a.P > (int64_t)(threads / S) * (each_of(threads, W) / W)) return false;
+  return !bwd || last_bwd_lds(a, W, threads) + 2 * (threads / 64) * sizeof(Sums) <= kLdsMax;
 }
 
 template <typename T, int ACT, int THREADS>
@@ -414,7 +422,7 @@ hipError_t launch_last(const NormArgs& a, bool bwd, unsigned grid, hipStream_t s
     hipLaunchKernelGGL((res_last_fwd_kernel<T, W, ACT, THREADS>), dim3(grid), dim3(THREADS), 0, s, a);
     return hipSuccess;
   }
-  const size_t lds = (size_t)THREADS * W * sizeof(float2) + a.Cg * sizeof(Sums);
+  const size_t lds = last_bwd_lds(a, W, THREADS);
   auto k = res_last_bwd_kernel<T, W, ACT, THREADS>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k),
@@ -434,7 +442,7 @@ hipError_t launch_act(const NormArgs& a, int dtype, bool first, bool bwd, unsign
     return hipSuccess;
   }
   const int W = piece_of(a, dtype);
-  const bool small = last_fits(a, W, kSmall);
+  const bool small = last_fits(a, W, kSmall, bwd);
   if (W == V)
     return small ? launch_last<T, V, ACT, kSmall>(a, bwd, grid, s) : launch_last<T, V, ACT, kLarge>(a, bwd, grid, s);
   if (V == 8 && W == 4)
@@ -453,9 +461,9 @@ hipError_t launch_type(const NormArgs& a, int dtype, bool first, bool bwd, unsig
 
 }  // namespace
 
-bool norm_resident_fits(const NormArgs& a, int dtype, bool first) {
+bool norm_resident_fits(const NormArgs& a, int dtype, bool first, bool bwd) {
   if (first) return first_fits(a, vec_of(dtype), kLarge);
-  return last_fits(a, piece_of(a, dtype), kLarge);
+  return last_fits(a, piece_of(a, dtype), kLarge, bwd);
 }
 
 hipError_t norm_resident_launch(const NormArgs& a0, int dtype, bool first, bool bwd, hipStream_t s) {
