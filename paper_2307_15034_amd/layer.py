@@ -327,6 +327,10 @@ def _stream_of(device: torch.device, stream: Optional[int]) -> int:
     return torch.cuda.current_stream(current).cuda_stream if stream is None else stream
 
 
+def _external(device: torch.device, stream: int) -> torch.cuda.Stream:
+    return torch.cuda.ExternalStream(stream, device=device)
+
+
 class GroupNormAct:
     """Group norm with an activation (the fno_group_norm_act_* calls):
     out = act(gamma (x - mean) / sqrt(var + eps) + beta) (+ residual).
@@ -337,10 +341,10 @@ class GroupNormAct:
     (gamma None: ones, beta None: zeros); stats [batch, groups, 2] float32,
     (mean, 1 / sqrt(var + eps)), from the forward to the backward.
 
-    An object keeps one workspace, so its calls belong on one stream (or on
-    streams that wait for each other).  Where `stream` is given, outputs are
-    the caller's too: memory that torch hands out belongs to its current
-    stream.
+    An object keeps one workspace, memory of the first call's stream, so its
+    calls belong on one stream (or on streams that wait for each other).  Where
+    `stream` is given, outputs are the caller's too: memory that torch hands
+    out belongs to its current stream.
     """
 
     def __init__(self, grid: Sequence[int], batch: int, channels: int, groups: int,
@@ -365,10 +369,19 @@ class GroupNormAct:
         self.ws_bytes = {op: B.fno_group_norm_act_workspace_size(self.desc, op)
                          for op in (B.FNO_OP_FWD, B.FNO_OP_BWD)}
         self._ws: Optional[torch.Tensor] = None
+        self._ws_stream = 0
 
-    def _workspace(self, device):
+    def _workspace(self, device, s):
+        """(address, bytes) for a call on stream `s`: taken from that stream's
+        memory at the first call, and kept from others until the work of every
+        stream that used it is done."""
         if self._ws is None or self._ws.device != device:
-            self._ws = torch.empty(max(self.ws_bytes.values()), dtype=torch.uint8, device=device)
+            with torch.cuda.stream(_external(device, s)):
+                self._ws = torch.empty(max(self.ws_bytes.values()), dtype=torch.uint8,
+                                       device=device)
+            self._ws_stream = s
+        elif s != self._ws_stream:
+            self._ws.record_stream(_external(device, s))
         return self._ws.data_ptr(), self._ws.numel()
 
     def _t(self, t, name, device):
@@ -408,7 +421,7 @@ class GroupNormAct:
             self._given(stream, "stats")
             stats = torch.empty((self.batch, self.groups, 2), dtype=torch.float32, device=dev)
             ast = stats.data_ptr()
-        B.fno_group_norm_act_fwd(self.desc, ax, ag, ab, ar, ao, ast, *self._workspace(dev), s)
+        B.fno_group_norm_act_fwd(self.desc, ax, ag, ab, ar, ao, ast, *self._workspace(dev, s), s)
         return out, stats
 
     def bwd(self, x, g_out, stats, gamma=None, beta=None, gx=None, g_gamma=None, g_beta=None,
@@ -436,5 +449,5 @@ class GroupNormAct:
             g_beta = torch.empty(self.channels, dtype=torch.float32, device=dev)
             agb = g_beta.data_ptr()
         B.fno_group_norm_act_bwd(self.desc, ax, ag, ab, ast, ago, agx, agg, agb,
-                                 *self._workspace(dev), s)
+                                 *self._workspace(dev, s), s)
         return gx, g_gamma, g_beta
