@@ -13,7 +13,7 @@ from typing import Dict, List, Optional, Sequence, Union
 import torch
 
 from . import binding as B
-from .layer import DTYPE_CODES, _addr, _stream_of
+from .layer import DTYPE_CODES, _addr, _external, _stream_of
 
 _dtype_of = attrgetter("dtype")
 
@@ -41,7 +41,11 @@ class AdamW:
     device_control: the step number, the clipped scale and the skip of
     non-finite gradients live on the GPU; each `step` then follows one
     `clip_grads`, nothing is read by the host, and both can be captured in a
-    HIP graph.  Calls of one object belong on one stream.
+    HIP graph.  Calls of one object belong on one stream (or on streams that
+    wait for each other); what the object makes itself is filled when the
+    constructor returns, so that any stream may take the first call.  The
+    caller's tensors are the caller's: where `stream` is given, it has waited
+    for their values, and they stay until its work is done.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
@@ -103,6 +107,14 @@ class AdamW:
             self._factor = self.control[44:48].view(torch.float32)
             self._ws = torch.empty(B.fno_grad_norm_workspace_size(self._list, n),
                                    dtype=torch.uint8, device=self.device)
+        # memory that torch handed out here, and the streams whose work it outlives
+        self._made = [v for s in self.states for v in s.values()] if states is None else []
+        if device_control:
+            self._made += [self.control, self._ws]
+        home = torch.cuda.current_stream(self.device)
+        self._outlives = {home.cuda_stream}
+        if self._made:
+            home.synchronize()
 
     # -- construction ------------------------------------------------------------
     def _per_tensor(self, v, name):
@@ -165,6 +177,14 @@ class AdamW:
                 v for s in self.states for v in s.values()]]
 
     # -- the calls ---------------------------------------------------------------
+    def _on(self, stream):
+        s = _stream_of(self.device, stream)
+        if s not in self._outlives:
+            for t in self._made:
+                t.record_stream(_external(self.device, s))
+            self._outlives.add(s)
+        return s
+
     def clip_grads(self, max_norm: float = float("inf"), loss_scale: float = 1.0,
                    stream: Optional[int] = None) -> torch.Tensor:
         """The global norm of the gradients over `loss_scale` (returned, a
@@ -176,7 +196,7 @@ class AdamW:
             raise ValueError(f"loss_scale {loss_scale}, expected more than 0")
         B.fno_grad_norm(self.desc, self._list, len(self.params), max_norm, 1.0 / loss_scale,
                         self.control.data_ptr(), self._ws.data_ptr(), self._ws.numel(),
-                        _stream_of(self.device, stream))
+                        self._on(stream))
         return self._norm
 
     def step(self, grads: Optional[Sequence[torch.Tensor]] = None, lr: Optional[float] = None,
@@ -189,7 +209,7 @@ class AdamW:
             self.set_grads(grads)
         if lr is not None:
             self.desc.lr = float(lr)
-        s = _stream_of(self.device, stream)
+        s = self._on(stream)
         if self.control is not None:
             B.fno_adamw_step(self.desc, self._list, len(self.params), 0, self.control.data_ptr(), s)
         else:
@@ -228,7 +248,7 @@ class AdamW:
         in `dtype` or the caller's (then a full list of one type each; entries
         of 32-bit states stay as they are)."""
         eight = self._eight
-        s = _stream_of(self.device, stream)
+        s = self._on(stream)
         outs, ptrs = [], []
         for k, given in (("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq)):
             if given is None:

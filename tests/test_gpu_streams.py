@@ -11,6 +11,7 @@ pytestmark = [pytest.mark.gpu,
 
 from paper_2307_15034_amd import binding as B  # noqa: E402
 from paper_2307_15034_amd.layer import GroupNormAct  # noqa: E402
+from paper_2307_15034_amd.optim import AdamW  # noqa: E402
 
 WAIT = 20_000_000  # cycles
 
@@ -98,3 +99,60 @@ def test_norm_first_call_inside_a_capture():
         torch.cuda.synchronize()
         assert torch.equal(out, ref) and torch.equal(st, rst)
         del junk
+
+
+N = 300001
+
+
+def _params():
+    g = torch.Generator(device="cuda").manual_seed(7)
+    return [torch.randn(N, device="cuda", generator=g) for _ in range(2)]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("control", [False, True])
+def test_adamw_first_step_on_another_stream(bits, control):
+    """The constructor's own tensors are filled behind a busy current stream,
+    in blocks that held other values; the first step on another stream finds
+    them filled."""
+    p, g = _params()
+    ref = p.clone()
+    AdamW([ref], [g], state_bits=bits).step()
+    q = p.clone()
+    torch.cuda.synchronize()
+    junk = [torch.full((N,), 3.0, device="cuda") for _ in range(4)]
+    junk += [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (N, N, 64, 512, 8192)]
+    torch.cuda._sleep(WAIT)
+    del junk
+    opt = AdamW([q], [g], state_bits=bits, device_control=control)
+    s = torch.cuda.Stream()
+    if control:
+        opt.clip_grads(stream=s.cuda_stream)
+    opt.step(stream=s.cuda_stream)
+    s.synchronize()
+    assert torch.equal(q, ref)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_states_outlive_their_object(bits):
+    """The object goes while another stream's step is still queued."""
+    p, g = _params()
+    ref = p.clone()
+    opt = AdamW([ref], [g], state_bits=bits, device_control=True)
+    opt.clip_grads()
+    opt.step()
+    q = p.clone()
+    opt = AdamW([q], [g], state_bits=bits, device_control=True)
+    made = {t.data_ptr(): (t.numel(), t.dtype) for t in opt._made}
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    _busy(s)
+    opt.clip_grads(stream=s.cuda_stream)
+    opt.step(stream=s.cuda_stream)
+    del opt
+    others = [torch.full((n,), 1, dtype=dt, device="cuda") for n, dt in made.values()
+              for _ in range(3)]
+    assert not s.query()
+    assert not made.keys() & {t.data_ptr() for t in others}
+    s.synchronize()
+    assert torch.equal(q, ref)
