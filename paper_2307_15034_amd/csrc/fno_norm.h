@@ -294,40 +294,61 @@ __device__ __forceinline__ void write_stat(const NormArgs& a, int64_t bg, const 
   a.stats[2 * bg + 1] = st.rstd;
 }
 
-// What the backward needs of a channel: d = x - mu, z = d k + beta (k = r gamma),
-// h = g_out act'(z); the sums of h and, with r put to it at the end, of h d.
+// What the backward needs of a channel: d = (x - mu) s, z = d k + beta with
+// k = (r / s) gamma; h = g_out act'(z); the sums of h and of h d, r / s put to
+// it at the end; gx = r (gamma h - a - xh m), m the group's mean of gamma h xh.
+// s is the power of two below r, so that d, k and the sums are of the size of
+// xh and gamma at any spread (with x - mu itself r^2 would come in, which leaves
+// fp32 at spreads of 1e19 and, with eps 0, of 1e-19), and x s - mu s is one
+// operation, rounded like x - mu.  An fp16 group's spread lies between 1e-13 and
+// 1e5, which squared stay inside: s = 1.
+template <typename T>
+constexpr bool kNarrow = false;
+template <>
+inline constexpr bool kNarrow<_Float16> = true;
+
 struct Coef {
-  float mu, rs, k, ga, be;
+  float mu, s;    // mu times s
+  float rs, rel;  // r, r / s
+  float k, ga, be;
 };
+template <typename T>
 __device__ __forceinline__ Coef bwd_coef(const NormArgs& a, int64_t bg, int c) {
-  const float* st = a.stats_in + 2 * bg;
+  const float mu = a.stats_in[2 * bg], rs = a.stats_in[2 * bg + 1];
+  // (of an r below the normal numbers: the smallest of these)
+  const float s = kNarrow<T> ? 1.0f : __uint_as_float(max(__float_as_uint(rs) & 0x7f800000u, 0x00800000u));
+  const float rel = kNarrow<T> ? rs : rs / s;
   const float ga = a.gamma ? a.gamma[c] : 1.0f;
-  return Coef{st[0], st[1], st[1] * ga, ga, a.beta ? a.beta[c] : 0.0f};
+  return Coef{mu * s, s, rs, rel, rel * ga, ga, a.beta ? a.beta[c] : 0.0f};
+}
+template <typename T>
+__device__ __forceinline__ float distance(const Coef& k, T x) {
+  return kNarrow<T> ? less(x, k.mu) : __builtin_fmaf((float)x, k.s, -k.mu);
 }
 // (Both passes form h alike: in a group whose values hardly differ gx is the
 // small difference of large terms, and would show any difference of the two.)
 template <int ACT, typename T>
 __device__ __forceinline__ void bwd_terms(const Coef& k, T x, T g, float* h, float* d) {
-  *d = less(x, k.mu);
+  *d = distance(k, x);
   *h = (float)g * act_grad_f<ACT>(__builtin_fmaf(*d, k.k, k.be));
 }
 // The sums of h and h xh; where the statistics are not finite, not numbers (h
 // itself may be finite there).
 __device__ __forceinline__ float2 bwd_sums(const Coef& k, float s, float q) {
-  return make_float2(__builtin_fmaf(0.0f, k.rs, s), q * k.rs);
+  return make_float2(__builtin_fmaf(0.0f, k.rel, s), q * k.rel);
 }
-// gx = r (gamma h - a - xh d) with xh = r (x - mu).
+// gx = r gamma h + c1 d + c0.
 struct Means {
   float a, d;
 };
 struct Gx {
-  float c0, c1;
+  float c0, c1, k;
 };
 __device__ __forceinline__ Gx gx_coef(const Coef& k, const Means& m) {
-  return Gx{-k.rs * m.a, -(k.rs * m.d) * k.rs};
+  return Gx{-k.rs * m.a, -(k.rs * m.d) * k.rel, k.rs * k.ga};
 }
-__device__ __forceinline__ float bwd_gx(const Coef& k, const Gx& m, float h, float d) {
-  return __builtin_fmaf(k.k, h, __builtin_fmaf(d, m.c1, m.c0));
+__device__ __forceinline__ float bwd_gx(const Gx& m, float h, float d) {
+  return __builtin_fmaf(m.k, h, __builtin_fmaf(d, m.c1, m.c0));
 }
 __device__ __forceinline__ Means means_of(const NormArgs& a, const Sums& t) {
   const double m = (double)a.P * a.Cg;

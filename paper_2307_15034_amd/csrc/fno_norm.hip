@@ -214,10 +214,11 @@ __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float
     Coef k[V];
     float s[V], q[V];
     my_channels<V, UNI>(a, [&](int j, int c, int gr) {
-      k[j] = bwd_coef(a, b * a.G + gr, c);
+      k[j] = bwd_coef<T>(a, b * a.G + gr, c);
       if (UNI && j) {
         k[j].mu = k[0].mu;
-        k[j].rs = k[0].rs;
+        k[j].s = k[0].s;
+        k[j].rel = k[0].rel;
       }
       s[j] = q[j] = 0.0f;
     });
@@ -289,11 +290,13 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means*
   Coef k[V];
   Gx gk[V];
   my_channels<V, UNI>(a, [&](int j, int c, int gr) {
-    k[j] = bwd_coef(a, b * a.G + gr, c);
+    k[j] = bwd_coef<T>(a, b * a.G + gr, c);
     gk[j] = gx_coef(k[j], lds[gr]);
     if (UNI && j) {
       k[j].mu = k[0].mu;
-      gk[j] = gk[0];
+      k[j].s = k[0].s;
+      gk[j].c0 = gk[0].c0;
+      gk[j].c1 = gk[0].c1;
     }
   });
   data.run(
@@ -303,7 +306,7 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means*
         for (int j = 0; j < V; ++j) {
           float h, d;
           bwd_terms<ACT>(k[j], p.x.e[j], p.y.e[j], &h, &d);
-          o.e[j] = (T)bwd_gx(k[j], gk[j], h, d);
+          o.e[j] = (T)bwd_gx(gk[j], h, d);
         }
         store_result<T, V>(out + my_at(a, i, V), o, KIND != kAny);
       });
@@ -314,7 +317,7 @@ __device__ __forceinline__ void flat_bwd(const NormArgs& a, int64_t unit, Means*
       if (m.base + at + j < a.R) {
         float h, d;
         bwd_terms<ACT>(k[j], x[at + j], g[at + j], &h, &d);
-        out[at + j] = (T)bwd_gx(k[j], gk[j], h, d);
+        out[at + j] = (T)bwd_gx(gk[j], h, d);
       }
   }
 }
@@ -448,14 +451,14 @@ __global__ __launch_bounds__(NT) void wide_sums_kernel(NormArgs a) {
     float s[W], q[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      k[j] = bwd_coef(a, w.b * a.G + (w.c + j) / a.Cg, w.c + j);
+      k[j] = bwd_coef<T>(a, w.b * a.G + (w.c + j) / a.Cg, w.c + j);
       s[j] = q[j] = 0.0f;
     }
     over_rows<T, W>(a, w, static_cast<const T*>(a.x), static_cast<const T*>(a.gout),
                     [&](int64_t, const Vec<T, W>& x, const Vec<T, W>& g) {
 #pragma unroll
                       for (int j = 0; j < W; ++j) {
-                        const float d = (float)x.e[j] - k[j].mu;
+                        const float d = distance(k[j], x.e[j]);
                         const float h = (float)g.e[j] *
                                         act_grad_any(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
                         s[j] += h;
@@ -483,7 +486,7 @@ __global__ __launch_bounds__(NT) void wide_bwd_kernel(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const int64_t bg = w.b * a.G + (w.c + j) / a.Cg;
-      k[j] = bwd_coef(a, bg, w.c + j);
+      k[j] = bwd_coef<T>(a, bg, w.c + j);
       gk[j] = gx_coef(k[j], means_of(a, a.joined[bg]));
     }
     T* out = static_cast<T*>(a.out) + w.at;
@@ -492,10 +495,10 @@ __global__ __launch_bounds__(NT) void wide_bwd_kernel(NormArgs a) {
                       Vec<T, W> o;
 #pragma unroll
                       for (int j = 0; j < W; ++j) {
-                        const float d = (float)x.e[j] - k[j].mu;
+                        const float d = distance(k[j], x.e[j]);
                         const float h = (float)g.e[j] *
                                         act_grad_any(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
-                        o.e[j] = (T)bwd_gx(k[j], gk[j], h, d);
+                        o.e[j] = (T)bwd_gx(gk[j], h, d);
                       }
                       store_result<T, W>(out + i * a.C, o, a.nt);
                     });
@@ -625,7 +628,7 @@ __global__ __launch_bounds__(NT) void first_sums_kernel(NormArgs a) {
     const T* x = static_cast<const T*>(a.x) + s.at;
     const T* g = static_cast<const T*>(a.gout) + s.at;
     auto data = segment<T, TEAM, 1, false>(x, g, s.len);
-    const Coef k = bwd_coef(a, s.bg, s.c);
+    const Coef k = bwd_coef<T>(a, s.bg, s.c);
     float sh = 0.0f, sx = 0.0f;
     auto one = [&](T xv, T gv) {
       float h, d;
@@ -658,13 +661,13 @@ __global__ __launch_bounds__(NT) void first_bwd_kernel(NormArgs a) {
     const T* x = static_cast<const T*>(a.x) + s.at;
     const T* g = static_cast<const T*>(a.gout) + s.at;
     auto data = segment<T, TEAM, 3, true>(x, g, s.len);
-    const Coef k = bwd_coef(a, s.bg, s.c);
+    const Coef k = bwd_coef<T>(a, s.bg, s.c);
     const Gx gk = gx_coef(k, means_of(a, group_of<TEAM>(a, s.bg)));
     T* out = static_cast<T*>(a.out) + s.at;
     auto one = [&](T xv, T gv) {
       float h, d;
       bwd_terms<ACT>(k, xv, gv, &h, &d);
-      return bwd_gx(k, gk, h, d);
+      return bwd_gx(gk, h, d);
     };
     over_segment<T, TEAM>(
         data, s.len,

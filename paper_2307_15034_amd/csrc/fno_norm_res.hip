@@ -190,7 +190,7 @@ __global__ __launch_bounds__(THREADS) void res_first_bwd_kernel(NormArgs a) {
     over_pieces<K>(s, [&](int k, int c, int v, bool start) {
       if (c >= a.Cg) return;  // the same for the wave's lanes
       if (start) sh = sq = 0.0f;
-      const Coef q = bwd_coef(a, bg, c0 + c);
+      const Coef q = bwd_coef<T>(a, bg, c0 + c);
       float d;
       if (v < nv)
 #pragma unroll
@@ -225,16 +225,16 @@ __global__ __launch_bounds__(THREADS) void res_first_bwd_kernel(NormArgs a) {
     const Means m = means_of(a, block_sums<THREADS>(t, red));
     over_pieces<K>(s, [&](int k, int c, int v, bool start) {
       if (c >= a.Cg) return;
-      const Coef q = bwd_coef(a, bg, c0 + c);
+      const Coef q = bwd_coef<T>(a, bg, c0 + c);
       const Gx gk = gx_coef(q, m);
       if (v < nv) {
         Vec<T, V> o;
 #pragma unroll
-        for (int j = 0; j < V; ++j) o.e[j] = (T)bwd_gx(q, gk, h[k][j], less(xv[k].e[j], q.mu));
+        for (int j = 0; j < V; ++j) o.e[j] = (T)bwd_gx(gk, h[k][j], distance(q, xv[k].e[j]));
         store_vec<T, V>(out + (uint32_t)(c * P + v * V), o);
       }
       if (start && s.lane < rest)
-        out[(uint32_t)(c * P + nv * V + s.lane)] = (T)bwd_gx(q, gk, ht[k], less(xt[k], q.mu));
+        out[(uint32_t)(c * P + nv * V + s.lane)] = (T)bwd_gx(gk, ht[k], distance(q, xt[k]));
     });
     __syncthreads();
   }
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(THREADS) void res_last_bwd_kernel(NormArgs a) {
     float h[K][W], sh[W], sq[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      q[j] = bwd_coef(a, bg, w.c + j);
+      q[j] = bwd_coef<T>(a, bg, w.c + j);
       sh[j] = sq[j] = 0.0f;
     }
 #pragma unroll
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(THREADS) void res_last_bwd_kernel(NormArgs a) {
         if (row >= P) continue;
         Vec<T, W> o;
 #pragma unroll
-        for (int j = 0; j < W; ++j) o.e[j] = (T)bwd_gx(q[j], gk[j], h[k][j], less(xv[k].e[j], q[j].mu));
+        for (int j = 0; j < W; ++j) o.e[j] = (T)bwd_gx(gk[j], h[k][j], distance(q[j], xv[k].e[j]));
         store_vec<T, W>(out + (int64_t)row * a.C, o);
       }
     }

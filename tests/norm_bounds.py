@@ -73,15 +73,18 @@ def close(name, got, ref, bound):
 
 
 def check_elements(grid, batch, channels, groups, dt, act, last, residual=False, seed=0,
-                   eps=1e-5, g_out=None):
+                   eps=1e-5, g_out=None, spread=1.0):
     """Forward and backward into buffers that hold NaN, with inputs of ordinary
-    size (g_out: a constant in place of noise)."""
+    size (x times `spread`; g_out: a constant in place of noise)."""
     from tests.test_gpu_norm import ACT, DT, _inputs
-    say(f"norm elements grid={grid} B={batch} C={channels} G={groups} {dt} {act} last={last}")
+    say(f"norm elements grid={grid} B={batch} C={channels} G={groups} {dt} {act} last={last} "
+        f"spread={spread}")
     op = GroupNormAct(grid, batch, channels, groups, DT[dt], ACT[act], last, eps)
     x, ga, be, g, res = _inputs(seed, grid, batch, channels, dt, last)
     if g_out is not None:
         g.fill_(g_out)
+    if spread != 1.0:
+        x = (x.float() * spread).to(x.dtype)
     nan = float("nan")
     f32 = dict(dtype=torch.float32, device="cuda")
     out, gx = torch.full_like(x, nan), torch.full_like(x, nan)

@@ -21,3 +21,28 @@ from tests.norm_bounds import check_elements  # noqa: E402
 def test_wide_groups_of_few_rows(channels, groups, points, dt):
     """Channels last, one or two rows to a sample: a layer norm over features."""
     check_elements((points,), 3, channels, groups, dt, "gelu", True, points == 2, seed=400)
+
+
+ROUTES = [
+    # (points, batch, channels, groups, channels last)
+    (100, 2, 12, 3, False),      # a group held by one work-group
+    (100, 2, 12, 3, True),
+    (6000, 2, 16, 2, True),      # two passes, whole vectors of a group
+    (6000, 2, 20, 4, True),      # groups that cross vectors
+    (200, 2, 1025, 5, True),     # more channels than a work-group has pieces
+    (300, 2, 4096, 2, True),
+    (8000, 1, 12, 3, False),     # a wave to a plane
+    (40001, 1, 6, 2, False),     # a work-group to a segment of it
+]
+
+
+@pytest.mark.parametrize("spread", [1e-22, 1e-12, 1e12, 1e19, 1e21, 1e24, 1e30, 1e36])
+@pytest.mark.parametrize("dt", ["fp32", "bf16"])
+@pytest.mark.parametrize("route", range(len(ROUTES)))
+def test_spreads(route, dt, spread):
+    """Values whose squares leave fp32, and 1 / spread's: the statistics are
+    finite (eps 0 for the small ones) and so is every term of the formula."""
+    points, b, c, groups, last = ROUTES[route]
+    act = ("gelu", "silu", "none")[route % 3]
+    check_elements((points,), b, c, groups, dt, act, last, route % 2 == 0 and spread < 1e30,
+                   seed=410 + route, eps=0.0 if spread < 1 else 1e-5, spread=spread)
