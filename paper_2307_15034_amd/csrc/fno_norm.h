@@ -332,10 +332,13 @@ __device__ __forceinline__ void bwd_terms(const Coef& k, T x, T g, float* h, flo
   *d = distance(k, x);
   *h = (float)g * act_grad_f<ACT>(__builtin_fmaf(*d, k.k, k.be));
 }
-// The sums of h and h xh; where the statistics are not finite, not numbers (h
-// itself may be finite there).
-__device__ __forceinline__ float2 bwd_sums(const Coef& k, float s, float q) {
-  return make_float2(__builtin_fmaf(0.0f, k.rel, s), q * k.rel);
+// The sums of h and h xh.  Where the statistics are not finite, or behind an
+// activation gamma or beta, they are not numbers: h itself may be finite there
+// (the derivative of GELU is, for any z), and so would gx be.
+__device__ __forceinline__ float2 bwd_sums(const Coef& k, int act, float s, float q) {
+  float bad = 0.0f * k.rel;
+  if (act != FNO_NORM_ACT_NONE) bad = __builtin_fmaf(0.0f, k.k, __builtin_fmaf(0.0f, k.be, bad));
+  return make_float2(s + bad, __builtin_fmaf(q, k.rel, bad));
 }
 // gx = r gamma h + c1 d + c0.
 struct Means {

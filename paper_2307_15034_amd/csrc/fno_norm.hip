@@ -244,7 +244,7 @@ __device__ __forceinline__ void flat_sums(const NormArgs& a, int64_t unit, float
         }
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) lds[threadIdx.x * V + j] = bwd_sums(k[j], s[j], q[j]);
+    for (int j = 0; j < V; ++j) lds[threadIdx.x * V + j] = bwd_sums(k[j], ACT, s[j], q[j]);
   }
   __syncthreads();
   // element f = V t + j of the threads is channel f mod C's
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(NT) void wide_sums_kernel(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const int64_t at = (w.b * a.C + w.c + j) * a.n1 + w.chunk;
-      const float2 t = bwd_sums(k[j], s[j], q[j]);
+      const float2 t = bwd_sums(k[j], a.act, s[j], q[j]);
       a.chan[at] = Sums{t.x, t.y};
       a.part[at] = Sums{(double)k[j].ga * t.x, (double)k[j].ga * t.y};
     }
@@ -643,7 +643,7 @@ __global__ __launch_bounds__(NT) void first_sums_kernel(NormArgs a) {
           for (int j = 0; j < V; ++j) one(xv.e[j], gv.e[j]);
         },
         [&](int e) { one(x[e], g[e]); });
-    const float2 mine = bwd_sums(k, sh, sx);
+    const float2 mine = bwd_sums(k, ACT, sh, sx);
     const Sums t = team_sum<TEAM>(Sums{mine.x, mine.y});
     if ((threadIdx.x & (TEAM - 1)) == 0) {
       a.chan[u] = t;

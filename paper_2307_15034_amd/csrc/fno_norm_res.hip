@@ -207,7 +207,7 @@ __global__ __launch_bounds__(THREADS) void res_first_bwd_kernel(NormArgs a) {
       // the plane's last piece: its sums over the wave
       const int turn = (c - s.team) / s.teams, done = k - turn * s.per + 1;
       if (done < s.per) return;
-      const float2 m = bwd_sums(q, sh, sq);
+      const float2 m = bwd_sums(q, ACT, sh, sq);
       const Sums w = team_sum<64>(Sums{m.x, m.y});
       if ((threadIdx.x & 63) == 0) part[((int)threadIdx.x >> 6) * K + turn] = make_float2((float)w.s, (float)w.q);
     });
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(THREADS) void res_last_bwd_kernel(NormArgs a) {
           sq[j] = __builtin_fmaf(h[k][j], d, sq[j]);
         }
 #pragma unroll
-    for (int j = 0; j < W; ++j) lds[threadIdx.x * W + j] = bwd_sums(q[j], sh[j], sq[j]);
+    for (int j = 0; j < W; ++j) lds[threadIdx.x * W + j] = bwd_sums(q[j], ACT, sh[j], sq[j]);
     __syncthreads();
     // entry [t][j] is channel (t mod S) W + j of the group
     group_sums<THREADS>(a.Cg, w.step,

@@ -1,5 +1,6 @@
 """Group norm with an activation on the GPU where its kernels' limits, ranges
 and values that are not numbers lie: every element within a bound of its own."""
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -7,7 +8,9 @@ torch = pytest.importorskip("torch")
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
 
-from tests.norm_bounds import check_elements  # noqa: E402
+from tests.norm_bounds import check_elements, rows  # noqa: E402
+from tests.test_gpu_norm import ACT, DT, _inputs  # noqa: E402
+from paper_2307_15034_amd.layer import GroupNormAct  # noqa: E402
 
 
 @pytest.mark.parametrize("dt", ["fp16", "bf16"])
@@ -46,3 +49,38 @@ def test_spreads(route, dt, spread):
     act = ("gelu", "silu", "none")[route % 3]
     check_elements((points,), b, c, groups, dt, act, last, route % 2 == 0 and spread < 1e30,
                    seed=410 + route, eps=0.0 if spread < 1 else 1e-5, spread=spread)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("where", ["beta", "gamma"])
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+@pytest.mark.parametrize("dt", ["fp16", "fp32"])
+@pytest.mark.parametrize("route", range(len(ROUTES)))
+def test_parameter_that_is_no_number(route, dt, act, where, bad):
+    """It reaches what depends on it, and only that: behind an activation the
+    channel's parameter gradients and its group's gx; without one, gx alone and
+    by gamma alone.  (Infinite ones are so too: z is, and z exp(-z^2) is 0 inf.)"""
+    points, b, c, groups, last = ROUTES[route]
+    op = GroupNormAct((points,), b, c, groups, DT[dt], ACT[act], last, 1e-5)
+    x, ga, be, g, _ = _inputs(430 + route, (points,), b, c, dt, last)
+    _, st = op.fwd(x, ga, be)
+    clean = [rows(op.bwd(x, g, st, ga, be)[0], last)] + list(op.bwd(x, g, st, ga, be)[1:])
+    ch, per = c - 2, c // groups
+    (be if where == "beta" else ga)[ch] = bad
+    out, st2 = op.fwd(x, ga, be)
+    assert torch.equal(st, st2)
+    if bad != bad:
+        o = rows(out, last)
+        assert np.isnan(o[:, ch]).all() and np.isfinite(np.delete(o, ch, 1)).all()
+    gx, gg, gb = op.bwd(x, g, st, ga, be)
+    gx = rows(gx, last)
+    group = np.arange(c) // per == ch // per
+    if act != "none":
+        assert torch.isnan(gg[ch]) and torch.isnan(gb[ch])
+        clean[1][ch] = clean[2][ch] = gg[ch] = gb[ch] = 0
+    if act != "none" or where == "gamma":
+        # (the formula with an infinite gamma and no activation: r (gamma h - a - xh m), a and m infinite)
+        assert (np.isnan(gx) if act != "none" or bad != bad else ~np.isfinite(gx))[:, group].all()
+        gx[:, group] = clean[0][:, group] = 0
+    assert np.array_equal(gx, clean[0])
+    assert torch.equal(gg, clean[1]) and torch.equal(gb, clean[2])
