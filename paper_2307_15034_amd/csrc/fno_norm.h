@@ -70,7 +70,8 @@ __device__ __forceinline__ void store_result(T* p, const Vec<T, W>& v, int nt) {
 // Activations
 // --------------------------------------------------------------------------
 // GELU z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt 2) / 2, with half of erfc by
-// Abramowitz & Stegun 7.1.26 (absolute error at most 0.75e-7).
+// Abramowitz & Stegun 7.1.26 (absolute error at most 0.75e-7).  inf for inf, NaN
+// for -inf (-inf times 0), as the definition has it.
 __device__ __forceinline__ float gelu_of(float z) {
   const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.23164189f, 1.0f));
   float p = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);
@@ -78,7 +79,7 @@ __device__ __forceinline__ float gelu_of(float z) {
   p = __builtin_fmaf(t, p, -0.142248368f);
   p = __builtin_fmaf(t, p, 0.127414796f);
   const float e = __builtin_amdgcn_exp2f(z * (z * -0.72134752044448f));
-  return __builtin_fmaf(-__builtin_fabsf(z), p * t * e, __builtin_fmaxf(z, 0.0f));
+  return __builtin_fmaf(-__builtin_fabsf(__builtin_fminf(z, 3.402823466e+38f)), p * t * e, __builtin_fmaxf(z, 0.0f));
 }
 // Its derivative Phi(z) + z phi(z) as 1/2 + z P(z^2) / Q(z^2) for |z| <= 5.6,
 // constant beyond: a rational fit of degrees (5, 5) to the definition (least

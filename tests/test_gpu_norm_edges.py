@@ -84,3 +84,26 @@ def test_parameter_that_is_no_number(route, dt, act, where, bad):
         gx[:, group] = clean[0][:, group] = 0
     assert np.array_equal(gx, clean[0])
     assert torch.equal(gg, clean[1]) and torch.equal(gb, clean[2])
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+@pytest.mark.parametrize("dt", ["fp16", "fp32"])
+@pytest.mark.parametrize("route", range(len(ROUTES)))
+def test_infinite_arguments_of_the_activation(route, dt, act):
+    """z Phi(z) and z / (1 + exp(-z)) are inf for inf and not defined (-inf 0)
+    for -inf; a z that overflows is one of them."""
+    points, b, c, groups, last = ROUTES[route]
+    op = GroupNormAct((points,), b, c, groups, DT[dt], ACT[act], last, 1e-5)
+    x, _, _, _, _ = _inputs(440 + route, (points,), b, c, dt, last)
+    be = torch.zeros(c, device="cuda")
+    be[0], be[c - 1] = float("inf"), -float("inf")
+    out = rows(op.fwd(x, None, be)[0], last)
+    assert (out[:, 0] == np.inf).all()
+    assert (out[:, c - 1] == -np.inf).all() if act == "none" else np.isnan(out[:, c - 1]).all()
+    assert np.isfinite(out[:, 1:c - 1]).all()
+    # z = 3e38 xh passes the largest float where xh > 1.2
+    ga = torch.ones(c, device="cuda")
+    ga[0] = 3e38
+    out, st = op.fwd(x, ga)
+    xh = (rows(x, last)[:, :1] - st[:, :1, :1].double().cpu().numpy()) * st[:, :1, 1:].double().cpu().numpy()
+    assert (rows(out, last)[:, :1][xh > 1.2] == np.inf).all()
