@@ -170,7 +170,7 @@ __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* 
       [&](const Pair<T, V>& p, int k) {
         float y[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) y[j] = act_f<ACT>(on_line(l[j], p.x.e[j]));
+        for (int j = 0; j < V; ++j) y[j] = act_any<T>(on_line(l[j], p.x.e[j]), ACT);
         if (res)
 #pragma unroll
           for (int j = 0; j < V; ++j) y[j] += (float)p.y.e[j];
@@ -184,7 +184,7 @@ __device__ __forceinline__ void flat_fwd(const NormArgs& a, int64_t unit, Stat* 
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (m.base + at + j < a.R) {
-        float y = act_f<ACT>(on_line(l[j], x[at + j]));
+        float y = act_any<T>(on_line(l[j], x[at + j]), ACT);
         if (res) y += (float)r[at + j];
         out[at + j] = (T)y;
       }
@@ -377,13 +377,6 @@ __device__ __forceinline__ Wide my_wide(const NormArgs& a, int64_t unit) {
   return w;
 }
 
-__device__ __forceinline__ float act_any(float z, int act) {
-  return act == FNO_NORM_ACT_GELU ? gelu_of(z) : act == FNO_NORM_ACT_SILU ? silu_f(z) : z;
-}
-__device__ __forceinline__ float act_grad_any(float z, int act) {
-  return act == FNO_NORM_ACT_GELU ? gelu_grad_of(z) : act == FNO_NORM_ACT_SILU ? silu_grad_f(z) : 1.0f;
-}
-
 // f(row, vector of x, vector of the second tensor) for the thread's rows.
 template <typename T, int W, typename F>
 __device__ __forceinline__ void over_rows(const NormArgs& a, const Wide& w, const T* x, const T* y, F f) {
@@ -433,7 +426,7 @@ __global__ __launch_bounds__(NT) void wide_fwd_kernel(NormArgs a) {
                       Vec<T, W> o;
 #pragma unroll
                       for (int j = 0; j < W; ++j) {
-                        float y = act_any(on_line(l[j], v.e[j]), a.act);
+                        float y = act_any<T>(on_line(l[j], v.e[j]), a.act);
                         if (a.res) y += (float)r.e[j];
                         o.e[j] = (T)y;
                       }
@@ -460,7 +453,7 @@ __global__ __launch_bounds__(NT) void wide_sums_kernel(NormArgs a) {
                       for (int j = 0; j < W; ++j) {
                         const float d = distance(k[j], x.e[j]);
                         const float h = (float)g.e[j] *
-                                        act_grad_any(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
+                                        act_grad_any<T>(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
                         s[j] += h;
                         q[j] = __builtin_fmaf(h, d, q[j]);
                       }
@@ -497,7 +490,7 @@ __global__ __launch_bounds__(NT) void wide_bwd_kernel(NormArgs a) {
                       for (int j = 0; j < W; ++j) {
                         const float d = distance(k[j], x.e[j]);
                         const float h = (float)g.e[j] *
-                                        act_grad_any(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
+                                        act_grad_any<T>(__builtin_fmaf(d, k[j].k, k[j].be), a.act);
                         o.e[j] = (T)bwd_gx(gk[j], h, d);
                       }
                       store_result<T, W>(out + i * a.C, o, a.nt);
@@ -603,7 +596,7 @@ __global__ __launch_bounds__(NT) void first_fwd_kernel(NormArgs a) {
         [&](int e, const Vec<T, V>& v, const Vec<T, V>& rv) {
           float y[V];
 #pragma unroll
-          for (int j = 0; j < V; ++j) y[j] = act_f<ACT>(on_line(l, v.e[j]));
+          for (int j = 0; j < V; ++j) y[j] = act_any<T>(on_line(l, v.e[j]), ACT);
           if (r)
 #pragma unroll
             for (int j = 0; j < V; ++j) y[j] += (float)rv.e[j];
@@ -613,7 +606,7 @@ __global__ __launch_bounds__(NT) void first_fwd_kernel(NormArgs a) {
           store_result<T, V>(out + e, o, a.nt);
         },
         [&](int e) {
-          float y = act_f<ACT>(on_line(l, x[e]));
+          float y = act_any<T>(on_line(l, x[e]), ACT);
           if (r) y += (float)r[e];
           out[e] = (T)y;
         });

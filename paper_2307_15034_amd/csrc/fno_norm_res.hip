@@ -48,7 +48,7 @@ template <typename T, int W, int ACT>
 __device__ __forceinline__ Vec<T, W> forward_vec(const Vec<T, W>& x, const Vec<T, W>& r, bool res, const Line* l, int step) {
   float y[W];
 #pragma unroll
-  for (int j = 0; j < W; ++j) y[j] = act_f<ACT>(on_line(l[j * step], x.e[j]));
+  for (int j = 0; j < W; ++j) y[j] = act_any<T>(on_line(l[j * step], x.e[j]), ACT);
   if (res)
 #pragma unroll
     for (int j = 0; j < W; ++j) y[j] += (float)r.e[j];
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(THREADS) void res_first_fwd_kernel(NormArgs a) {
       const Line l = line_of(a, st, c0 + c);
       if (v < nv) store_vec<T, V>(out + (uint32_t)(c * P + v * V), forward_vec<T, V, ACT>(xv[k], rv[k], r != nullptr, &l, 0));
       if (start && s.lane < rest) {
-        float y = act_f<ACT>(on_line(l, xt[k]));
+        float y = act_any<T>(on_line(l, xt[k]), ACT);
         if (r) y += (float)rt[k];
         out[(uint32_t)(c * P + nv * V + s.lane)] = (T)y;
       }

@@ -8,7 +8,9 @@ torch = pytest.importorskip("torch")
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
 
-from tests.norm_bounds import check_elements, rows  # noqa: E402
+from scipy.special import ndtr  # noqa: E402
+
+from tests.norm_bounds import E, SUB, U, check_elements, close, rows  # noqa: E402
 from tests.test_gpu_norm import ACT, DT, _inputs  # noqa: E402
 from paper_2307_15034_amd.layer import GroupNormAct  # noqa: E402
 
@@ -107,3 +109,50 @@ def test_infinite_arguments_of_the_activation(route, dt, act):
     out, st = op.fwd(x, ga)
     xh = (rows(x, last)[:, :1] - st[:, :1, :1].double().cpu().numpy()) * st[:, :1, 1:].double().cpu().numpy()
     assert (rows(out, last)[:, :1][xh > 1.2] == np.inf).all()
+
+
+FLAT = [
+    # (points, channels, groups, channels last): the routes again, of many channels
+    (16, 1024, 4, True), (16, 1024, 4, False), (6000, 64, 8, True), (6000, 60, 4, True),
+    (200, 4096, 1, True), (200, 1025, 5, True), (8000, 64, 8, False), (40001, 64, 8, False)]
+
+
+@pytest.mark.parametrize("dt", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("route", range(len(FLAT)))
+def test_gelu_itself(route, dt):
+    """A group of zeros: z is beta, exactly; with g_out 1 at one point and 0
+    elsewhere g_beta is the derivative.
+
+    16-bit tensors: 10 E |z| (erfc to 0.75e-7) beside the stored result's
+    rounding, and 10 E for the derivative (3.3e-7).  fp32 (E = 2^-24): below 1.5
+    z (1/2 + z A) is off by 2 E |z| and the rounding of the result, 1/2 + z A by 3 E;
+    beyond, the tail T = Phi(-|z|) by (16 + z^2) E T (its fit 3.5, 1 / (1 + p |z|) 4,
+    six steps 4, the products 2, exp 2 and its argument's rounding z^2), |z| T
+    likewise, z phi by (4 + z^2) E of itself."""
+    points, c, groups, last = FLAT[route]
+    r = np.random.default_rng(450 + route)
+    z = np.concatenate([r.uniform(-9, 9, c // 2), r.normal(0, 1, c - c // 2)])
+    z[:4] = 1.5, -1.5, 0.0, 1.4999999
+    z = z.astype(np.float32).astype(np.float64)
+    op = GroupNormAct((points,), 1, c, groups, DT[dt], ACT["gelu"], last, 1e-5)
+    x, g = torch.zeros(op.shape, dtype=DT[dt], device="cuda"), torch.zeros(
+        op.shape, dtype=DT[dt], device="cuda")
+    at = points * 2 // 3
+    (g[0, at] if last else g[0, :, at]).fill_(1.0)
+    be = torch.tensor(z, dtype=torch.float32, device="cuda")
+    out, st = op.fwd(x, None, be)
+    _, _, gb = op.bwd(x, g, st, None, be)
+    s = np.abs(z)
+    tail, slope = ndtr(-s), z * np.exp(-z * z / 2) / np.sqrt(2 * np.pi)
+    ref, dref = z * ndtr(z), ndtr(z) + slope
+    if dt == "fp32":
+        far = (16 + z * z) * tail
+        b = E * (np.abs(ref) + np.where(s < 1.5, 2 * s, s * far)) + 2.0 ** -126
+        db = E * (np.abs(dref) + np.where(s < 1.5, 3.0, 1.0 + far) + (4 + z * z) * np.abs(slope))
+        # below -1.5 nothing is rounded against 1
+        db = np.where(z <= -1.5, db - E, db) + 2.0 ** -126
+    else:
+        b, db = U[dt] * np.abs(ref) * 1.001 + SUB[dt] + 10 * E * s, np.full(c, 10 * E)
+    close("out", rows(out, last), np.broadcast_to(ref[None, :, None], (1, c, points)),
+          np.broadcast_to(b[None, :, None], (1, c, points)))
+    close("derivative", gb.double().cpu().numpy(), dref, db)
