@@ -442,13 +442,22 @@ __global__ __launch_bounds__(NT) void wide_sums_kernel(NormArgs a) {
     if (!w.rows) continue;
     Coef k[W];
     float s[W], q[W];
+    Sums t[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       k[j] = bwd_coef<T>(a, w.b * a.G + (w.c + j) / a.Cg, w.c + j);
       s[j] = q[j] = 0.0f;
+      t[j] = Sums{0.0, 0.0};
     }
+    auto flush = [&] {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        t[j] = add(t[j], Sums{s[j], q[j]});
+        s[j] = q[j] = 0.0f;
+      }
+    };
     over_rows<T, W>(a, w, static_cast<const T*>(a.x), static_cast<const T*>(a.gout),
-                    [&](int64_t, const Vec<T, W>& x, const Vec<T, W>& g) {
+                    [&](int64_t i, const Vec<T, W>& x, const Vec<T, W>& g) {
 #pragma unroll
                       for (int j = 0; j < W; ++j) {
                         const float d = distance(k[j], x.e[j]);
@@ -457,13 +466,15 @@ __global__ __launch_bounds__(NT) void wide_sums_kernel(NormArgs a) {
                         s[j] += h;
                         q[j] = __builtin_fmaf(h, d, q[j]);
                       }
+                      if (i % kChain == kChain - 1) flush();
                     });
+    flush();
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const int64_t at = (w.b * a.C + w.c + j) * a.n1 + w.chunk;
-      const float2 t = bwd_sums(k[j], a.act, s[j], q[j]);
-      a.chan[at] = Sums{t.x, t.y};
-      a.part[at] = Sums{(double)k[j].ga * t.x, (double)k[j].ga * t.y};
+      const Sums v = bwd_sums(k[j], a.act, t[j]);
+      a.chan[at] = v;
+      a.part[at] = Sums{(double)k[j].ga * v.s, (double)k[j].ga * v.q};
     }
   }
 }
@@ -623,21 +634,31 @@ __global__ __launch_bounds__(NT) void first_sums_kernel(NormArgs a) {
     auto data = segment<T, TEAM, 1, false>(x, g, s.len);
     const Coef k = bwd_coef<T>(a, s.bg, s.c);
     float sh = 0.0f, sx = 0.0f;
+    int n = 0;  // vectors (a wave's plane has at most 16 for a lane)
+    Sums mine{0.0, 0.0};
     auto one = [&](T xv, T gv) {
       float h, d;
       bwd_terms<ACT>(k, xv, gv, &h, &d);
       sh += h;
       sx = __builtin_fmaf(h, d, sx);
     };
+    auto flush = [&] {
+      mine = add(mine, Sums{sh, sx});
+      sh = sx = 0.0f;
+    };
     over_segment<T, TEAM>(
         data, s.len,
         [&](int, const Vec<T, V>& xv, const Vec<T, V>& gv) {
 #pragma unroll
           for (int j = 0; j < V; ++j) one(xv.e[j], gv.e[j]);
+          if (TEAM == NT && ++n % (kChain / V) == 0) flush();
         },
-        [&](int e) { one(x[e], g[e]); });
-    const float2 mine = bwd_sums(k, ACT, sh, sx);
-    const Sums t = team_sum<TEAM>(Sums{mine.x, mine.y});
+        [&](int e) {
+          flush();
+          one(x[e], g[e]);
+        });
+    flush();
+    const Sums t = team_sum<TEAM>(bwd_sums(k, ACT, mine));
     if ((threadIdx.x & (TEAM - 1)) == 0) {
       a.chan[u] = t;
       a.part[u] = Sums{(double)k.ga * t.s, (double)k.ga * t.q};
@@ -774,7 +795,9 @@ NormPlan plan_of(const fno_norm_desc& d, bool bwd) {
     const int fill = bwd && !p.uni ? kFillFew : kFill;
     const int64_t want = std::clamp<int64_t>(a.B * nv / per, fill, 4 * fill) / a.B;
     const int64_t room = std::max<int64_t>(1, nv / ((int64_t)a.A * 4));
-    const int64_t n = std::max(std::clamp<int64_t>(want, 1, room), cdiv(nv, (int64_t)1 << 26));
+    // (the backward's chunks also so that a thread adds at most kChain values of a channel)
+    const int64_t n = std::max(std::clamp<int64_t>(want, 1, room),
+                               cdiv(nv, bwd ? (int64_t)a.A * kChain : (int64_t)1 << 26));
     a.v1 = rup(cdiv(nv, n), a.A);
     a.n1 = (int)cdiv(nv, a.v1);
     a.n = a.nc = a.n1;

@@ -10,7 +10,7 @@ pytestmark = [pytest.mark.gpu,
 
 from scipy.special import ndtr  # noqa: E402
 
-from tests.norm_bounds import E, SUB, U, check_elements, close, rows  # noqa: E402
+from tests.norm_bounds import CHAIN, E, SUB, U, check_elements, close, rows  # noqa: E402
 from tests.test_gpu_norm import ACT, DT, _inputs  # noqa: E402
 from paper_2307_15034_amd.layer import GroupNormAct  # noqa: E402
 
@@ -156,3 +156,26 @@ def test_gelu_itself(route, dt):
     close("out", rows(out, last), np.broadcast_to(ref[None, :, None], (1, c, points)),
           np.broadcast_to(b[None, :, None], (1, c, points)))
     close("derivative", gb.double().cpu().numpy(), dref, db)
+
+
+@pytest.mark.parametrize("points, batch, channels, groups, last, value", [
+    (2048, 512, 257, 1, True, 0.9276756),       # a thread has a channel's rows of a sample
+    (2048, 256, 4096, 1, True, 0.9276756),      # or four channels'
+    (1 << 18, 8, 1024, 1, False, 0.9411933),    # a work-group a plane
+    (1 << 25, 2, 64, 8, True, 0.9411933),       # more than 2^32 values
+], ids=["wide", "wide-vectors", "first", "flat"])
+def test_long_sums_of_one_sign(points, batch, channels, groups, last, value):
+    """The gradient of a mean loss: one value everywhere, no activation, x zero.
+    g_beta is a plain sum, gx = value - mean(value).  In a single fp32 chain of
+    a thread's values the sums would be off by 1.4e-5 and more; CHAIN E = 7.6e-6 is
+    the bound of the longest that there is."""
+    op = GroupNormAct((points,), batch, channels, groups, torch.float32, ACT["none"], last, 1.0)
+    x = torch.zeros(op.shape, device="cuda")
+    g = torch.full(op.shape, value, device="cuda")
+    v = float(np.float32(value))
+    stats = torch.zeros((batch, groups, 2), device="cuda")
+    stats[..., 1] = 1.0
+    gx, gg, gb = op.bwd(x, g, stats, gx=g)
+    assert not gg.any()
+    assert float((gb.double() - v * batch * points).abs().max()) <= (CHAIN + 2) * E * v * batch * points
+    assert float(gx.abs().max()) <= (CHAIN + 4) * E * v
