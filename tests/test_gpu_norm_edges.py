@@ -11,7 +11,8 @@ pytestmark = [pytest.mark.gpu,
 from scipy.special import ndtr  # noqa: E402
 
 from tests.norm_bounds import CHAIN, E, SUB, U, check_elements, close, rows  # noqa: E402
-from tests.test_gpu_norm import ACT, DT, _inputs  # noqa: E402
+from tests.test_gpu_norm import ACT, DT, SHAPES, _inputs  # noqa: E402
+from tests.test_gpu_train_sizes import NORM  # noqa: E402
 from paper_2307_15034_amd.layer import GroupNormAct  # noqa: E402
 
 
@@ -179,3 +180,29 @@ def test_long_sums_of_one_sign(points, batch, channels, groups, last, value):
     assert not gg.any()
     assert float((gb.double() - v * batch * points).abs().max()) <= (CHAIN + 2) * E * v * batch * points
     assert float(gx.abs().max()) <= (CHAIN + 4) * E * v
+
+
+@pytest.mark.parametrize("case", range(len(NORM)))
+def test_every_element_at_the_kernels_sizes(case):
+    """The sizes where kernels change, their odd ends and the ends of segments
+    and chunks, element by element."""
+    points, b, c, g, dt, last = NORM[case]
+    check_elements((points,), b, c, g, dt, ("gelu", "none", "silu")[case % 3], last, case % 2 == 0,
+                   seed=460 + case)
+
+
+@pytest.mark.parametrize("last", [False, True], ids=["first", "last"])
+@pytest.mark.parametrize("dt", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_every_element_of_the_shapes(case, dt, last):
+    grid, b, c, g = SHAPES[case]
+    check_elements(grid, b, c, g, dt, ("silu", "gelu", "none")[(case + len(dt) + last) % 3], last,
+                   case % 2 == 1, seed=500 + case)
+
+
+@pytest.mark.parametrize("points, channels, dt", [
+    (300001, 48, "fp16"), (2500003, 4, "fp16"), (1200005, 4, "fp32"), (70001, 20, "bf16")])
+@pytest.mark.parametrize("last", [False, True], ids=["first", "last"])
+def test_every_element_of_long_rows(points, channels, dt, last):
+    check_elements((points,), 1, channels, 1 if channels != 20 else 4, dt, "gelu", last, True,
+                   seed=520)
