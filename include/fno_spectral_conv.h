@@ -531,8 +531,9 @@ fno_status fno_grad_norm(const fno_adamw_desc *desc, const fno_adamw_tensor *ten
 
 /* One step.  control null: step number `step` (>= 1) with gradients as they
  * are (s = 1).  control (device memory) not null: the step number, s and skip
- * that fno_grad_norm left there; `step` is ignored.  `tensors` is read during
- * the call only.  count 0 does nothing. */
+ * that fno_grad_norm left there (each step needs a norm of its own before it: a
+ * block that none has filled holds no bias corrections); `step` is ignored.
+ * `tensors` is read during the call only.  count 0 does nothing. */
 fno_status fno_adamw_step(const fno_adamw_desc *desc, const fno_adamw_tensor *tensors,
                           int64_t count, int64_t step, const fno_adamw_control *control,
                           hipStream_t stream);

@@ -40,8 +40,9 @@ class AdamW:
 
     device_control: the step number, the clipped scale and the skip of
     non-finite gradients live on the GPU; each `step` then follows one
-    `clip_grads`, nothing is read by the host, and both can be captured in a
-    HIP graph.  Calls of one object belong on one stream (or on streams that
+    `clip_grads` (and is refused otherwise, unless clip_grads was captured:
+    its replays are not seen here), nothing is read by the host, and both can
+    be captured in a HIP graph.  Calls of one object belong on one stream (or on streams that
     wait for each other); what the object makes itself is filled when the
     constructor returns, so that any stream may take the first call.  The
     caller's tensors are the caller's: where `stream` is given, it has waited
@@ -100,6 +101,7 @@ class AdamW:
             *[self._list[i] for i in self._eight])
         self.set_grads(grads)
         self.control: Optional[torch.Tensor] = None
+        self._clipped = self._replayed = False  # a clip_grads awaits its step; one was captured
         if device_control:
             c = B.FnoAdamwControl(step=self.steps, lr_factor=1.0, grad_scale=1.0)
             self.control = torch.frombuffer(bytearray(bytes(c)), dtype=torch.uint8).to(self.device)
@@ -194,9 +196,15 @@ class AdamW:
             raise ValueError("clip_grads needs device_control=True")
         if not loss_scale > 0:
             raise ValueError(f"loss_scale {loss_scale}, expected more than 0")
+        s = self._on(stream)
         B.fno_grad_norm(self.desc, self._list, len(self.params), max_norm, 1.0 / loss_scale,
-                        self.control.data_ptr(), self._ws.data_ptr(), self._ws.numel(),
-                        self._on(stream))
+                        self.control.data_ptr(), self._ws.data_ptr(), self._ws.numel(), s)
+        self._clipped = True
+        if stream is None:
+            self._replayed |= torch.cuda.is_current_stream_capturing()
+        else:
+            with torch.cuda.stream(_external(self.device, s)):
+                self._replayed |= torch.cuda.is_current_stream_capturing()
         return self._norm
 
     def step(self, grads: Optional[Sequence[torch.Tensor]] = None, lr: Optional[float] = None,
@@ -207,11 +215,14 @@ class AdamW:
             if self.control is not None:
                 raise ValueError("set_grads before clip_grads: the clip reads the gradients")
             self.set_grads(grads)
+        if self.control is not None and not (self._clipped or self._replayed):
+            raise ValueError("with device_control every step follows a clip_grads of its own")
         if lr is not None:
             self.desc.lr = float(lr)
         s = self._on(stream)
         if self.control is not None:
             B.fno_adamw_step(self.desc, self._list, len(self.params), 0, self.control.data_ptr(), s)
+            self._clipped = False
         else:
             B.fno_adamw_step(self.desc, self._list, len(self.params), self.steps + 1, 0, s)
             self.steps += 1
