@@ -71,7 +71,7 @@ class AdamW:
                 raise ValueError(f"state_bits {b}, expected 32 or 8")
         if step < 0:
             raise ValueError(f"step {step}, expected at least 0")
-        self.steps = int(step)
+        self._steps = int(step)
         self.desc = B.FnoAdamwDesc(float(lr), float(betas[0]), float(betas[1]), float(eps))
         self.states: List[Dict[str, torch.Tensor]] = (
             [self._zero_state(p, b) for p, b in zip(self.params, self.state_bits)]
@@ -103,7 +103,7 @@ class AdamW:
         self.control: Optional[torch.Tensor] = None
         self._clipped = self._replayed = False  # a clip_grads awaits its step; one was captured
         if device_control:
-            c = B.FnoAdamwControl(step=self.steps, lr_factor=1.0, grad_scale=1.0)
+            c = B.FnoAdamwControl(step=self._steps, lr_factor=1.0, grad_scale=1.0)
             self.control = torch.frombuffer(bytearray(bytes(c)), dtype=torch.uint8).to(self.device)
             self._norm = self.control[32:36].view(torch.float32)[0]
             self._factor = self.control[44:48].view(torch.float32)
@@ -224,8 +224,15 @@ class AdamW:
             B.fno_adamw_step(self.desc, self._list, len(self.params), 0, self.control.data_ptr(), s)
             self._clipped = False
         else:
-            B.fno_adamw_step(self.desc, self._list, len(self.params), self.steps + 1, 0, s)
-            self.steps += 1
+            B.fno_adamw_step(self.desc, self._list, len(self.params), self._steps + 1, 0, s)
+            self._steps += 1
+
+    @property
+    def steps(self) -> int:
+        """Steps taken, those left out for gradients that are not finite not
+        among them (with device_control read from the device, behind the
+        current stream's work)."""
+        return self._steps if self.control is None else self.read_control()["step"]
 
     def set_lr_factor(self, factor: float) -> None:
         """Multiplies lr on the device (a schedule for captured steps), in the

@@ -52,3 +52,22 @@ def test_a_captured_clip_serves_every_step_behind_its_replays(given):
         ref.step()
         torch.cuda.synchronize()
         assert torch.equal(p, q) and opt.read_control() == ref.read_control()
+
+
+def test_steps_counts_in_both_ways():
+    """What a checkpoint keeps and a new object starts from."""
+    _, _, host = _opt(step=4)
+    _, d, dev = _opt(step=4, device_control=True)
+    assert (host.steps, dev.steps) == (4, 4)
+    for k in range(3):
+        host.step()
+        if k == 1:  # one that is left out
+            keep = d[7].clone()
+            d[7] = float("inf")
+            dev.clip_grads()
+            dev.step()
+            d[7] = keep
+        dev.clip_grads()
+        dev.step()
+    assert (host.steps, dev.steps) == (7, 7)
+    assert torch.equal(host.params[0], dev.params[0])
