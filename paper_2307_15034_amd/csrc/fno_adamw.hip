@@ -85,8 +85,7 @@ struct Vec4<__bf16> {
 };
 
 // Elements e .. e + 4 of an array of n (e a multiple of four): in one access
-// where all four are there, one by one at the tensor's end (others read as 0
-// and are not written).
+// where all four are there, one by one at the tensor's end (others read as 0).
 template <typename V, typename T>
 __device__ __forceinline__ V load4(const T* p, int64_t e, int64_t n) {
   if (e + 4 <= n) return *reinterpret_cast<const V*>(p + e);
@@ -95,16 +94,6 @@ __device__ __forceinline__ V load4(const T* p, int64_t e, int64_t n) {
   for (int j = 0; j < 4; ++j)
     if (e + j < n) v[j] = p[e + j];
   return v;
-}
-template <typename V, typename T>
-__device__ __forceinline__ void store4(T* p, int64_t e, int64_t n, const V& v) {
-  if (e + 4 <= n) {
-    *reinterpret_cast<V*>(p + e) = v;
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (e + j < n) p[e + j] = v[j];
 }
 
 // An fp32 result rounded to the storage type: two roundings, as stated.  (The
