@@ -219,7 +219,9 @@ __device__ __forceinline__ Sums team_sum(Sums v) {
 }
 
 // For each of `groups` groups the sum of its `n` entries entry(g, i), handed
-// to put(g, sum) by one thread; all threads of the work-group take part.
+// to put(g, sum) by one thread; all threads of the work-group take part.  Two
+// wait states behind a put, which may end in a 16-byte store and a branch: its
+// data registers are not written sooner, wherever the branch leads.
 template <int THREADS = NT, typename Entry, typename Put>
 __device__ __forceinline__ void group_sums(int groups, int n, Entry entry, Put put) {
   __shared__ Sums red[THREADS / 64];
@@ -234,7 +236,10 @@ __device__ __forceinline__ void group_sums(int groups, int n, Entry entry, Put p
       if (g < groups)
         for (int i = s; i < n; i += sub) v = add(v, entry(g, i));
       for (int d = sub / 2; d > 0; d >>= 1) v = add(v, Sums{__shfl_xor(v.s, d), __shfl_xor(v.q, d)});
-      if (g < groups && s == 0) put(g, v);
+      if (g < groups && s == 0) {
+        put(g, v);
+        asm volatile("s_nop 1" ::: "memory");
+      }
     }
     return;
   }
