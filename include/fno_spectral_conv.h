@@ -520,8 +520,8 @@ typedef struct {
  * into `control`, step += 1 and the new step's bias corrections (desc's beta1
  * and beta2); where the sum is not finite instead skip = 1 and skipped += 1,
  * and the fno_adamw_step that follows changes nothing.  max_norm > 0
- * (INFINITY: no clip), inv_loss_scale > 0 and finite.  The sum has a fixed
- * order: bit-identical from run to run. */
+ * (INFINITY: no clip), inv_loss_scale > 0 and at most 3.4e38 (grad_scale is
+ * fp32).  The sum has a fixed order: bit-identical from run to run. */
 fno_status fno_grad_norm_workspace_size(const fno_adamw_tensor *tensors, int64_t count,
                                         size_t *bytes);
 fno_status fno_grad_norm(const fno_adamw_desc *desc, const fno_adamw_tensor *tensors,

@@ -817,7 +817,7 @@ extern "C" fno_status fno_grad_norm(const fno_adamw_desc* d, const fno_adamw_ten
                                     fno_adamw_control* control, void* ws, size_t ws_len,
                                     hipStream_t stream) {
   if (!check_hyper(d) || !check_list(t, count) || !ok16(control)) return FNO_ERR_INVALID_ARGUMENT;
-  if (!(max_norm > 0.0) || !(inv_loss_scale > 0.0 && inv_loss_scale <= 1.7e308))
+  if (!(max_norm > 0.0) || !(inv_loss_scale > 0.0 && inv_loss_scale <= 3.4e38))
     return FNO_ERR_INVALID_ARGUMENT;
   for (int64_t i = 0; i < count; ++i)
     if (!check_grad(t[i])) return FNO_ERR_INVALID_ARGUMENT;
