@@ -109,6 +109,8 @@ class AdamW:
             self._factor = self.control[44:48].view(torch.float32)
             self._ws = torch.empty(B.fno_grad_norm_workspace_size(self._list, n),
                                    dtype=torch.uint8, device=self.device)
+            self._control_at = self.control.data_ptr()
+            self._ws_at, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
         # memory that torch handed out here, and the streams whose work it outlives
         self._made = [v for s in self.states for v in s.values()] if states is None else []
         if device_control:
@@ -198,7 +200,7 @@ class AdamW:
             raise ValueError(f"loss_scale {loss_scale}, expected more than 0")
         s = self._on(stream)
         B.fno_grad_norm(self.desc, self._list, len(self.params), max_norm, 1.0 / loss_scale,
-                        self.control.data_ptr(), self._ws.data_ptr(), self._ws.numel(), s)
+                        self._control_at, self._ws_at, self._ws_bytes, s)
         self._clipped = True
         if stream is None:
             self._replayed |= torch.cuda.is_current_stream_capturing()
@@ -221,7 +223,7 @@ class AdamW:
             self.desc.lr = float(lr)
         s = self._on(stream)
         if self.control is not None:
-            B.fno_adamw_step(self.desc, self._list, len(self.params), 0, self.control.data_ptr(), s)
+            B.fno_adamw_step(self.desc, self._list, len(self.params), 0, self._control_at, s)
             self._clipped = False
         else:
             B.fno_adamw_step(self.desc, self._list, len(self.params), self._steps + 1, 0, s)
