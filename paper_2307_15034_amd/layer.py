@@ -376,9 +376,13 @@ class GroupNormAct:
         memory at the first call, and kept from others until the work of every
         stream that used it is done."""
         if self._ws is None or self._ws.device != device:
-            with torch.cuda.stream(_external(device, s)):
-                self._ws = torch.empty(max(self.ws_bytes.values()), dtype=torch.uint8,
+            make = lambda: torch.empty(max(self.ws_bytes.values()), dtype=torch.uint8,  # noqa: E731
                                        device=device)
+            if s == torch.cuda.current_stream(device).cuda_stream:
+                self._ws = make()
+            else:
+                with torch.cuda.stream(_external(device, s)):
+                    self._ws = make()
             self._ws_stream = s
         elif s != self._ws_stream:
             self._ws.record_stream(_external(device, s))
