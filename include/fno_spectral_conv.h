@@ -391,7 +391,9 @@ fno_status fno_block_epilogue_bwd_data(const fno_block_desc *desc, const void *g
  * statistics [batch][groups][2] = (mean, 1 / sqrt(var + eps)).  Sums are
  * formed in at least fp32, the statistics joined in double, results rounded
  * once.  Every sum has a fixed order: results are bit-identical from run to
- * run.  A group that holds a non-finite value gives NaN throughout.
+ * run.  A group that holds a non-finite value gives NaN throughout; so does, in
+ * the backward behind an activation, the group of a channel whose gamma or beta
+ * is not finite.
  * ------------------------------------------------------------------------ */
 typedef enum { FNO_DTYPE_F32 = 0, FNO_DTYPE_F16 = 1, FNO_DTYPE_BF16 = 2 } fno_dtype;
 
@@ -459,7 +461,8 @@ fno_status fno_group_norm_act_bwd(const fno_norm_desc *desc, const void *x,
  *     m       = (A / 127^2) q |q|  int8 q,   A = max |m| of the block
  *     sqrt(v) = (B / 255^2) q^2    uint8 q,  B = max sqrt(v) of the block
  * rounded to nearest in the square root of the value, with q >= 1 wherever
- * v > 0: a second moment that is not zero does not become zero, so that the
+ * v > 0: a second moment that is not zero does not become zero (but where
+ * B < 2^-59, the square of whose smallest fraction leaves fp32), so that the
  * next step's quotient stays bounded.  The step itself uses the new moments
  * before they are rounded.  A block that holds a non-finite moment stands for
  * non-finite values throughout.

@@ -1,4 +1,5 @@
-// Pointwise activations shared by the block epilogue and the group norm.
+// Pointwise activations: GELU of the block epilogue, SiLU of the group norm
+// (whose GELU is chosen by the tensors' type, in fno_norm.h).
 #pragma once
 
 #include <hip/hip_runtime.h>

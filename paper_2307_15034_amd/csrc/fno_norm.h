@@ -259,9 +259,9 @@ __device__ __forceinline__ void group_sums(int groups, int n, Entry entry, Put p
   }
 }
 
-// x and x^2 added in double: nothing cancels however far a group's mean or a
-// few of its values lie from the rest, and the unit's double additions run at
-// the rate of float ones.
+// x and x^2 added in double: the variance loses (mean / sigma)^2 2^-53 of itself,
+// however far a group's mean or a few of its values lie from the rest, and the
+// unit's double additions run at the rate of float ones.
 __device__ __forceinline__ void add_value(Sums* t, float x) {
   const double d = (double)x;
   t->s += d;

@@ -25,11 +25,12 @@
 //     of channels (one channel where C is no multiple of a vector) down the rows;
 //   channels first:  a team of threads takes one plane or a segment of it.
 //
-// Bound by memory: 8 x 64 x 1024^2, fp16: sums 167 us (6.4 TB/s), results with a
-// residual 548 (6.1); the backward of 16 x 128 x 256^2, bf16: 102 and 138 (5.3
-// and 6.1).  Channels last 32 x 128^2 x 64, fp16: forward 13.6 + 27 us (5.0
-// TB/s), backward 34 + 36 (4.2 and 5.9), its sums as much by their arithmetic
-// (29% of a wave's time in vector operations, four waves to a unit).
+// Bound by memory: 8 x 64 x 1024^2, fp16: sums 165 us (6.5 TB/s), results with a
+// residual 542 (6.2); the backward of 16 x 128 x 256^2, bf16: 98 and 135 (5.5
+// and 6.2).  Channels last 32 x 128^2 x 64, fp16: forward 13 + 28 us (5.2 and
+// 4.9 TB/s), backward 34 + 36 (4.2 and 5.9), its sums as much by their arithmetic
+// (28% of a wave's time in vector operations, four work-groups to a unit, the
+// GELU body with two registers in scratch).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -360,6 +361,10 @@ __global__ __launch_bounds__(NT) void join_kernel(NormArgs a) {
 // --------------------------------------------------------------------------
 // Channels last, wide: a thread takes W channels down the rows of a chunk
 // --------------------------------------------------------------------------
+// Three to five times the bytes' time: one channel to a load where C is no
+// multiple of a vector (16 x 128^2 x 257, fp16: forward 190 us for 41, backward
+// 272 for 61), else registers for two work-groups a unit in the backward's sums
+// (8 x 64^2 x 4096: 231 for 81 and 420 for 122).
 struct Wide {
   int64_t b, chunk, at, rows;  // at: the element of the first row's channel c
   int c;                       // first channel (past the last: no work)
@@ -762,7 +767,9 @@ NormPlan plan_of(const fno_norm_desc& d, bool bwd) {
     // 232 and 248.  Longer ones where a group would have more than the 1024
     // entries that the second pass joins itself, unless work-groups are few
     // (the same planes in one group: 603 us with sixteen segments a plane, 635
-    // with 64 and a launch that joins them).
+    // with 64 and a launch that joins them).  Few or small planes leave compute
+    // units idle: 2 x 16 x 90^2 runs in eight work-groups, 15 us forward and 21
+    // backward, where a launch and its calls take 10.
     p.route = FIRST;
     p.team = a.P <= 64 * V * 16 ? 64 : NT;
     a.n1 = 1;

@@ -4,7 +4,9 @@
 // one launch (the backward of several samples adds one that joins the
 // parameter gradients).  Groups of at most 16384 elements: a thread holds 32
 // elements of each tensor in work-groups of 256, 16 in those of 1024 (half as many
-// where they come one by one), what the registers take without spills.
+// where they come one by one).  That fills the registers: the channels-last
+// backward of 1024 threads keeps 24 to 88 bytes a lane in scratch in 16 of its
+// bodies (64 samples of 2048 x 8, fp16: 14.8 us, their forward 10.4).
 //
 // channels first:  a plane of the group belongs to a team of waves (planes to
 //                  teams in turn, where there are more planes than waves);
