@@ -5,9 +5,9 @@
 // table to upload, nothing kept between calls): each work-group finds its
 // tensor by a search over the batch's first-chunk numbers and works on one
 // chunk of it.  The kernels stream every operand once; they are bound by HBM
-// (67 M fp16 weights with masters: step 300 us, 6.7 TB/s, norm 47, 5.7; with
-// 8-bit states 228, 5.4; read-out 59, 6.9; 268 M fp32 weights with 8-bit states
-// 789, 5.5, read-out 284, 5.8), small lists by the latency of a chain of loads
+// (67 M fp16 weights with masters: step 300 us, 6.7 TB/s, norm 46, 5.8; with
+// 8-bit states 228 to 251, 4.9 to 5.4; read-out 59, 6.9; 268 M fp32 weights with
+// 8-bit states 762 to 789, 5.5 to 5.7, read-out 265 to 287, 5.7 to 6.2), small lists by the latency of a chain of loads
 // (5 us a step, 6 to 7 the norm).
 #include <hip/hip_runtime.h>
 

@@ -26,9 +26,9 @@
 //   channels first:  a team of threads takes one plane or a segment of it.
 //
 // Bound by memory: 8 x 64 x 1024^2, fp16: sums 165 us (6.5 TB/s), results with a
-// residual 542 (6.2); the backward of 16 x 128 x 256^2, bf16: 98 and 135 (5.5
-// and 6.2).  Channels last 32 x 128^2 x 64, fp16: forward 13 + 28 us (5.2 and
-// 4.9 TB/s), backward 34 + 36 (4.2 and 5.9), its sums as much by their arithmetic
+// residual 542 (6.2); the backward of 16 x 128 x 256^2, bf16: 98 to 102 and
+// 135 to 142 (5.3 to 5.5, 5.9 to 6.2).  Channels last 32 x 128^2 x 64, fp16: forward 13 + 28 us (5.2 and
+// 4.9 TB/s), backward 35 + 36 (4.0 and 5.8), its sums as much by their arithmetic
 // (28% of a wave's time in vector operations, four work-groups to a unit, the
 // GELU body with two registers in scratch).
 #include <hip/hip_runtime.h>
