@@ -364,8 +364,10 @@ struct Coef {
 template <typename T>
 __device__ __forceinline__ Coef bwd_coef(const NormArgs& a, int64_t bg, int c) {
   const float mu = a.stats_in[2 * bg], rs = a.stats_in[2 * bg + 1];
-  // (of an r below the normal numbers: the smallest of these)
-  const float s = kNarrow<T> ? 1.0f : __uint_as_float(max(__float_as_uint(rs) & 0x7f800000u, 0x00800000u));
+  // (of an r below the normal numbers: the smallest of these; and mu s below 2^126,
+  // where values that hardly differ are as large as the type has them)
+  const uint32_t mask = 0x7f800000u, top = (379u << 23) - (__float_as_uint(mu) & mask);
+  const float s = kNarrow<T> ? 1.0f : __uint_as_float(min(max(__float_as_uint(rs) & mask, 0x00800000u), top));
   const float rel = kNarrow<T> ? rs : rs / s;
   const float ga = a.gamma ? a.gamma[c] : 1.0f;
   return Coef{mu * s, s, rs, rel, rel * ga, ga, a.beta ? a.beta[c] : 0.0f};

@@ -206,3 +206,34 @@ def test_every_element_of_the_shapes(case, dt, last):
 def test_every_element_of_long_rows(points, channels, dt, last):
     check_elements((points,), 1, channels, 1 if channels != 20 else 4, dt, "gelu", last, True,
                    seed=520)
+
+
+@pytest.mark.parametrize("value", [-1.0, 1.0], ids=["lowest", "largest"])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("dt", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("route", range(len(ROUTES)))
+def test_groups_of_the_types_extreme_value(route, dt, act, value):
+    """Every value of some groups is the lowest (largest) that the type, fp32
+    here bfloat16, has: the variance is zero exactly (the squares' sums are
+    exact), x - mean too, so the results are those of zeros, bit for bit.  With
+    half of a group there all results are finite."""
+    points, b, c, groups, last = ROUTES[route]
+    op = GroupNormAct((points,), b, c, groups, DT[dt], ACT[act], last, 1e-5)
+    x, ga, be, g, _ = _inputs(540 + route, (points,), b, c, dt, last)
+    v = value * torch.finfo(torch.bfloat16 if dt == "fp32" else DT[dt]).max
+    masked = x.clone()
+    part = slice(0, c // groups)
+    (x[..., part] if last else x[:, part]).zero_()
+    (masked[..., part] if last else masked[:, part]).fill_(v)
+    want, st = op.fwd(x, ga, be)
+    wx, wg, wb = op.bwd(x, g, st, ga, be)
+    got, st = op.fwd(masked, ga, be)
+    assert (st[:, 0, 0] == v).all()
+    gx, gg, gb = op.bwd(masked, g, st, ga, be)
+    for a, r in ((got, want), (gx, wx), (gg, wg), (gb, wb)):
+        assert torch.isfinite(r).all() and torch.equal(a, r)
+    half = masked.clone()
+    (half[:, ::2, part] if last else half[:, part, ::2]).zero_()
+    out, st = op.fwd(half, ga, be)
+    for t in (out, st) + op.bwd(half, g, st, ga, be):
+        assert torch.isfinite(t).all()
