@@ -549,6 +549,76 @@ fno_status fno_adamw_moments(const fno_adamw_tensor *tensors, int64_t count, fno
                              void *const *exp_avg_out, void *const *exp_avg_sq_out,
                              hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The norms around a block with its gate and residual scale, rows of `channels`
+ * values (a grid's points, channels last, or any other rows):
+ *
+ *     n = post_w norm(u) + post_b          u: the block's output
+ *     y = scale x + gate n                 x: the residual stream before it
+ *     h = pre_w norm(y) + pre_b            h: the next block's input
+ *
+ *     norm(v) = (v - mean) / sqrt(var + eps)     FNO_ROW_NORM_LAYER
+ *             = v / sqrt(mean(v^2) + eps)        FNO_ROW_NORM_RMS
+ *
+ * over the channels of each row, in one pass over the rows.  Without u it is
+ * the norm before the first block, h = pre_w norm(x) + pre_b; without h the
+ * join behind the last.  Rows x, u, y, h and their gradients are [rows][channels]
+ * of one type (dtype).  Parameters are fp32 [channels], null ones are 1
+ * (post_w, scale, pre_w) or 0 (post_b, pre_b).  The gate is [gate_rows][channels],
+ * fp32 or of the rows' type; gate_rows divides rows, and each of its rows serves
+ * rows / gate_rows consecutive rows: 1 (one gate for all), one per sample, or
+ * one per row.  gate_rows 0: no gate (1).
+ *
+ * Sums are fp32 chains of at most 128 additions, joined in double; every sum
+ * has a fixed order.  h is formed from y before its rounding.  A row with a
+ * value that is not finite, or beyond 2^126 in size, gives NaN throughout.
+ * ------------------------------------------------------------------------ */
+typedef enum { FNO_ROW_NORM_LAYER = 0, FNO_ROW_NORM_RMS = 1 } fno_row_norm;
+
+typedef struct {
+  int32_t dtype;       /* fno_dtype of the rows */
+  int32_t norm;        /* fno_row_norm */
+  int32_t gate_dtype;  /* FNO_DTYPE_F32 or dtype */
+  float eps;           /* >= 0, finite */
+  int64_t rows;        /* 1 .. 2^40, rows x channels up to 2^42 */
+  int64_t channels;    /* 1 .. 16384 */
+  int64_t gate_rows;   /* 0, or a divisor of rows */
+} fno_residual_norm_desc;
+
+typedef struct {
+  const float *post_w, *post_b;
+  const void *gate;  /* null if and only if gate_rows is 0 or there is no u */
+  const float *scale, *pre_w, *pre_b;
+} fno_residual_norm_params;
+
+/* Gradients of the parameters, each null (not wanted) or of its parameter's
+ * shape and type; overwritten, not accumulated. */
+typedef struct {
+  float *post_w, *post_b;
+  void *gate;
+  float *scale, *pre_w, *pre_b;
+} fno_residual_norm_grads;
+
+/* Forward.  u null: y, gate, scale, post_w, post_b are null too.  h null: pre_w
+ * and pre_b are null too.  y may be the buffer of x or u, h that of u. */
+fno_status fno_residual_norm_fwd(const fno_residual_norm_desc *desc,
+                                 const fno_residual_norm_params *params, const void *x,
+                                 const void *u, void *y, void *h, hipStream_t stream);
+
+/* Backward, from the gradients g_y of y (null: zeros) and g_h of h (null: there
+ * was no h), not both null:
+ *     G = g_y + (gradient of the second norm at y)(g_h),   g_x = scale G,
+ *     g_u = (gradient of the first norm at u)(gate G),
+ * and the parameters' gradients, sums over rows.  y (the forward's) is needed
+ * with g_h, x only for the scale's gradient.  Without u, x takes the place of y
+ * and g_u is null.  g_x may be the buffer of g_y or g_h, g_u that of u or g_h. */
+fno_status fno_residual_norm_workspace_size(const fno_residual_norm_desc *desc, size_t *bytes);
+fno_status fno_residual_norm_bwd(const fno_residual_norm_desc *desc,
+                                 const fno_residual_norm_params *params, const void *x,
+                                 const void *u, const void *y, const void *g_y, const void *g_h,
+                                 void *g_x, void *g_u, const fno_residual_norm_grads *grads,
+                                 void *ws, size_t ws_len, hipStream_t stream);
+
 /* Per-kernel timing with HIP events (a profiling aid, off by default).
  * While enabled, every kernel the library launches is bracketed by a pair of
  * HIP events recorded on the launch stream (events are created per launch, so

@@ -152,6 +152,28 @@ class FnoAdamwControl(ctypes.Structure):
     ]
 
 
+FNO_ROW_NORM_LAYER = 0
+FNO_ROW_NORM_RMS = 1
+
+
+class FnoResidualNormDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("norm", ctypes.c_int32),
+        ("gate_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("rows", ctypes.c_int64),
+        ("channels", ctypes.c_int64),
+        ("gate_rows", ctypes.c_int64),
+    ]
+
+
+class FnoResidualNormParams(ctypes.Structure):
+    """Layout of the parameters and, with the same names, of their gradients."""
+    _fields_ = [(k, ctypes.c_void_p)
+                for k in ("post_w", "post_b", "gate", "scale", "pre_w", "pre_b")]
+
+
 class FnoWeights(ctypes.Structure):
     _fields_ = [
         ("dense", ctypes.c_void_p),
@@ -186,6 +208,7 @@ def _load() -> ctypes.CDLL:
     BD = P(FnoBlockDesc)
     ND = P(FnoNormDesc)
     AT, f64 = P(FnoAdamwTensor), ctypes.c_double
+    RD, RP = P(FnoResidualNormDesc), P(FnoResidualNormParams)
     sig = {
         "fno_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "fno_last_error": (ctypes.c_char_p, []),
@@ -218,6 +241,10 @@ def _load() -> ctypes.CDLL:
         "fno_grad_norm": (ctypes.c_int, [P(FnoAdamwDesc), AT, i64, f64, f64, vp, vp, sz, vp]),
         "fno_adamw_step": (ctypes.c_int, [P(FnoAdamwDesc), AT, i64, i64, vp, vp]),
         "fno_adamw_moments": (ctypes.c_int, [AT, i64, ctypes.c_int, P(vp), P(vp), vp]),
+        "fno_residual_norm_workspace_size": (ctypes.c_int, [RD, P(sz)]),
+        "fno_residual_norm_fwd": (ctypes.c_int, [RD, RP, vp, vp, vp, vp, vp]),
+        "fno_residual_norm_bwd": (ctypes.c_int,
+                                  [RD, RP, vp, vp, vp, vp, vp, vp, vp, RP, vp, sz, vp]),
         "fno_release_caches": (ctypes.c_int, []),
         "fno_profile_enable": (ctypes.c_int, [i32]),
         "fno_profile_reset": (ctypes.c_int, []),
@@ -245,6 +272,7 @@ EXPORTED = [
     "fno_block_epilogue_bwd_weight", "fno_block_epilogue_bwd_data",
     "fno_group_norm_act_workspace_size", "fno_group_norm_act_fwd", "fno_group_norm_act_bwd",
     "fno_grad_norm_workspace_size", "fno_grad_norm", "fno_adamw_step", "fno_adamw_moments",
+    "fno_residual_norm_workspace_size", "fno_residual_norm_fwd", "fno_residual_norm_bwd",
 ]
 
 
@@ -515,6 +543,41 @@ def fno_adamw_moments(tensors, count: int, dtype: int, exp_avg_out, exp_avg_sq_o
                                 stream or None)
     if check:
         _check(st, "fno_adamw_moments")
+    return st
+
+
+def make_residual_norm_desc(rows: int, channels: int, gate_rows: int = 0,
+                            dtype: int = FNO_DTYPE_F16, norm: int = FNO_ROW_NORM_LAYER,
+                            gate_dtype: int = FNO_DTYPE_F32,
+                            eps: float = 1e-5) -> FnoResidualNormDesc:
+    return FnoResidualNormDesc(dtype, norm, gate_dtype, eps, rows, channels, gate_rows)
+
+
+def fno_residual_norm_workspace_size(desc: FnoResidualNormDesc) -> int:
+    b = ctypes.c_size_t()
+    _check(_lib.fno_residual_norm_workspace_size(ctypes.byref(desc), ctypes.byref(b)),
+           "fno_residual_norm_workspace_size")
+    return b.value
+
+
+def fno_residual_norm_fwd(desc, params: FnoResidualNormParams, x: int, u: int, y: int, h: int,
+                          stream: int, check: bool = True) -> int:
+    st = _lib.fno_residual_norm_fwd(ctypes.byref(desc), ctypes.byref(params), x or None,
+                                    u or None, y or None, h or None, stream or None)
+    if check:
+        _check(st, "fno_residual_norm_fwd")
+    return st
+
+
+def fno_residual_norm_bwd(desc, params: FnoResidualNormParams, x: int, u: int, y: int, g_y: int,
+                          g_h: int, g_x: int, g_u: int, grads: FnoResidualNormParams, ws: int,
+                          ws_bytes: int, stream: int, check: bool = True) -> int:
+    st = _lib.fno_residual_norm_bwd(ctypes.byref(desc), ctypes.byref(params), x or None,
+                                    u or None, y or None, g_y or None, g_h or None, g_x or None,
+                                    g_u or None, ctypes.byref(grads), ws or None, ws_bytes,
+                                    stream or None)
+    if check:
+        _check(st, "fno_residual_norm_bwd")
     return st
 
 

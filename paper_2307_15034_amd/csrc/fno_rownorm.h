@@ -1,0 +1,293 @@
+// What the kernels of the residual norm share: teams of threads that hold a
+// row, the rows' vectors and statistics, and the launches by type.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/fno_spectral_conv.h"
+
+namespace fno {
+
+// The sums of a backward's rows, in the order of the workspace.
+enum RowSum { RS_POST_W, RS_POST_B, RS_GATE, RS_SCALE, RS_PRE_W, RS_PRE_B, RS_COUNT };
+
+struct RowNormArgs {
+  const void *x, *u, *y_in, *g_y, *g_h;
+  void *y, *h, *g_x, *g_u;
+  const float *post_w, *post_b, *scale, *pre_w, *pre_b;
+  const void* gate;
+  void* g_gate;         // one gate per row: written by the rows' own threads
+  float* part;          // [units][sums][C]
+  int64_t rows;
+  int64_t per_gate;     // rows that a row of the gate serves
+  int64_t span;         // rows that units share: per_gate, or all with one gate per row
+  int64_t per_unit, units_per_gate;  // of a span
+  int C, nvec;
+  int layer;            // FNO_ROW_NORM_LAYER
+  int gate_f32;         // the gate is fp32 (else of the rows' type)
+  int slot[RS_COUNT];   // where a sum stands in `part`, -1: not wanted
+  int sums;
+  float eps;
+  float shrink, per_channel;  // 2^-p >= 1 / C, and 2^p / C
+  float inv_c;
+};
+
+// Threads of a team (a row's) and the vectors that each holds.  Teams of up to a
+// wave share work-groups of 256, larger ones are a work-group each.
+constexpr int row_threads(int team) { return team < 256 ? 256 : team; }
+
+hipError_t launch_row_norm_fwd(const RowNormArgs& a, int dtype, int team, int vecs, unsigned grid,
+                               hipStream_t s);
+hipError_t launch_row_norm_bwd(const RowNormArgs& a, int dtype, bool post, bool pre, int team,
+                               int vecs, unsigned grid, hipStream_t s);
+
+// --------------------------------------------------------------------------
+// Device code
+// --------------------------------------------------------------------------
+template <typename T>
+constexpr int kRowVec = 16 / (int)sizeof(T);
+
+template <typename T>
+struct RowVec {
+  T e[kRowVec<T>];
+};
+
+// Vector v of a row of C values at `row`; zeros behind the row's end and where
+// `on` is false.  Rows start at any element.
+template <typename T>
+__device__ __forceinline__ RowVec<T> load_row_vec(const T* row, int v, int C, bool on) {
+  constexpr int V = kRowVec<T>;
+  RowVec<T> r;
+  if (on && (v + 1) * V <= C) {
+    __builtin_memcpy(&r, __builtin_assume_aligned(row + v * V, sizeof(T)), sizeof(r));
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      r.e[j] = (T)0.0f;
+      if (on && v * V + j < C) r.e[j] = row[v * V + j];
+    }
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_row_vec(T* row, int v, int C, const RowVec<T>& r) {
+  constexpr int V = kRowVec<T>;
+  if ((v + 1) * V <= C) {
+    __builtin_memcpy(__builtin_assume_aligned(row + v * V, sizeof(T)), &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (v * V + j < C) row[v * V + j] = r.e[j];
+  }
+}
+// The same of fp32 parameters (V values from channel v V on); `other` where
+// there are none, zeros behind the row's end (what is multiplied by them there
+// leaves no trace in the row's sums).
+template <int V>
+__device__ __forceinline__ void load_param(float (&out)[V], const float* p, int v, int C,
+                                           float other) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) out[j] = v * V + j < C ? (p ? p[v * V + j] : other) : 0.0f;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// Sums over N consecutive lanes (a power of two up to 64), in all of them.  Lane
+// permutations of the vector unit: each step adds the neighbour at distance 1, 2,
+// then mirrors (equal lanes by then) of 8 and 16, then rows and halves swapped.
+template <int N>
+__device__ __forceinline__ float lane_sum(float v) {
+  if constexpr (N >= 2) v += dpp<0xB1>(v);
+  if constexpr (N >= 4) v += dpp<0x4E>(v);
+  if constexpr (N >= 8) v += dpp<0x141>(v);
+  if constexpr (N >= 16) v += dpp<0x140>(v);
+  if constexpr (N >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v),
+                                                    __builtin_bit_cast(unsigned, v), false, false);
+    v = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+  }
+  if constexpr (N >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v),
+                                                    __builtin_bit_cast(unsigned, v), false, false);
+    v = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+  }
+  return v;
+}
+
+// Sums over a team.  A team of several waves is a whole work-group, all of whose
+// threads call with the same number of values; two buffers taken in turn need
+// one barrier a call.
+template <int TEAM>
+struct Team {
+  int turn = 0;
+  template <int K>
+  __device__ __forceinline__ void sum(float (&v)[K]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = lane_sum<(TEAM < 64 ? TEAM : 64)>(v[k]);
+    if constexpr (TEAM > 64) {
+      constexpr int W = TEAM / 64;
+      __shared__ float red[2][4][W];
+      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+      if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) red[turn][k][wave] = v[k];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] = lane_sum<W>(red[turn][k][lane & (W - 1)]);
+      turn ^= 1;
+    }
+  }
+};
+
+struct RowStat {
+  float mean, r;
+};
+
+// Means and 1 / sqrt(var + eps) of K rows at once (v[k]: a thread's values,
+// `valid` of each vector's are the row's).  The mean is of values scaled by a
+// power of two, whose sum stays within fp32; the squares are of distances from
+// it.  Where their sum leaves what fp32 holds exactly enough (rows far larger
+// than 2^45, or as small as eps = 0 would need), they are formed again at
+// another power of two.
+template <int K, int VPT, int V, int TEAM>
+__device__ __forceinline__ void row_stats(Team<TEAM>& team, const float (&v)[K][VPT][V],
+                                          const int (&valid)[VPT], const RowNormArgs& a,
+                                          RowStat (&st)[K]) {
+  float s[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) s[k] = 0.0f;
+  if (a.layer) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[k] = __builtin_fmaf(v[k][i][j], a.shrink, s[k]);
+    team.template sum<K>(s);
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) st[k].mean = s[k] * a.per_channel;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    s[k] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float d = j < valid[i] ? v[k][i][j] - st[k].mean : 0.0f;
+        s[k] = __builtin_fmaf(d, d, s[k]);
+      }
+  }
+  team.template sum<K>(s);
+  bool odd = false;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    st[k].r = __builtin_amdgcn_rsqf(__builtin_fmaf(s[k], a.inv_c, a.eps));
+    odd |= !(s[k] < 0x1p120f) || (s[k] < 0x1p-70f && a.eps < 0x1p-90f);
+  }
+  if (odd) {  // the same for all threads of the team
+    float q[2 * K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      q[2 * k] = q[2 * k + 1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float d = j < valid[i] ? v[k][i][j] - st[k].mean : 0.0f;
+          const float lo = d * 0x1p-72f, hi = d * 0x1p72f;
+          q[2 * k] = __builtin_fmaf(lo, lo, q[2 * k]);
+          q[2 * k + 1] = __builtin_fmaf(hi, hi, q[2 * k + 1]);
+        }
+    }
+    team.template sum<2 * K>(q);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!(s[k] < 0x1p120f)) {
+        const float big = q[2 * k] * a.inv_c;
+        st[k].r = big < 0x1p127f
+                      ? __builtin_amdgcn_rsqf(__builtin_fmaf(a.eps, 0x1p-144f, big)) * 0x1p-72f
+                      : __builtin_nanf("");  // a value that is not finite
+      }
+      if (s[k] < 0x1p-70f && a.eps < 0x1p-90f)
+        st[k].r = (float)(1.0 / sqrt((double)q[2 * k + 1] * a.inv_c * 0x1p-144 + (double)a.eps));
+    }
+  }
+}
+
+// Everything of a thread that does not change from row to row.
+template <typename T, int TEAM, int VPT>
+struct RowPlace {
+  int vec[VPT], valid[VPT];
+  __device__ __forceinline__ explicit RowPlace(const RowNormArgs& a) {
+    constexpr int V = kRowVec<T>;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      vec[i] = (int)(threadIdx.x % TEAM) + i * TEAM;
+      const int left = a.C - vec[i] * V;
+      valid[i] = left < 0 ? 0 : left > V ? V : left;
+    }
+  }
+};
+
+template <typename T, int VPT>
+__device__ __forceinline__ void load_row(float (&out)[VPT][kRowVec<T>], const void* base,
+                                         int64_t at, const int (&vec)[VPT],
+                                         const int (&valid)[VPT], int C) {
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const RowVec<T> r = load_row_vec<T>(static_cast<const T*>(base) + at, vec[i], C, valid[i] > 0);
+#pragma unroll
+    for (int j = 0; j < kRowVec<T>; ++j) out[i][j] = (float)r.e[j];
+  }
+}
+template <typename T, int VPT>
+__device__ __forceinline__ void store_row(void* base, int64_t at, const int (&vec)[VPT],
+                                          const int (&valid)[VPT], int C,
+                                          const float (&v)[VPT][kRowVec<T>]) {
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+    if (valid[i] > 0) {
+      RowVec<T> r;
+#pragma unroll
+      for (int j = 0; j < kRowVec<T>; ++j) r.e[j] = (T)v[i][j];
+      store_row_vec<T>(static_cast<T*>(base) + at, vec[i], C, r);
+    }
+}
+// A row's gate (1 without one).
+template <typename T, int VPT>
+__device__ __forceinline__ void load_gate(float (&out)[VPT][kRowVec<T>], const RowNormArgs& a,
+                                          int64_t row, const int (&vec)[VPT],
+                                          const int (&valid)[VPT]) {
+  constexpr int V = kRowVec<T>;
+  if (!a.gate) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) out[i][j] = 1.0f;
+    return;
+  }
+  const int64_t at = (a.per_gate == 1 ? row : row / a.per_gate) * a.C;
+  if (a.gate_f32) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) {
+        const int v = vec[i] * (V / 4) + q;
+        const RowVec<float> r = load_row_vec<float>(static_cast<const float*>(a.gate) + at, v, a.C,
+                                                    valid[i] > 4 * q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[i][4 * q + j] = r.e[j];
+      }
+  } else {
+    load_row<T, VPT>(out, a.gate, at, vec, valid, a.C);
+  }
+}
+
+}  // namespace fno

@@ -1,0 +1,237 @@
+// Residual norm, backward.  With xh the normalised row, r = 1 / sqrt(var + eps)
+// and t = w g the gradient of xh, a norm's gradient is
+//     r (t - mean(t) - xh mean(t xh))     (LAYER; without mean(t): RMS).
+// Both rows' statistics are formed again from the rows, which a team of threads
+// holds whole; the parameters' sums stay in registers over a unit's rows and
+// leave as one partial row a unit.
+#include "fno_rownorm.h"
+
+namespace fno {
+namespace {
+
+template <int VPT, int V, int TEAM>
+__device__ __forceinline__ void norm_grad(Team<TEAM>& team, const float (&t)[VPT][V],
+                                          const float (&xh)[VPT][V], const RowNormArgs& a, float r,
+                                          float (&out)[VPT][V]) {
+  float s[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      s[0] += t[i][j];
+      s[1] = __builtin_fmaf(t[i][j], xh[i][j], s[1]);
+    }
+  team.template sum<2>(s);
+  const float m = a.layer ? s[0] * a.inv_c : 0.0f, q = s[1] * a.inv_c;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) out[i][j] = r * __builtin_fmaf(-xh[i][j], q, t[i][j] - m);
+}
+
+// Adds a sum over the work-group's teams and writes it to `part`.
+template <int TEAM, int VPT, int V>
+__device__ __forceinline__ void write_sums(const RowNormArgs& a, int which, float (&v)[VPT][V],
+                                           const int (&vec)[VPT], float* lds) {
+  const int slot = a.slot[which];
+  if (slot < 0) return;
+  float* out = a.part + ((int64_t)blockIdx.x * a.sums + slot) * a.C;
+  if constexpr (TEAM > 64) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (vec[i] * V + j < a.C) out[vec[i] * V + j] = v[i][j];
+  } else {
+    constexpr int WAVES = row_threads(TEAM) / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int d = TEAM; d < 64; d *= 2) v[i][j] += __shfl_xor(v[i][j], d);
+    __syncthreads();
+    if (lane < TEAM) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) lds[wave * (TEAM * VPT * V) + vec[i] * V + j] = v[i][j];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.C; c += row_threads(TEAM)) {
+      float s = lds[c];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) s += lds[w * (TEAM * VPT * V) + c];
+      out[c] = s;
+    }
+  }
+}
+
+template <typename T, int TEAM, int VPT, bool POST, bool PRE>
+__global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNormArgs a) {
+  constexpr int V = kRowVec<T>, SLOTS = row_threads(TEAM) / TEAM;
+  constexpr int K = (POST ? 1 : 0) + (PRE ? 1 : 0);  // rows with statistics
+  __shared__ float lds[TEAM > 64 ? 1 : row_threads(TEAM) / 64 * TEAM * VPT * V];
+  const RowPlace<T, TEAM, VPT> at(a);
+  float post_w[VPT][V], post_b[VPT][V], scale[VPT][V], pre_w[VPT][V];
+  float sums[RS_COUNT][VPT][V];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    if constexpr (POST) {
+      load_param<V>(post_w[i], a.post_w, at.vec[i], a.C, 1.0f);
+      load_param<V>(post_b[i], a.post_b, at.vec[i], a.C, 0.0f);
+      load_param<V>(scale[i], a.scale, at.vec[i], a.C, 1.0f);
+    }
+    if constexpr (PRE) load_param<V>(pre_w[i], a.pre_w, at.vec[i], a.C, 1.0f);
+#pragma unroll
+    for (int q = 0; q < RS_COUNT; ++q)
+#pragma unroll
+      for (int j = 0; j < V; ++j) sums[q][i][j] = 0.0f;
+  }
+  Team<TEAM> team;
+  // the unit's rows: a piece of one span
+  const int64_t g = (int64_t)blockIdx.x / a.units_per_gate;
+  const int64_t first = g * a.span + ((int64_t)blockIdx.x - g * a.units_per_gate) * a.per_unit;
+  const int64_t end = first + a.per_unit < (g + 1) * a.span ? first + a.per_unit : (g + 1) * a.span;
+  for (int64_t row = first + threadIdx.x / TEAM; row < end; row += SLOTS) {
+    const int64_t start = row * a.C;
+    float v[K][VPT][V], G[VPT][V], t[VPT][V], xh[VPT][V];
+    RowStat st[K];
+    if constexpr (POST) load_row<T, VPT>(v[0], a.u, start, at.vec, at.valid, a.C);
+    if constexpr (PRE) {
+      load_row<T, VPT>(v[K - 1], a.y_in, start, at.vec, at.valid, a.C);
+      load_row<T, VPT>(t, a.g_h, start, at.vec, at.valid, a.C);
+    }
+    if (a.g_y) {
+      load_row<T, VPT>(G, a.g_y, start, at.vec, at.valid, a.C);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) G[i][j] = 0.0f;
+    }
+    row_stats<K, VPT, V, TEAM>(team, v, at.valid, a, st);
+    if constexpr (PRE) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          xh[i][j] = (v[K - 1][i][j] - st[K - 1].mean) * st[K - 1].r;
+          sums[RS_PRE_W][i][j] = __builtin_fmaf(t[i][j], xh[i][j], sums[RS_PRE_W][i][j]);
+          sums[RS_PRE_B][i][j] += t[i][j];
+          t[i][j] *= pre_w[i][j];
+        }
+      float d[VPT][V];
+      norm_grad<VPT, V, TEAM>(team, t, xh, a, st[K - 1].r, d);
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) G[i][j] += d[i][j];
+    }
+    if constexpr (POST) {
+      if (a.slot[RS_SCALE] >= 0) {
+        float x[VPT][V];
+        load_row<T, VPT>(x, a.x, start, at.vec, at.valid, a.C);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            sums[RS_SCALE][i][j] = __builtin_fmaf(G[i][j], x[i][j], sums[RS_SCALE][i][j]);
+      }
+      float gate[VPT][V];
+      load_gate<T, VPT>(gate, a, row, at.vec, at.valid);
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          xh[i][j] = (v[0][i][j] - st[0].mean) * st[0].r;
+          t[i][j] = G[i][j] * __builtin_fmaf(xh[i][j], post_w[i][j], post_b[i][j]);
+          sums[RS_GATE][i][j] += t[i][j];
+        }
+      if (a.g_gate) {
+        if (a.gate_f32) {
+#pragma unroll
+          for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) {
+              RowVec<float> r;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) r.e[j] = t[i][4 * q + j];
+              if (at.valid[i] > 4 * q)
+                store_row_vec<float>(static_cast<float*>(a.g_gate) + start, at.vec[i] * (V / 4) + q, a.C, r);
+            }
+        } else {
+          store_row<T, VPT>(a.g_gate, start, at.vec, at.valid, a.C, t);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          t[i][j] = G[i][j] * gate[i][j];
+          G[i][j] *= scale[i][j];
+          sums[RS_POST_W][i][j] = __builtin_fmaf(t[i][j], xh[i][j], sums[RS_POST_W][i][j]);
+          sums[RS_POST_B][i][j] += t[i][j];
+          t[i][j] *= post_w[i][j];
+        }
+      float d[VPT][V];
+      norm_grad<VPT, V, TEAM>(team, t, xh, a, st[0].r, d);
+      store_row<T, VPT>(a.g_u, start, at.vec, at.valid, a.C, d);
+    }
+    store_row<T, VPT>(a.g_x, start, at.vec, at.valid, a.C, G);
+  }
+  if (a.sums) {
+    if constexpr (POST) {
+      write_sums<TEAM, VPT, V>(a, RS_POST_W, sums[RS_POST_W], at.vec, lds);
+      write_sums<TEAM, VPT, V>(a, RS_POST_B, sums[RS_POST_B], at.vec, lds);
+      write_sums<TEAM, VPT, V>(a, RS_GATE, sums[RS_GATE], at.vec, lds);
+      write_sums<TEAM, VPT, V>(a, RS_SCALE, sums[RS_SCALE], at.vec, lds);
+    }
+    if constexpr (PRE) {
+      write_sums<TEAM, VPT, V>(a, RS_PRE_W, sums[RS_PRE_W], at.vec, lds);
+      write_sums<TEAM, VPT, V>(a, RS_PRE_B, sums[RS_PRE_B], at.vec, lds);
+    }
+  }
+}
+
+template <typename T, bool POST, bool PRE>
+hipError_t launch_of(const RowNormArgs& a, int team, int vecs, unsigned grid, hipStream_t s) {
+#define FNO_ROW(T_, V_)                                                                          \
+  if (team == T_ && vecs == V_) {                                                                \
+    row_norm_bwd_kernel<T, T_, V_, POST, PRE><<<dim3(grid), dim3(row_threads(T_)), 0, s>>>(a);   \
+    return hipGetLastError();                                                                    \
+  }
+  FNO_ROW(4, 1)
+  FNO_ROW(8, 1)
+  FNO_ROW(16, 1)
+  FNO_ROW(32, 1)
+  FNO_ROW(64, 1)
+  FNO_ROW(64, 2)
+  FNO_ROW(256, 1)
+  FNO_ROW(256, 2)
+  FNO_ROW(512, 2)
+  FNO_ROW(1024, 2)
+  FNO_ROW(1024, 4)
+#undef FNO_ROW
+  return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t launch_form(const RowNormArgs& a, bool post, bool pre, int team, int vecs, unsigned grid,
+                       hipStream_t s) {
+  if (post && pre) return launch_of<T, true, true>(a, team, vecs, grid, s);
+  if (post) return launch_of<T, true, false>(a, team, vecs, grid, s);
+  return launch_of<T, false, true>(a, team, vecs, grid, s);
+}
+
+}  // namespace
+
+hipError_t launch_row_norm_bwd(const RowNormArgs& a, int dtype, bool post, bool pre, int team,
+                               int vecs, unsigned grid, hipStream_t s) {
+  if (dtype == FNO_DTYPE_F32) return launch_form<float>(a, post, pre, team, vecs, grid, s);
+  if (dtype == FNO_DTYPE_F16) return launch_form<_Float16>(a, post, pre, team, vecs, grid, s);
+  return launch_form<__bf16>(a, post, pre, team, vecs, grid, s);
+}
+
+}  // namespace fno

@@ -455,3 +455,183 @@ class GroupNormAct:
         B.fno_group_norm_act_bwd(self.desc, ax, ag, ab, ast, ago, agx, agg, agb,
                                  *self._workspace(dev, s), s)
         return gx, g_gamma, g_beta
+
+
+class _Workspace:
+    """Scratch memory that an object keeps: taken from the memory of the first
+    call's stream, taken anew where a call needs more or runs on another device,
+    and kept from others until the work of every stream that used it is done."""
+
+    def __init__(self):
+        self._t: Optional[torch.Tensor] = None
+        self._stream = 0
+
+    def get(self, nbytes: int, device: torch.device, s: int):
+        """(address, bytes) for a call on stream `s`."""
+        t = self._t
+        if t is None or t.device != device or t.numel() < nbytes:
+            if s == torch.cuda.current_stream(device).cuda_stream:
+                t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            else:
+                with torch.cuda.stream(_external(device, s)):
+                    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            self._t, self._stream = t, s
+        elif s != self._stream:
+            t.record_stream(_external(device, s))
+        return t.data_ptr(), t.numel()
+
+
+class ResidualNorm:
+    """The norms around a block with its gate and residual scale (the
+    fno_residual_norm_* calls):
+
+        y = scale x + gate (post_w norm(u) + post_b),   h = pre_w norm(y) + pre_b
+
+    u is the block's output, x the residual stream before it, y the stream behind
+    it and h the next block's input; norm is over the channels of each row, with
+    (FNO_ROW_NORM_LAYER) or without (FNO_ROW_NORM_RMS) its mean.  Without u: h =
+    pre_w norm(x) + pre_b; with pre=False: y alone.
+
+    Rows x, u, y, h and their gradients are [..., channels], `rows` of them, of
+    `dtype` (float32, float16 or bfloat16): a grid's points with channels last.
+    Parameters are float32 [channels] (None: 1 for post_w, scale and pre_w, 0 for
+    post_b and pre_b).  The gate is [gate_rows, channels], float32 or of `dtype`,
+    gate_rows a divisor of rows: [1, C] for all rows, [batch, C] per sample,
+    [rows, C] per row (None: 1).
+
+    The backward keeps one workspace, memory of the first call's stream, so an
+    object's backward calls belong on one stream (or on streams that wait for
+    each other).  Where `stream` is given, outputs are the caller's too.
+    """
+
+    PARAMS = ("post_w", "post_b", "gate", "scale", "pre_w", "pre_b")
+
+    def __init__(self, rows: int, channels: int, dtype: torch.dtype = torch.float16,
+                 norm: int = B.FNO_ROW_NORM_LAYER, eps: float = 1e-5, device: str = "cuda"):
+        if dtype not in DTYPE_CODES:
+            raise ValueError(f"dtype {dtype}, expected float32, float16 or bfloat16")
+        self.rows, self.channels = int(rows), int(channels)
+        self.dtype, self.norm, self.eps = dtype, norm, float(eps)
+        self.device = torch.device(device)
+        self._descs: Dict[tuple, tuple] = {}
+        self._ws = _Workspace()
+        self._desc(0, torch.float32)  # descriptor checks run in the library
+
+    def _desc(self, gate_rows: int, gate_dtype: torch.dtype):
+        """(descriptor, workspace bytes) with a gate of so many rows."""
+        key = (gate_rows, gate_dtype)
+        if key not in self._descs:
+            d = B.make_residual_norm_desc(self.rows, self.channels, gate_rows,
+                                          DTYPE_CODES[self.dtype], self.norm,
+                                          DTYPE_CODES[gate_dtype], self.eps)
+            self._descs[key] = (d, B.fno_residual_norm_workspace_size(d))
+        return self._descs[key]
+
+    def _t(self, t, name, device):
+        """Address of rows [..., channels]."""
+        if t is None:
+            return 0
+        a = _addr(t, None, self.dtype, name, device)
+        if t.dim() < 1 or t.shape[-1] != self.channels or t.numel() != self.rows * self.channels:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [..., {self.channels}] "
+                             f"with {self.rows} rows")
+        return a
+
+    def _params(self, p, device):
+        s = B.FnoResidualNormParams()
+        for k, t in p.items():
+            if t is not None and k != "gate":
+                setattr(s, k, _addr(t, (self.channels,), torch.float32, k, device))
+        gate = p["gate"]
+        if gate is None:
+            return s, self._desc(0, torch.float32)
+        if gate.dtype not in (torch.float32, self.dtype):
+            raise ValueError(f"gate: dtype {gate.dtype}, expected float32 or {self.dtype}")
+        if gate.dim() != 2 or gate.shape[1] != self.channels or not 0 < gate.shape[0] <= self.rows \
+                or self.rows % gate.shape[0]:
+            raise ValueError(f"gate: shape {tuple(gate.shape)}, expected [gate_rows, "
+                             f"{self.channels}], gate_rows a divisor of {self.rows}")
+        s.gate = _addr(gate, None, None, "gate", device)
+        return s, self._desc(gate.shape[0], gate.dtype)
+
+    @staticmethod
+    def _new(like, stream, name):
+        GroupNormAct._given(stream, name)
+        return torch.empty_like(like)
+
+    def fwd(self, x, u=None, post_w=None, post_b=None, gate=None, scale=None, pre_w=None,
+            pre_b=None, pre: bool = True, y=None, h=None, stream: Optional[int] = None):
+        """Returns (y, h); y is x itself without u, h is None with pre=False.
+        y may be x or u, h may be u (in place)."""
+        if x is None:
+            raise ValueError("x is required")
+        if u is None and (y is not None or not pre):
+            raise ValueError("without u there is no y, and h is what is formed")
+        if not pre and h is not None:
+            raise ValueError("h is given, but pre is False")
+        ax, dev = self._t(x, "x", self.device), x.device
+        au, ay, ah = self._t(u, "u", dev), self._t(y, "y", dev), self._t(h, "h", dev)
+        par, (desc, _) = self._params(dict(post_w=post_w, post_b=post_b, gate=gate, scale=scale,
+                                           pre_w=pre_w, pre_b=pre_b), dev)
+        s = _stream_of(dev, stream)
+        if u is not None and y is None:
+            y = self._new(x, stream, "y")
+            ay = y.data_ptr()
+        if pre and h is None:
+            h = self._new(x, stream, "h")
+            ah = h.data_ptr()
+        B.fno_residual_norm_fwd(desc, par, ax, au, ay, ah, s)
+        return (x if u is None else y), h
+
+    def bwd(self, g_y, g_h=None, x=None, u=None, y=None, post_w=None, post_b=None, gate=None,
+            scale=None, pre_w=None, pre_b=None, out: Optional[Dict[str, torch.Tensor]] = None,
+            stream: Optional[int] = None) -> Dict[str, Optional[torch.Tensor]]:
+        """The gradients {"g_x", "g_u", "g_post_w", ...}: of the rows and of every
+        parameter that is given (None for the others).  g_y and g_h are the
+        gradients of y and h (None: zeros, and no h; not both).  y is the forward's,
+        needed with g_h and u; x is needed with `scale` and where there is no u.
+        `out` may hold tensors to write to, by the same names; its g_x may be g_y or
+        g_h, its g_u may be u or g_h."""
+        first = next((t for t in (g_y, g_h) if t is not None), None)
+        if first is None:
+            raise ValueError("g_y or g_h is required")
+        if u is None and (x is None or g_h is None):
+            raise ValueError("without u, x and g_h are required")
+        if u is not None and g_h is not None and y is None:
+            raise ValueError("y is required")
+        if u is not None and scale is not None and x is None:
+            raise ValueError("x is required for the scale's gradient")
+        out = {} if out is None else out
+        params = dict(post_w=post_w, post_b=post_b, gate=gate, scale=scale, pre_w=pre_w,
+                      pre_b=pre_b)
+        unknown = set(out) - {"g_x", "g_u"} - {"g_" + k for k, t in params.items() if t is not None}
+        if unknown or (u is None and "g_u" in out):
+            raise ValueError(f"out: nothing to write to {sorted(unknown) or ['g_u']}")
+        self._t(first, "g_y" if g_y is not None else "g_h", self.device)
+        dev = first.device
+        ax, au, ay = self._t(x, "x", dev), self._t(u, "u", dev), self._t(y, "y", dev)
+        agy, agh = self._t(g_y, "g_y", dev), self._t(g_h, "g_h", dev)
+        par, (desc, nbytes) = self._params(params, dev)
+        got: Dict[str, Optional[torch.Tensor]] = {}
+        grads = B.FnoResidualNormParams()
+        for k, t in params.items():  # checked whole before anything is allocated
+            if out.get("g_" + k) is not None:
+                _addr(out["g_" + k], t.shape, t.dtype, "g_" + k, dev)
+        agx, agu = self._t(out.get("g_x"), "g_x", dev), self._t(out.get("g_u"), "g_u", dev)
+        s = _stream_of(dev, stream)
+        for k, like in (("g_x", first), ("g_u", u)):
+            got[k] = out.get(k)
+            if got[k] is None and like is not None:
+                got[k] = self._new(like, stream, k)
+        for k, t in params.items():
+            g = out.get("g_" + k)
+            if g is None and t is not None:
+                g = self._new(t, stream, "g_" + k)
+            got["g_" + k] = g
+            if g is not None:
+                setattr(grads, k, g.data_ptr())
+        ws = self._ws.get(nbytes, dev, s)
+        B.fno_residual_norm_bwd(desc, par, ax, au, ay if u is not None else 0, agy, agh,
+                                got["g_x"].data_ptr(), got["g_u"].data_ptr() if u is not None else 0,
+                                grads, *ws, s)
+        return got
