@@ -619,6 +619,67 @@ fno_status fno_residual_norm_bwd(const fno_residual_norm_desc *desc,
                                  void *g_x, void *g_u, const fno_residual_norm_grads *grads,
                                  void *ws, size_t ws_len, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Products in 8-bit floating point with a scale for each block of 128.
+ *
+ * A matrix [rows][cols] is held as codes of e4m3 (largest value 448, no
+ * infinity) or e5m2 (57344), one byte each, rows of fno_fp8_pitch(cols) =
+ * cols rounded up to 16 codes (zeros behind cols), and one scale for each block:
+ *     FNO_BLOCKS_ROW   128 consecutive columns of one row: [ceil(cols/128)][rows]
+ *     FNO_BLOCKS_TILE  128 x 128:           [ceil(cols/128)][ceil(rows/128)]
+ * (the last blocks may be short).  A value is its code times its block's scale.
+ * Scales are powers of two held in one byte, 2^(byte - 127) (FNO_SCALE_POW2; 255
+ * stands for NaN), or fp32 numbers (FNO_SCALE_F32).
+ * ------------------------------------------------------------------------ */
+#define FNO_FP8_BLOCK 128
+typedef enum { FNO_FP8_E4M3 = 0, FNO_FP8_E5M2 = 1 } fno_fp8_format;
+typedef enum { FNO_SCALE_POW2 = 0, FNO_SCALE_F32 = 1 } fno_scale_type;
+typedef enum { FNO_BLOCKS_ROW = 0, FNO_BLOCKS_TILE = 1 } fno_fp8_blocks;
+
+typedef struct {
+  int32_t dtype;       /* fno_dtype of x */
+  int32_t format;      /* fno_fp8_format of the codes */
+  int32_t scale_type;  /* fno_scale_type */
+  int32_t blocks;      /* fno_fp8_blocks */
+  int32_t activation;  /* fno_norm_activation */
+  int64_t rows, cols;  /* >= 1, each up to 2^31 - 1; rows x cols up to 2^40 */
+} fno_fp8_quantize_desc;
+
+/* x [rows][cols] to the codes of v = act(x): `codes` [rows][pitch(cols)] with
+ * blocks along its rows (or tiles), and `codes_t`, those of the transpose
+ * [cols][pitch(rows)] with blocks along its own rows (the columns of x).
+ * Either pair of codes and scales may be null.  With F the format's largest
+ * value and a the largest size of a block's finite values, the scale is
+ *     POW2   2^max(e, -126), e the least with a <= F 2^e;  F32  max(a / F, 2^-126);
+ * 1 where a = 0; the code is v times the scale's reciprocal (an fp32 product)
+ * rounded to nearest, ties to even.  NaN stays NaN; an infinity becomes NaN in
+ * e4m3.  col_sums, if not null, receives the sums of v over rows (fp32 [cols],
+ * fixed order: what a bias's gradient is). */
+int64_t fno_fp8_pitch(int64_t cols);
+fno_status fno_fp8_quantize_workspace_size(const fno_fp8_quantize_desc *desc, size_t *bytes);
+fno_status fno_fp8_quantize(const fno_fp8_quantize_desc *desc, const void *x, void *codes,
+                            void *scale, void *codes_t, void *scale_t, float *col_sums, void *ws,
+                            size_t ws_len, hipStream_t stream);
+
+typedef struct {
+  int32_t format_a, format_b;  /* fno_fp8_format */
+  int32_t scale_type;          /* fno_scale_type of both */
+  int32_t blocks_a, blocks_b;  /* fno_fp8_blocks */
+  int32_t out_dtype;           /* fno_dtype of out and z */
+  int32_t activation;          /* fno_norm_activation: whose derivative multiplies */
+  int64_t rows, cols, inner;   /* >= 1, each up to 2^31 - 1 */
+} fno_fp8_matmul_desc;
+
+/* out = (A B^T) act'(z) + bias:  A [rows][inner] and B [cols][inner] in codes,
+ * out and z [rows][cols], bias fp32 [cols] (null: none).  z is null if and only
+ * if the activation is NONE.  Products are exact, sums fp32 (a fixed order), one
+ * rounding to out_dtype.  A row of codes is read whole, fno_fp8_pitch(inner)
+ * bytes: what stands behind `inner` has to be zero. */
+fno_status fno_fp8_matmul_workspace_size(const fno_fp8_matmul_desc *desc, size_t *bytes);
+fno_status fno_fp8_matmul(const fno_fp8_matmul_desc *desc, const void *a, const void *scale_a,
+                          const void *b, const void *scale_b, const void *z, const float *bias,
+                          void *out, void *ws, size_t ws_len, hipStream_t stream);
+
 /* Per-kernel timing with HIP events (a profiling aid, off by default).
  * While enabled, every kernel the library launches is bracketed by a pair of
  * HIP events recorded on the launch stream (events are created per launch, so

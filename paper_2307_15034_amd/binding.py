@@ -174,6 +174,42 @@ class FnoResidualNormParams(ctypes.Structure):
                 for k in ("post_w", "post_b", "gate", "scale", "pre_w", "pre_b")]
 
 
+FNO_FP8_BLOCK = 128
+FNO_FP8_E4M3 = 0
+FNO_FP8_E5M2 = 1
+FNO_SCALE_POW2 = 0
+FNO_SCALE_F32 = 1
+FNO_BLOCKS_ROW = 0
+FNO_BLOCKS_TILE = 1
+
+
+class FnoFp8QuantizeDesc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("scale_type", ctypes.c_int32),
+        ("blocks", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+    ]
+
+
+class FnoFp8MatmulDesc(ctypes.Structure):
+    _fields_ = [
+        ("format_a", ctypes.c_int32),
+        ("format_b", ctypes.c_int32),
+        ("scale_type", ctypes.c_int32),
+        ("blocks_a", ctypes.c_int32),
+        ("blocks_b", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("inner", ctypes.c_int64),
+    ]
+
+
 class FnoWeights(ctypes.Structure):
     _fields_ = [
         ("dense", ctypes.c_void_p),
@@ -245,6 +281,13 @@ def _load() -> ctypes.CDLL:
         "fno_residual_norm_fwd": (ctypes.c_int, [RD, RP, vp, vp, vp, vp, vp]),
         "fno_residual_norm_bwd": (ctypes.c_int,
                                   [RD, RP, vp, vp, vp, vp, vp, vp, vp, RP, vp, sz, vp]),
+        "fno_fp8_pitch": (i64, [i64]),
+        "fno_fp8_quantize_workspace_size": (ctypes.c_int, [P(FnoFp8QuantizeDesc), P(sz)]),
+        "fno_fp8_quantize": (ctypes.c_int,
+                             [P(FnoFp8QuantizeDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "fno_fp8_matmul_workspace_size": (ctypes.c_int, [P(FnoFp8MatmulDesc), P(sz)]),
+        "fno_fp8_matmul": (ctypes.c_int,
+                           [P(FnoFp8MatmulDesc), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "fno_release_caches": (ctypes.c_int, []),
         "fno_profile_enable": (ctypes.c_int, [i32]),
         "fno_profile_reset": (ctypes.c_int, []),
@@ -273,6 +316,8 @@ EXPORTED = [
     "fno_group_norm_act_workspace_size", "fno_group_norm_act_fwd", "fno_group_norm_act_bwd",
     "fno_grad_norm_workspace_size", "fno_grad_norm", "fno_adamw_step", "fno_adamw_moments",
     "fno_residual_norm_workspace_size", "fno_residual_norm_fwd", "fno_residual_norm_bwd",
+    "fno_fp8_pitch", "fno_fp8_quantize_workspace_size", "fno_fp8_quantize",
+    "fno_fp8_matmul_workspace_size", "fno_fp8_matmul",
 ]
 
 
@@ -578,6 +623,61 @@ def fno_residual_norm_bwd(desc, params: FnoResidualNormParams, x: int, u: int, y
                                     stream or None)
     if check:
         _check(st, "fno_residual_norm_bwd")
+    return st
+
+
+def fno_fp8_pitch(cols: int) -> int:
+    return _lib.fno_fp8_pitch(cols)
+
+
+def make_fp8_quantize_desc(rows: int, cols: int, dtype: int = FNO_DTYPE_F16,
+                           format: int = FNO_FP8_E4M3, scale_type: int = FNO_SCALE_POW2,
+                           blocks: int = FNO_BLOCKS_ROW,
+                           activation: int = FNO_NORM_ACT_NONE) -> FnoFp8QuantizeDesc:
+    return FnoFp8QuantizeDesc(dtype, format, scale_type, blocks, activation, rows, cols)
+
+
+def fno_fp8_quantize_workspace_size(desc: FnoFp8QuantizeDesc) -> int:
+    b = ctypes.c_size_t()
+    _check(_lib.fno_fp8_quantize_workspace_size(ctypes.byref(desc), ctypes.byref(b)),
+           "fno_fp8_quantize_workspace_size")
+    return b.value
+
+
+def fno_fp8_quantize(desc, x: int, codes: int, scale: int, codes_t: int, scale_t: int,
+                     col_sums: int, ws: int, ws_bytes: int, stream: int,
+                     check: bool = True) -> int:
+    st = _lib.fno_fp8_quantize(ctypes.byref(desc), x or None, codes or None, scale or None,
+                               codes_t or None, scale_t or None, col_sums or None, ws or None,
+                               ws_bytes, stream or None)
+    if check:
+        _check(st, "fno_fp8_quantize")
+    return st
+
+
+def make_fp8_matmul_desc(rows: int, cols: int, inner: int, out_dtype: int = FNO_DTYPE_F16,
+                         format_a: int = FNO_FP8_E4M3, format_b: int = FNO_FP8_E4M3,
+                         scale_type: int = FNO_SCALE_POW2, blocks_a: int = FNO_BLOCKS_ROW,
+                         blocks_b: int = FNO_BLOCKS_ROW,
+                         activation: int = FNO_NORM_ACT_NONE) -> FnoFp8MatmulDesc:
+    return FnoFp8MatmulDesc(format_a, format_b, scale_type, blocks_a, blocks_b, out_dtype,
+                            activation, rows, cols, inner)
+
+
+def fno_fp8_matmul_workspace_size(desc: FnoFp8MatmulDesc) -> int:
+    b = ctypes.c_size_t()
+    _check(_lib.fno_fp8_matmul_workspace_size(ctypes.byref(desc), ctypes.byref(b)),
+           "fno_fp8_matmul_workspace_size")
+    return b.value
+
+
+def fno_fp8_matmul(desc, a: int, scale_a: int, b: int, scale_b: int, z: int, bias: int, out: int,
+                   ws: int, ws_bytes: int, stream: int, check: bool = True) -> int:
+    st = _lib.fno_fp8_matmul(ctypes.byref(desc), a or None, scale_a or None, b or None,
+                             scale_b or None, z or None, bias or None, out or None, ws or None,
+                             ws_bytes, stream or None)
+    if check:
+        _check(st, "fno_fp8_matmul")
     return st
 
 

@@ -1,0 +1,487 @@
+// Products of 8-bit codes with block scales, out = (A B^T) act'(z) + bias, on the
+// matrix cores.
+//
+// 16-bit results: 16 x 16 x 128 products of codes, whose inner length is one scale
+// block.  That instruction joins eight neighbouring products at a time in fewer
+// bits than fp32: each is cut towards zero to a multiple of 2^-13 of the power of
+// two below the largest of the eight (measured, as for the 8-bit products of inner
+// length 32); the eights are joined in fp32.  On normally distributed codes the
+// sums are 1.5e-5 off in the 2-norm, a thirtieth of fp16's rounding of the result.
+// fp32 results, whose rounding is below that: the codes are widened to bfloat16,
+// which holds them exactly, and multiplied at half the rate by products that keep
+// fp32 throughout (8e-9 off).
+//
+// Powers of two as scales are the 8-bit instruction's own (one byte for each row
+// of its operands), or the widening's, so the sums over all blocks stay in the
+// accumulators.  fp32 scales multiply each block's product on the vector unit as
+// it joins the sum.
+//
+// Rows of a tile are dealt to the matrix operands so that four operands' rows
+// lie next to each other in memory: element i of operand 4 h + m is row 64 h + 4 i
+// + m.  Four bytes next to each other then are the scales of four operands, and
+// a lane ends with four consecutive columns of a row.
+#include <algorithm>
+#include <type_traits>
+
+#include "fno_fp8.h"
+#include "fno_host.h"
+#include "fno_norm.h"
+
+namespace fno {
+namespace {
+
+typedef int V8I __attribute__((ext_vector_type(8)));
+typedef int V4I __attribute__((ext_vector_type(4)));
+typedef float V4F __attribute__((ext_vector_type(4)));
+typedef __bf16 V2B __attribute__((ext_vector_type(2)));
+typedef __bf16 V8B __attribute__((ext_vector_type(8)));
+
+// What chunks behind a row's last code read.
+__device__ const uint4 kZeros = {0, 0, 0, 0};
+
+// 16 bytes a lane from global memory into LDS, a wave's lanes one behind the other
+// from `to` on (the same for the whole wave).  Written out, because behind the
+// builtin the compiler waits for the copy before any read of LDS that may be its
+// target, the other buffer's among them; here all_arrived() is the wait.
+__device__ __forceinline__ void copy16_to_lds(uint64_t from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(from), "s"(to)
+               : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane(
+      (int)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
+}
+
+// Waits for this wave's copies into LDS (which no other wait covers) and for the
+// other waves.
+__device__ __forceinline__ void all_arrived() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// ROWS x 128 codes of block column `kb` from row `r0` on into LDS: row r's piece
+// c of 16 at place c ^ (r / 4 mod 8) of the row, so that the lanes of an operand's
+// load (rows 4 apart) spread over the banks.  Rows behind the last repeat it.
+// Addresses are formed anew at each call (a few operations beside thousands of
+// cycles of products): kept over the loop, they would cost 16 registers.
+template <int ROWS, int THREADS>
+__device__ __forceinline__ void load_tile(const uint8_t* codes, int64_t r0, int64_t rows,
+                                          int64_t pitch, int kb, uint8_t* lds) {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  const int r = t >> 3, c = ((t & 7) ^ ((t >> 5) & 7)) << 4;
+  const int most = rows - r0 < ROWS ? (int)(rows - r0) - 1 : ROWS - 1;
+  const uint8_t* base = codes + r0 * pitch + (int64_t)kb * kBlock;
+  const bool there = (int64_t)kb * kBlock + c < pitch;
+  const uint32_t to = lds_address(lds + (threadIdx.x & ~63) * 16);
+#pragma unroll
+  for (int i = 0; i < ROWS * 8 / THREADS; ++i) {
+    const int row = r + i * (THREADS / 8) < most ? r + i * (THREADS / 8) : most;
+    uint64_t from = (uint64_t)base + (uint64_t)(unsigned)row * (unsigned)pitch + (unsigned)c;
+    from = there ? from : (uint64_t)&kZeros;
+    copy16_to_lds(from, to + i * THREADS * 16);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void finish4(const MatmulArgs& g, int64_t row, int64_t col, V4F v,
+                                        bool whole) {
+  const int64_t at = row * g.N + col;
+  T r[4];
+  if (g.z) {
+    const T* z = static_cast<const T*>(g.z) + at;
+    if (whole) {
+      __builtin_memcpy(r, __builtin_assume_aligned(z, sizeof(T)), sizeof(r));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] *= act_grad_any<T>((float)r[j], g.act);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (col + j < g.N) v[j] *= act_grad_any<T>((float)z[j], g.act);
+    }
+  }
+  if (g.bias) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (col + j < g.N) v[j] += g.bias[col + j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = (T)v[j];
+  T* out = static_cast<T*>(g.out) + at;
+  if (whole) {
+    __builtin_memcpy(__builtin_assume_aligned(out, sizeof(T)), r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (col + j < g.N) out[j] = r[j];
+  }
+}
+__device__ __forceinline__ void finish4_any(const MatmulArgs& g, int64_t row, int64_t col, V4F v) {
+  const bool whole = col + 4 <= g.N;
+  if (g.dtype == FNO_DTYPE_F32)
+    finish4<float>(g, row, col, v, whole);
+  else if (g.dtype == FNO_DTYPE_F16)
+    finish4<_Float16>(g, row, col, v, whole);
+  else
+    finish4<__bf16>(g, row, col, v, whole);
+}
+
+// Work-groups go round the eight dies in turn: the tiles of a die are made
+// consecutive ones, and those go through bands of eight tile rows, column by
+// column, so that what a die reads at a time is read again from its cache.
+__device__ __forceinline__ void tile_of(const MatmulArgs& g, int64_t id, int64_t* tm, int64_t* tn) {
+  const int64_t total = g.tiles_m * g.tiles_n, each = total >> 3;
+  if (id < each * 8) id = (id & 7) * each + (id >> 3);
+  const int64_t band = id / (8 * g.tiles_n), m0 = band * 8;
+  const int64_t rows = g.tiles_m - m0 < 8 ? g.tiles_m - m0 : 8;
+  id -= band * 8 * g.tiles_n;
+  *tn = id / rows;
+  *tm = m0 + (id - *tn * rows);
+}
+
+// The 32 codes of a lane's operand in bfloat16, times a power of two.
+template <int FMT>
+__device__ __forceinline__ void widen(V8I codes, float scale, V8B (&out)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = codes[2 * i + (j >> 1)];
+      V2B v;
+      if constexpr (FMT == FNO_FP8_E4M3)
+        v = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true)
+                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false);
+      else
+        v = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, scale, true)
+                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, scale, false);
+      out[i][2 * j] = v[0];
+      out[i][2 * j + 1] = v[1];
+    }
+}
+// Byte m of four scales as a number (255: NaN).
+__device__ __forceinline__ float scale_of(int four, int m) {
+  const unsigned b = ((unsigned)four >> (8 * m)) & 255u;
+  return __builtin_bit_cast(float, b == 255u ? 0x7fc00000u : b ? b << 23 : 0x00400000u);
+}
+
+template <int FA, int FB, bool F32S, bool WIDE, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN) void gemm_kernel(MatmulArgs g) {
+  constexpr int THREADS = 64 * WGM * WGN;
+  constexpr int TM = BM / WGM, TN = BN / WGN;  // a wave's part
+  constexpr int HM = TM / 64, HN = TN / 64;
+  __shared__ __attribute__((aligned(16))) uint8_t tile_a[2][BM * kBlock], tile_b[2][BN * kBlock];
+  using S = std::conditional_t<F32S, float, uint8_t>;
+  static_assert(BM + BN == THREADS, "a scale for each thread");
+  __shared__ __attribute__((aligned(16))) S scales[2][BM + BN];
+  const int lane = threadIdx.x & 63, i16 = lane & 15, kg = lane >> 4;
+  const int wave = threadIdx.x >> 6, wm = wave / WGN, wn = wave % WGN;
+  int64_t tm, tn;
+  tile_of(g, blockIdx.x, &tm, &tn);
+  const int64_t m0 = tm * BM, n0 = tn * BN;
+  const int first = blockIdx.y * g.kb_per_split;
+  const int last = first + g.kb_per_split < g.kb ? first + g.kb_per_split : g.kb;
+
+  V4F acc[HM * 4][HN * 4];
+#pragma unroll
+  for (int i = 0; i < HM * 4; ++i)
+#pragma unroll
+    for (int j = 0; j < HN * 4; ++j) acc[i][j] = V4F{0.0f, 0.0f, 0.0f, 0.0f};
+
+  // Thread t brings the scales of row t of A's tile, or row t - BM of B's.
+  const bool of_a = threadIdx.x < BM;
+  int64_t srow = of_a ? m0 + threadIdx.x : n0 + threadIdx.x - BM;
+  const int64_t most = (of_a ? g.M : g.N) - 1;
+  srow = (srow < most ? srow : most) >> (of_a ? g.shift_a : g.shift_b);
+  const uint64_t sbase = of_a ? (uint64_t)g.scale_a : (uint64_t)g.scale_b;
+  const int64_t sstep = of_a ? g.scales_a : g.scales_b;
+  uint64_t sat = sbase + (uint64_t)(srow + first * sstep) * sizeof(S);
+  S next_s;
+  auto fetch = [&](int kb, uint8_t* a, uint8_t* b) {
+    next_s = *reinterpret_cast<const __attribute__((address_space(1))) S*>(sat);
+    sat += (uint64_t)sstep * sizeof(S);
+    load_tile<BM, THREADS>(g.a, m0, g.M, g.pitch, kb, a);
+    load_tile<BN, THREADS>(g.b, n0, g.N, g.pitch, kb, b);
+  };
+  auto operand = [&](const uint8_t* lds, int row) {  // rows row + 4 i
+    const uint8_t* p = lds + (row + i16 * 4) * kBlock;
+    const V4I lo = *reinterpret_cast<const V4I*>(p + ((kg ^ (i16 & 7)) << 4));
+    const V4I hi = *reinterpret_cast<const V4I*>(p + (((kg + 4) ^ (i16 & 7)) << 4));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto step = [&](const uint8_t* a, const uint8_t* b, const S* s) {
+    int sb[HN];  // of four operands, a byte each
+    if constexpr (!F32S) {
+#pragma unroll
+      for (int q = 0; q < HN; ++q) sb[q] = *reinterpret_cast<const int*>(s + BM + wn * TN + q * 64 + i16 * 4);
+    }
+    V8I fb[WIDE ? 1 : HN * 4];
+    V8B wb[WIDE ? HN * 4 : 1][4];
+#pragma unroll
+    for (int j = 0; j < HN * 4; ++j) {
+      const V8I f = operand(b, wn * TN + (j >> 2) * 64 + (j & 3));
+      if constexpr (WIDE)
+        widen<FB>(f, F32S ? 1.0f : scale_of(sb[j >> 2], j & 3), wb[j]);
+      else
+        fb[j] = f;
+    }
+#pragma unroll
+    for (int h = 0; h < HM; ++h) {
+      V4F ra[4], cb[HN];
+      if constexpr (F32S) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          ra[r] = *reinterpret_cast<const V4F*>(s + wm * TM + h * 64 + kg * 16 + r * 4);
+#pragma unroll
+        for (int q = 0; q < HN; ++q)
+          cb[q] = *reinterpret_cast<const V4F*>(s + BM + wn * TN + q * 64 + i16 * 4);
+      }
+      int sa = 0;
+      if constexpr (!F32S) sa = *reinterpret_cast<const int*>(s + wm * TM + h * 64 + i16 * 4);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        __builtin_amdgcn_sched_barrier(0);  // one operand's loads ahead: registers
+        const V8I fa = operand(a, wm * TM + h * 64 + m);
+        V8B wa[4];
+        if constexpr (WIDE) widen<FA>(fa, F32S ? 1.0f : scale_of(sa, m), wa);
+#pragma unroll
+        for (int q = 0; q < HN; ++q) {
+          V4F* c = &acc[h * 4 + m][q * 4];
+          if constexpr (WIDE || F32S) {
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              V4F p = F32S ? V4F{0.0f, 0.0f, 0.0f, 0.0f} : c[n];
+              if constexpr (WIDE) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[i], wb[q * 4 + n][i], p, 0, 0, 0);
+              } else {
+                p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + n], p, FA, FB, 0, 0, 0, 0);
+              }
+              if constexpr (F32S) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  c[n][r] = __builtin_fmaf(p[r], ra[r][m] * cb[q][n], c[n][r]);
+              } else {
+                c[n] = p;
+              }
+            }
+          } else {
+#define FNO_MFMA(M_, N_)                                                                          \
+  c[N_] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + N_], c[N_], FA, FB, M_, \
+                                                           sa, N_, sb[q]);
+#define FNO_MFMA4(M_) FNO_MFMA(M_, 0) FNO_MFMA(M_, 1) FNO_MFMA(M_, 2) FNO_MFMA(M_, 3)
+            if (m == 0) { FNO_MFMA4(0) }
+            if (m == 1) { FNO_MFMA4(1) }
+            if (m == 2) { FNO_MFMA4(2) }
+            if (m == 3) { FNO_MFMA4(3) }
+#undef FNO_MFMA4
+#undef FNO_MFMA
+          }
+        }
+      }
+    }
+  };
+
+  fetch(first, tile_a[0], tile_b[0]);
+  scales[0][threadIdx.x] = next_s;
+  for (int kb = first; kb < last; ++kb) {
+    const int cur = (kb - first) & 1;
+    all_arrived();  // this block's tiles are there, the other buffers free
+    if (kb + 1 < last) fetch(kb + 1, tile_a[cur ^ 1], tile_b[cur ^ 1]);
+    step(tile_a[cur], tile_b[cur], scales[cur]);
+    if (kb + 1 < last) scales[cur ^ 1][threadIdx.x] = next_s;
+  }
+
+  const bool split = g.splits > 1;
+  float* part = split ? g.part + (int64_t)blockIdx.y * g.M * g.N : nullptr;
+#pragma unroll
+  for (int h = 0; h < HM; ++h)
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t row = m0 + wm * TM + h * 64 + kg * 16 + r * 4 + m;
+        if (row >= g.M) continue;
+#pragma unroll
+        for (int q = 0; q < HN; ++q) {
+          const int64_t col = n0 + wn * TN + q * 64 + i16 * 4;
+          if (col >= g.N) continue;
+          const V4F v = {acc[h * 4 + m][q * 4][r], acc[h * 4 + m][q * 4 + 1][r],
+                         acc[h * 4 + m][q * 4 + 2][r], acc[h * 4 + m][q * 4 + 3][r]};
+          if (split) {
+            float* p = part + row * g.N + col;
+            if (col + 4 <= g.N) {
+              __builtin_memcpy(__builtin_assume_aligned(p, 4), &v, 16);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (col + j < g.N) p[j] = v[j];
+            }
+          } else {
+            finish4_any(g, row, col, v);
+          }
+        }
+      }
+}
+
+// Joins the splits' sums in their order, four columns a thread.
+__global__ __launch_bounds__(256) void join_splits_kernel(MatmulArgs g) {
+  const int64_t per_row = (g.N + 3) / 4, total = g.M * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per_row, col = (i - row * per_row) * 4;
+    const float* p = g.part + row * g.N + col;
+    V4F v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (col + 4 <= g.N) {
+      for (int s = 0; s < g.splits; ++s, p += g.M * g.N) {
+        float t[4];
+        __builtin_memcpy(t, __builtin_assume_aligned(p, 4), 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += t[j];
+      }
+    } else {
+      for (int s = 0; s < g.splits; ++s, p += g.M * g.N)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col + j < g.N) v[j] += p[j];
+    }
+    finish4_any(g, row, col, v);
+  }
+}
+
+// --------------------------------------------------------------------------
+// Host side
+// --------------------------------------------------------------------------
+fno_status check_desc(const fno_fp8_matmul_desc* d) {
+  if (!d) return FNO_ERR_INVALID_ARGUMENT;
+  for (int f : {d->format_a, d->format_b})
+    if (f != FNO_FP8_E4M3 && f != FNO_FP8_E5M2) return FNO_ERR_INVALID_ARGUMENT;
+  for (int b : {d->blocks_a, d->blocks_b})
+    if (b != FNO_BLOCKS_ROW && b != FNO_BLOCKS_TILE) return FNO_ERR_INVALID_ARGUMENT;
+  if (d->scale_type != FNO_SCALE_POW2 && d->scale_type != FNO_SCALE_F32)
+    return FNO_ERR_INVALID_ARGUMENT;
+  if (d->out_dtype < FNO_DTYPE_F32 || d->out_dtype > FNO_DTYPE_BF16) return FNO_ERR_INVALID_ARGUMENT;
+  if (d->activation < FNO_NORM_ACT_NONE || d->activation > FNO_NORM_ACT_SILU)
+    return FNO_ERR_INVALID_ARGUMENT;
+  for (int64_t n : {d->rows, d->cols, d->inner})
+    if (n < 1 || n > INT32_MAX) return FNO_ERR_INVALID_ARGUMENT;
+  if (d->rows > ((int64_t)1 << 42) / d->cols) return FNO_ERR_INVALID_ARGUMENT;
+  return FNO_OK;
+}
+
+struct MatmulPlan {
+  MatmulArgs g;
+  bool big;
+};
+
+MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
+  MatmulPlan p{};
+  MatmulArgs& g = p.g;
+  g.M = d.rows;
+  g.N = d.cols;
+  g.kb = (int)fp8_cdiv(d.inner, kBlock);
+  g.pitch = fp8_pitch(d.inner);
+  g.shift_a = d.blocks_a == FNO_BLOCKS_TILE ? 7 : 0;
+  g.shift_b = d.blocks_b == FNO_BLOCKS_TILE ? 7 : 0;
+  g.scales_a = g.shift_a ? fp8_cdiv(g.M, kBlock) : g.M;
+  g.scales_b = g.shift_b ? fp8_cdiv(g.N, kBlock) : g.N;
+  g.act = d.activation;
+  g.dtype = d.out_dtype;
+  p.big = d.scale_type == FNO_SCALE_POW2 && fp8_cdiv(g.M, 256) * fp8_cdiv(g.N, 256) >= 192;
+  const int side = p.big ? 256 : 128;
+  g.tiles_m = fp8_cdiv(g.M, side);
+  g.tiles_n = fp8_cdiv(g.N, side);
+  // Few tiles of a long inner axis: split along it, down to four blocks each.
+  const int64_t tiles = g.tiles_m * g.tiles_n;
+  g.splits = 1;
+  if (tiles < 512 && g.kb >= 8)
+    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, g.kb / 4));
+  g.kb_per_split = (int)fp8_cdiv(g.kb, g.splits);
+  g.splits = (int)fp8_cdiv(g.kb, g.kb_per_split);
+  return p;
+}
+
+struct MatmulLaunch {
+  MatmulPlan p;
+  int fa, fb;
+  bool f32s;
+  hipStream_t stream;
+};
+
+template <int FA, int FB>
+void launch_formats(const MatmulLaunch& L) {
+  const MatmulArgs& g = L.p.g;
+  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits);
+  const bool wide = g.dtype == FNO_DTYPE_F32;
+  if (L.f32s)
+    wide ? gemm_kernel<FA, FB, true, true, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g)
+         : gemm_kernel<FA, FB, true, false, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g);
+  else if (L.p.big)
+    wide ? gemm_kernel<FA, FB, false, true, 256, 256, 2, 4><<<grid, dim3(512), 0, L.stream>>>(g)
+         : gemm_kernel<FA, FB, false, false, 256, 256, 2, 4><<<grid, dim3(512), 0, L.stream>>>(g);
+  else
+    wide ? gemm_kernel<FA, FB, false, true, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g)
+         : gemm_kernel<FA, FB, false, false, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g);
+}
+
+hipError_t launch_matmul(void* ctx) {
+  const MatmulLaunch& L = *static_cast<MatmulLaunch*>(ctx);
+  // the instruction's format numbers are this ABI's: 0 e4m3, 1 e5m2
+  if (L.fa == FNO_FP8_E4M3)
+    L.fb == FNO_FP8_E4M3 ? launch_formats<0, 0>(L) : launch_formats<0, 1>(L);
+  else
+    L.fb == FNO_FP8_E4M3 ? launch_formats<1, 0>(L) : launch_formats<1, 1>(L);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || L.p.g.splits == 1) return e;
+  const int64_t groups = fp8_cdiv(L.p.g.M * fp8_cdiv(L.p.g.N, 4), 256);
+  join_splits_kernel<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 20)), dim3(256), 0, L.stream>>>(L.p.g);
+  return hipGetLastError();
+}
+
+size_t ws_bytes(const MatmulPlan& p) {
+  if (p.g.splits == 1) return 256;
+  return (size_t)(fp8_cdiv(p.g.splits * p.g.M * p.g.N * 4, 256) * 256);
+}
+
+}  // namespace
+}  // namespace fno
+
+using namespace fno;
+
+extern "C" fno_status fno_fp8_matmul_workspace_size(const fno_fp8_matmul_desc* d, size_t* bytes) {
+  const fno_status st = check_desc(d);
+  if (st != FNO_OK) return st;
+  if (!bytes) return FNO_ERR_INVALID_ARGUMENT;
+  *bytes = ws_bytes(plan_of(*d));
+  return FNO_OK;
+}
+
+extern "C" fno_status fno_fp8_matmul(const fno_fp8_matmul_desc* d, const void* a,
+                                     const void* scale_a, const void* b, const void* scale_b,
+                                     const void* z, const float* bias, void* out, void* ws,
+                                     size_t ws_len, hipStream_t stream) {
+  const fno_status st = check_desc(d);
+  if (st != FNO_OK) return st;
+  if (!fp8_ok16(a) || !fp8_ok16(scale_a) || !fp8_ok16(b) || !fp8_ok16(scale_b) || !fp8_ok16(out) ||
+      !fp8_null_or16(z) || !fp8_null_or16(bias))
+    return FNO_ERR_INVALID_ARGUMENT;
+  if ((z != nullptr) != (d->activation != FNO_NORM_ACT_NONE)) return FNO_ERR_INVALID_ARGUMENT;
+  MatmulLaunch L{plan_of(*d), d->format_a, d->format_b, d->scale_type == FNO_SCALE_F32, stream};
+  if (L.p.g.splits > 1) {
+    if (ws_len < ws_bytes(L.p)) return FNO_ERR_WORKSPACE_TOO_SMALL;
+    if (!fp8_ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
+  }
+  if (L.p.g.tiles_m * L.p.g.tiles_n > INT32_MAX) return FNO_ERR_UNSUPPORTED;
+  MatmulArgs& g = L.p.g;
+  g.a = static_cast<const uint8_t*>(a);
+  g.b = static_cast<const uint8_t*>(b);
+  g.scale_a = scale_a;
+  g.scale_b = scale_b;
+  g.z = z;
+  g.bias = bias;
+  g.out = out;
+  g.part = static_cast<float*>(ws);
+  const hipError_t e = timed_launch("fp8_matmul", stream, launch_matmul, &L);
+  return e == hipSuccess ? FNO_OK : report_hip_error(e, "fp8_matmul");
+}

@@ -52,3 +52,48 @@ def test_residual_norm_call_refusals():
         assert B.fno_residual_norm_bwd(d, **{**bwd, **kw}, check=False) == BAD, kw
     assert B.fno_residual_norm_bwd(d, **{**bwd, "ws_bytes": 0},
                                    check=False) == B.FNO_ERR_WORKSPACE_TOO_SMALL
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=0), dict(cols=0), dict(rows=-5), dict(rows=1 << 31), dict(cols=1 << 31),
+    dict(rows=1 << 30, cols=1 << 30), dict(dtype=3), dict(dtype=-1), dict(format=2), dict(format=-1),
+    dict(scale_type=2), dict(blocks=2), dict(activation=3), dict(activation=-1)])
+def test_quantize_descriptor_refused(kw):
+    with pytest.raises(B.FnoError) as e:
+        B.fno_fp8_quantize_workspace_size(B.make_fp8_quantize_desc(**{**dict(rows=10, cols=20), **kw}))
+    assert e.value.status == BAD
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=0), dict(cols=0), dict(inner=0), dict(rows=1 << 31), dict(inner=1 << 31),
+    dict(rows=1 << 30, cols=1 << 30), dict(out_dtype=3), dict(format_a=2), dict(format_b=-1),
+    dict(scale_type=2), dict(blocks_a=2), dict(blocks_b=-1), dict(activation=3)])
+def test_matmul_descriptor_refused(kw):
+    with pytest.raises(B.FnoError) as e:
+        B.fno_fp8_matmul_workspace_size(B.make_fp8_matmul_desc(**{**dict(rows=10, cols=20, inner=30), **kw}))
+    assert e.value.status == BAD
+
+
+def test_pitch():
+    assert [B.fno_fp8_pitch(n) for n in (-1, 0, 1, 16, 17, 128, (1 << 31) - 1)] == \
+        [0, 0, 16, 16, 32, 128, 1 << 31]
+
+
+def test_fp8_call_refusals():
+    d = B.make_fp8_quantize_desc(10, 20)
+    call = dict(x=A, codes=A, scale=A, codes_t=2 * A, scale_t=A, col_sums=A, ws=A, ws_bytes=1 << 20,
+                stream=0)
+    for kw in (dict(x=0), dict(x=A + 4), dict(codes=A + 4), dict(codes=0), dict(scale=0),
+               dict(codes_t=0), dict(scale_t=0), dict(scale=A + 1), dict(codes_t=A), dict(ws=0),
+               dict(ws=A + 4), dict(col_sums=A + 4),
+               dict(codes=0, scale=0, codes_t=0, scale_t=0)):
+        assert B.fno_fp8_quantize(d, **{**call, **kw}, check=False) == BAD, kw
+    assert B.fno_fp8_quantize(d, **{**call, "ws_bytes": 255}, check=False) == B.FNO_ERR_WORKSPACE_TOO_SMALL
+    d = B.make_fp8_matmul_desc(10, 20, 100000)
+    call = dict(a=A, scale_a=A, b=A, scale_b=A, z=0, bias=A, out=A, ws=A, ws_bytes=1 << 30, stream=0)
+    for kw in (dict(a=0), dict(b=0), dict(scale_a=0), dict(scale_b=0), dict(out=0), dict(a=A + 8),
+               dict(scale_b=A + 4), dict(z=A), dict(bias=A + 4), dict(out=A + 2), dict(ws=0), dict(ws=A + 4)):
+        assert B.fno_fp8_matmul(d, **{**call, **kw}, check=False) == BAD, kw
+    assert B.fno_fp8_matmul(d, **{**call, "ws_bytes": 255}, check=False) == B.FNO_ERR_WORKSPACE_TOO_SMALL
+    d = B.make_fp8_matmul_desc(10, 20, 30, activation=B.FNO_NORM_ACT_GELU)
+    assert B.fno_fp8_matmul(d, **call, check=False) == BAD
