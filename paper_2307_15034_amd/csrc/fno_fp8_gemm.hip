@@ -22,6 +22,7 @@
 // a lane ends with four consecutive columns of a row.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "fno_fp8.h"
 #include "fno_host.h"
@@ -49,6 +50,13 @@ __device__ __forceinline__ void copy16_to_lds(uint64_t from, uint32_t to) {
                : "v"(from), "s"(to)
                : "memory", "m0");
 }
+// The same from a base of the whole wave's and an offset of the lane's.
+__device__ __forceinline__ void copy16_to_lds(uint64_t base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(to)
+               : "memory", "m0");
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)__builtin_amdgcn_readfirstlane(
       (int)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
@@ -61,29 +69,50 @@ __device__ __forceinline__ void all_arrived() {
   __syncthreads();
 }
 
-// ROWS x 128 codes of block column `kb` from row `r0` on into LDS: row r's piece
-// c of 16 at place c ^ (r / 4 mod 8) of the row, so that the lanes of an operand's
-// load (rows 4 apart) spread over the banks.  Rows behind the last repeat it.
-// Addresses are formed anew at each call (a few operations beside thousands of
-// cycles of products): kept over the loop, they would cost 16 registers.
+// Brings ROWS x 128 codes of a block column into LDS: row r's piece c of 16 at
+// place c ^ (r / 4 mod 8) of the row, so that the lanes of an operand's load (rows
+// 4 apart) spread over the banks.  Rows behind the last repeat it, pieces behind a
+// row's last code are zeros.
 template <int ROWS, int THREADS>
-__device__ __forceinline__ void load_tile(const uint8_t* codes, int64_t r0, int64_t rows,
-                                          int64_t pitch, int kb, uint8_t* lds) {
-  int t = threadIdx.x;
-  asm volatile("" : "+v"(t));
-  const int r = t >> 3, c = ((t & 7) ^ ((t >> 5) & 7)) << 4;
-  const int most = rows - r0 < ROWS ? (int)(rows - r0) - 1 : ROWS - 1;
-  const uint8_t* base = codes + r0 * pitch + (int64_t)kb * kBlock;
-  const bool there = (int64_t)kb * kBlock + c < pitch;
-  const uint32_t to = lds_address(lds + (threadIdx.x & ~63) * 16);
+struct TileLoad {
+  static constexpr int N = ROWS * 8 / THREADS;
+  uint32_t off[N];  // of the thread's pieces, from the tile's first row on
+  const uint8_t* codes;
+  int64_t pitch;
+  int most;         // last row
+  bool near;        // offsets fit
+  __device__ __forceinline__ TileLoad(const uint8_t* base, int64_t r0, int64_t rows, int64_t pitch_)
+      : codes(base + r0 * pitch_), pitch(pitch_) {
+    const int r = threadIdx.x >> 3, c = ((threadIdx.x & 7) ^ ((threadIdx.x >> 5) & 7)) << 4;
+    most = rows - r0 < ROWS ? (int)(rows - r0) - 1 : ROWS - 1;
+    near = pitch <= ((int64_t)1 << 31) / ROWS;
 #pragma unroll
-  for (int i = 0; i < ROWS * 8 / THREADS; ++i) {
-    const int row = r + i * (THREADS / 8) < most ? r + i * (THREADS / 8) : most;
-    uint64_t from = (uint64_t)base + (uint64_t)(unsigned)row * (unsigned)pitch + (unsigned)c;
-    from = there ? from : (uint64_t)&kZeros;
-    copy16_to_lds(from, to + i * THREADS * 16);
+    for (int i = 0; i < N; ++i) {
+      const int row = r + i * (THREADS / 8) < most ? r + i * (THREADS / 8) : most;
+      off[i] = (uint32_t)row * (uint32_t)pitch + c;
+      asm volatile("" : "+v"(off[i]));  // one register each, not the product's two
+    }
   }
-}
+  __device__ __forceinline__ void fetch(int kb, uint8_t* lds) const {
+    const uint32_t to = lds_address(lds + (threadIdx.x & ~63) * 16);
+    const int64_t at = (int64_t)kb * kBlock;
+    if (near && at + kBlock <= pitch) {
+      const uint64_t base = (uint64_t)codes + at;
+#pragma unroll
+      for (int i = 0; i < N; ++i) copy16_to_lds(base, off[i], to + i * THREADS * 16);
+    } else {
+      int t = threadIdx.x;
+      asm volatile("" : "+v"(t));  // formed here, not kept over the caller's loop
+      const int r = t >> 3, c = ((t & 7) ^ ((t >> 5) & 7)) << 4;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = r + i * (THREADS / 8) < most ? r + i * (THREADS / 8) : most;
+        const uint64_t from = (uint64_t)codes + (uint64_t)row * (uint64_t)pitch + (uint64_t)(at + c);
+        copy16_to_lds(at + c < pitch ? from : (uint64_t)&kZeros, to + i * THREADS * 16);
+      }
+    }
+  }
+};
 
 template <typename T>
 __device__ __forceinline__ void finish4(const MatmulArgs& g, int64_t row, int64_t col, V4F v,
@@ -116,6 +145,49 @@ __device__ __forceinline__ void finish4(const MatmulArgs& g, int64_t row, int64_
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (col + j < g.N) out[j] = r[j];
+  }
+}
+// A wave's part of the tile: four columns at a time of the rows that a lane holds,
+// rows and columns behind the last left out.
+template <typename T, int RM, int RN>
+__device__ __forceinline__ void finish_tile(const MatmulArgs& g, const V4F (&acc)[RM][RN], int64_t row0,
+                                            int64_t col0) {
+#pragma unroll
+  for (int q = 0; q < RN / 4; ++q) {
+    const int64_t col = col0 + q * 64;
+    const bool whole = col + 4 <= g.N;
+    if (whole) {
+      V4F bias = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (g.bias) __builtin_memcpy(&bias, __builtin_assume_aligned(g.bias + col, 4), 16);
+      T* out = static_cast<T*>(g.out) + row0 * g.N + col;
+      const T* z = static_cast<const T*>(g.z) + row0 * g.N + col;
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t row = (i >> 2) * 64 + r * 4 + (i & 3);
+          if (row0 + row >= g.M) continue;
+          V4F v = {acc[i][q * 4][r], acc[i][q * 4 + 1][r], acc[i][q * 4 + 2][r], acc[i][q * 4 + 3][r]};
+          T t[4];
+          if (g.z) {
+            __builtin_memcpy(t, __builtin_assume_aligned(z + row * g.N, sizeof(T)), sizeof(t));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= act_grad_any<T>((float)t[j], g.act);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t[j] = (T)(v[j] + bias[j]);
+          __builtin_memcpy(__builtin_assume_aligned(out + row * g.N, sizeof(T)), t, sizeof(t));
+        }
+    } else if (col < g.N) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t row = row0 + (i >> 2) * 64 + r * 4 + (i & 3);
+          if (row < g.M)
+            finish4<T>(g, row, col, V4F{acc[i][q * 4][r], acc[i][q * 4 + 1][r], acc[i][q * 4 + 2][r], acc[i][q * 4 + 3][r]}, false);
+        }
+    }
   }
 }
 __device__ __forceinline__ void finish4_any(const MatmulArgs& g, int64_t row, int64_t col, V4F v) {
@@ -160,6 +232,14 @@ __device__ __forceinline__ void widen(V8I codes, float scale, V8B (&out)[4]) {
       out[i][2 * j + 1] = v[1];
     }
 }
+template <int N, typename F, int... I>
+__device__ __forceinline__ void unrolled_over(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F&& f) {
+  unrolled_over<N>(f, std::make_integer_sequence<int, N>{});
+}
 // Byte m of four scales as a number (255: NaN).
 __device__ __forceinline__ float scale_of(int four, int m) {
   const unsigned b = ((unsigned)four >> (8 * m)) & 255u;
@@ -197,12 +277,14 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_kernel(MatmulArgs g) {
   const uint64_t sbase = of_a ? (uint64_t)g.scale_a : (uint64_t)g.scale_b;
   const int64_t sstep = of_a ? g.scales_a : g.scales_b;
   uint64_t sat = sbase + (uint64_t)(srow + first * sstep) * sizeof(S);
+  const TileLoad<BM, THREADS> from_a(g.a, m0, g.M, g.pitch);
+  const TileLoad<BN, THREADS> from_b(g.b, n0, g.N, g.pitch);
   S next_s;
   auto fetch = [&](int kb, uint8_t* a, uint8_t* b) {
     next_s = *reinterpret_cast<const __attribute__((address_space(1))) S*>(sat);
     sat += (uint64_t)sstep * sizeof(S);
-    load_tile<BM, THREADS>(g.a, m0, g.M, g.pitch, kb, a);
-    load_tile<BN, THREADS>(g.b, n0, g.N, g.pitch, kb, b);
+    from_a.fetch(kb, a);
+    from_b.fetch(kb, b);
   };
   auto operand = [&](const uint8_t* lds, int row) {  // rows row + 4 i
     const uint8_t* p = lds + (row + i16 * 4) * kBlock;
@@ -210,143 +292,173 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_kernel(MatmulArgs g) {
     const V4I hi = *reinterpret_cast<const V4I*>(p + (((kg + 4) ^ (i16 & 7)) << 4));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  auto step = [&](const uint8_t* a, const uint8_t* b, const S* s) {
-    int sb[HN];  // of four operands, a byte each
-    if constexpr (!F32S) {
-#pragma unroll
-      for (int q = 0; q < HN; ++q) sb[q] = *reinterpret_cast<const int*>(s + BM + wn * TN + q * 64 + i16 * 4);
-    }
-    V8I fb[WIDE ? 1 : HN * 4];
-    V8B wb[WIDE ? HN * 4 : 1][4];
-#pragma unroll
-    for (int j = 0; j < HN * 4; ++j) {
-      const V8I f = operand(b, wn * TN + (j >> 2) * 64 + (j & 3));
-      if constexpr (WIDE)
-        widen<FB>(f, F32S ? 1.0f : scale_of(sb[j >> 2], j & 3), wb[j]);
-      else
-        fb[j] = f;
-    }
+  // A block's products, operand by operand of A (LAST + 1 of them); each of A's
+  // operands is read while the one before is multiplied.  B's operands of the next
+  // block take the place of this one's as its last products go.
+  constexpr int LAST = HM * 4 - 1;
+  V8I fa, fb[WIDE ? 1 : HN * 4];
+  V8B wb[WIDE ? HN * 4 : 1][4];
+  int sa[HM], sb[HN];  // scales of four operands, a byte each
+  V4F ra[F32S ? HM * 4 : 1], cb[F32S ? HN : 1];
+  auto read_a = [&](int buf, int idx) {
+    return operand(tile_a[buf], wm * TM + (idx >> 2) * 64 + (idx & 3));
+  };
+  auto read_b = [&](int buf, int j) {
+    return operand(tile_b[buf], wn * TN + (j >> 2) * 64 + (j & 3));
+  };
+  auto read_scales = [&](int buf) {
+    const S* s = scales[buf];
 #pragma unroll
     for (int h = 0; h < HM; ++h) {
-      V4F ra[4], cb[HN];
       if constexpr (F32S) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          ra[r] = *reinterpret_cast<const V4F*>(s + wm * TM + h * 64 + kg * 16 + r * 4);
-#pragma unroll
-        for (int q = 0; q < HN; ++q)
-          cb[q] = *reinterpret_cast<const V4F*>(s + BM + wn * TN + q * 64 + i16 * 4);
-      }
-      int sa = 0;
-      if constexpr (!F32S) sa = *reinterpret_cast<const int*>(s + wm * TM + h * 64 + i16 * 4);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        __builtin_amdgcn_sched_barrier(0);  // one operand's loads ahead: registers
-        const V8I fa = operand(a, wm * TM + h * 64 + m);
-        V8B wa[4];
-        if constexpr (WIDE) widen<FA>(fa, F32S ? 1.0f : scale_of(sa, m), wa);
-#pragma unroll
-        for (int q = 0; q < HN; ++q) {
-          V4F* c = &acc[h * 4 + m][q * 4];
-          if constexpr (WIDE || F32S) {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-              V4F p = F32S ? V4F{0.0f, 0.0f, 0.0f, 0.0f} : c[n];
-              if constexpr (WIDE) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[i], wb[q * 4 + n][i], p, 0, 0, 0);
-              } else {
-                p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + n], p, FA, FB, 0, 0, 0, 0);
-              }
-              if constexpr (F32S) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                  c[n][r] = __builtin_fmaf(p[r], ra[r][m] * cb[q][n], c[n][r]);
-              } else {
-                c[n] = p;
-              }
-            }
-          } else {
-#define FNO_MFMA(M_, N_)                                                                          \
-  c[N_] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + N_], c[N_], FA, FB, M_, \
-                                                           sa, N_, sb[q]);
-#define FNO_MFMA4(M_) FNO_MFMA(M_, 0) FNO_MFMA(M_, 1) FNO_MFMA(M_, 2) FNO_MFMA(M_, 3)
-            if (m == 0) { FNO_MFMA4(0) }
-            if (m == 1) { FNO_MFMA4(1) }
-            if (m == 2) { FNO_MFMA4(2) }
-            if (m == 3) { FNO_MFMA4(3) }
-#undef FNO_MFMA4
-#undef FNO_MFMA
-          }
-        }
+          ra[h * 4 + r] = *reinterpret_cast<const V4F*>(s + wm * TM + h * 64 + kg * 16 + r * 4);
+      } else {
+        sa[h] = *reinterpret_cast<const int*>(s + wm * TM + h * 64 + i16 * 4);
       }
     }
+#pragma unroll
+    for (int q = 0; q < HN; ++q) {
+      if constexpr (F32S)
+        cb[q] = *reinterpret_cast<const V4F*>(s + BM + wn * TN + q * 64 + i16 * 4);
+      else
+        sb[q] = *reinterpret_cast<const int*>(s + BM + wn * TN + q * 64 + i16 * 4);
+    }
+  };
+  auto widen_b = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < HN * 4; ++j)
+      widen<FB>(read_b(buf, j), F32S ? 1.0f : scale_of(sb[j >> 2], j & 3), wb[j]);
+  };
+  auto multiply = [&](auto index, auto reload, int buf) {
+    constexpr int IDX = decltype(index)::value, H = IDX >> 2, M = IDX & 3;
+    V8B wa[4];
+    if constexpr (WIDE) widen<FA>(fa, F32S ? 1.0f : scale_of(sa[H], M), wa);
+#pragma unroll
+    for (int q = 0; q < HN; ++q)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        V4F* c = &acc[IDX][q * 4 + n];
+        if constexpr (WIDE || F32S) {
+          V4F p = F32S ? V4F{0.0f, 0.0f, 0.0f, 0.0f} : *c;
+          if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[i], wb[q * 4 + n][i], p, 0, 0, 0);
+          } else {
+            p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + n], p, FA, FB, 0, 0, 0, 0);
+          }
+          if constexpr (F32S) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              (*c)[r] = __builtin_fmaf(p[r], ra[H * 4 + r][M] * cb[q][n], (*c)[r]);
+          } else {
+            *c = p;
+          }
+        } else {
+          // (the byte of the scales is part of the instruction)
+          if (n == 0)
+            *c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4], *c, FA, FB, M, sa[H], 0, sb[q]);
+          if (n == 1)
+            *c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + 1], *c, FA, FB, M, sa[H], 1, sb[q]);
+          if (n == 2)
+            *c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + 2], *c, FA, FB, M, sa[H], 2, sb[q]);
+          if (n == 3)
+            *c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[q * 4 + 3], *c, FA, FB, M, sa[H], 3, sb[q]);
+        }
+        if constexpr (decltype(reload)::value && !WIDE) {
+          __builtin_amdgcn_sched_barrier(0);
+          fb[q * 4 + n] = read_b(buf, q * 4 + n);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+  };
+  using No = std::false_type;
+  using Last = std::integral_constant<int, LAST>;
+  // Operands 0 to LAST - 1; leaves the last one read.
+  auto multiply_most = [&](int buf) {
+    unrolled<LAST>([&](auto index) {
+      const V8I next = read_a(buf, decltype(index)::value + 1);
+      __builtin_amdgcn_sched_barrier(0);  // one operand ahead, not more: registers
+      multiply(index, No{}, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      fa = next;
+    });
   };
 
   fetch(first, tile_a[0], tile_b[0]);
   scales[0][threadIdx.x] = next_s;
-  for (int kb = first; kb < last; ++kb) {
-    const int cur = (kb - first) & 1;
-    all_arrived();  // this block's tiles are there, the other buffers free
-    if (kb + 1 < last) fetch(kb + 1, tile_a[cur ^ 1], tile_b[cur ^ 1]);
-    step(tile_a[cur], tile_b[cur], scales[cur]);
-    if (kb + 1 < last) scales[cur ^ 1][threadIdx.x] = next_s;
+  all_arrived();
+  if (first + 1 < last) fetch(first + 1, tile_a[1], tile_b[1]);
+  read_scales(0);
+  if constexpr (WIDE) {
+    widen_b(0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < HN * 4; ++j) fb[j] = read_b(0, j);
   }
+  fa = read_a(0, 0);
+  multiply_most(0);
+  for (int kb = first + 1; kb < last; ++kb) {
+    const int cur = (kb - first) & 1;
+    scales[cur][threadIdx.x] = next_s;
+    all_arrived();  // this block's tiles are there, the last one's all read
+    if (kb + 1 < last) fetch(kb + 1, tile_a[cur ^ 1], tile_b[cur ^ 1]);
+    __builtin_amdgcn_sched_barrier(0);
+    const V8I next = read_a(cur, 0);
+    multiply(Last{}, std::true_type{}, cur);
+    fa = next;
+    read_scales(cur);
+    if constexpr (WIDE) widen_b(cur);
+    multiply_most(cur);
+  }
+  multiply(Last{}, No{}, 0);
 
-  const bool split = g.splits > 1;
-  float* part = split ? g.part + (int64_t)blockIdx.y * g.M * g.N : nullptr;
-#pragma unroll
-  for (int h = 0; h < HM; ++h)
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t row = m0 + wm * TM + h * 64 + kg * 16 + r * 4 + m;
-        if (row >= g.M) continue;
-#pragma unroll
-        for (int q = 0; q < HN; ++q) {
-          const int64_t col = n0 + wn * TN + q * 64 + i16 * 4;
-          if (col >= g.N) continue;
-          const V4F v = {acc[h * 4 + m][q * 4][r], acc[h * 4 + m][q * 4 + 1][r],
-                         acc[h * 4 + m][q * 4 + 2][r], acc[h * 4 + m][q * 4 + 3][r]};
-          if (split) {
-            float* p = part + row * g.N + col;
-            if (col + 4 <= g.N) {
-              __builtin_memcpy(__builtin_assume_aligned(p, 4), &v, 16);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (col + j < g.N) p[j] = v[j];
-            }
-          } else {
-            finish4_any(g, row, col, v);
-          }
-        }
-      }
+  const int64_t row0 = m0 + wm * TM + kg * 16, col0 = n0 + wn * TN + i16 * 4;
+  if (g.splits > 1) {
+    MatmulArgs sum = g;  // plain fp32 sums
+    sum.out = g.part + (int64_t)blockIdx.y * g.M * g.N;
+    sum.z = nullptr;
+    sum.bias = nullptr;
+    finish_tile<float>(sum, acc, row0, col0);
+  } else if (WIDE) {
+    finish_tile<float>(g, acc, row0, col0);
+  } else if (g.dtype == FNO_DTYPE_F16) {
+    finish_tile<_Float16>(g, acc, row0, col0);
+  } else {
+    finish_tile<__bf16>(g, acc, row0, col0);
+  }
 }
 
-// Joins the splits' sums in their order, four columns a thread.
-__global__ __launch_bounds__(256) void join_splits_kernel(MatmulArgs g) {
+// Joins the splits' sums: four columns for `lanes` threads (a power of two up to
+// 64), each of which adds every lanes-th split; a fixed order.
+__global__ __launch_bounds__(256) void join_splits_kernel(MatmulArgs g, int lanes) {
   const int64_t per_row = (g.N + 3) / 4, total = g.M * per_row;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+  const int lane = threadIdx.x & (lanes - 1);
+  const int64_t step = (int64_t)gridDim.x * (256 / lanes);
+  for (int64_t i = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes; i < total; i += step) {
     const int64_t row = i / per_row, col = (i - row * per_row) * 4;
-    const float* p = g.part + row * g.N + col;
+    const bool whole = col + 4 <= g.N;
     V4F v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (col + 4 <= g.N) {
-      for (int s = 0; s < g.splits; ++s, p += g.M * g.N) {
+#pragma unroll 4
+    for (int s = lane; s < g.splits; s += lanes) {
+      const float* p = g.part + ((int64_t)s * g.M + row) * g.N + col;
+      if (whole) {
         float t[4];
         __builtin_memcpy(t, __builtin_assume_aligned(p, 4), 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] += t[j];
-      }
-    } else {
-      for (int s = 0; s < g.splits; ++s, p += g.M * g.N)
+      } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (col + j < g.N) v[j] += p[j];
+      }
     }
-    finish4_any(g, row, col, v);
+    for (int d = 1; d < lanes; d *= 2)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], d);
+    if (lane == 0) finish4_any(g, row, col, v);
   }
 }
 
@@ -395,8 +507,9 @@ MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
   // Few tiles of a long inner axis: split along it, down to four blocks each.
   const int64_t tiles = g.tiles_m * g.tiles_n;
   g.splits = 1;
-  if (tiles < 512 && g.kb >= 8)
-    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / tiles, g.kb / 4));
+  const int64_t fill = p.big ? 256 : 512;  // work-groups that the chip holds at a time
+  if (tiles <= fill / 2 && g.kb >= 8)
+    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(fill / tiles, g.kb / 4));
   g.kb_per_split = (int)fp8_cdiv(g.kb, g.splits);
   g.splits = (int)fp8_cdiv(g.kb, g.kb_per_split);
   return p;
@@ -434,8 +547,13 @@ hipError_t launch_matmul(void* ctx) {
     L.fb == FNO_FP8_E4M3 ? launch_formats<1, 0>(L) : launch_formats<1, 1>(L);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || L.p.g.splits == 1) return e;
-  const int64_t groups = fp8_cdiv(L.p.g.M * fp8_cdiv(L.p.g.N, 4), 256);
-  join_splits_kernel<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 20)), dim3(256), 0, L.stream>>>(L.p.g);
+  // a thread for four columns where that fills the chip, else up to one for each
+  // four splits
+  const int64_t quads = L.p.g.M * fp8_cdiv(L.p.g.N, 4);
+  int lanes = 1;
+  while (lanes < 64 && lanes * 8 <= L.p.g.splits && quads * lanes < 128 * 1024) lanes *= 2;
+  const int64_t groups = fp8_cdiv(quads * lanes, 256);
+  join_splits_kernel<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 20)), dim3(256), 0, L.stream>>>(L.p.g, lanes);
   return hipGetLastError();
 }
 

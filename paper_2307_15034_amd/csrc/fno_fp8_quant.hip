@@ -1,6 +1,7 @@
 // Rounding to 8-bit codes with a scale for each block of 128, along the rows,
 // along the columns (into the transpose), or for tiles, in one pass over x.
 #include <algorithm>
+#include <type_traits>
 
 #include "fno_fp8.h"
 #include "fno_host.h"
@@ -61,59 +62,218 @@ __device__ __forceinline__ void put_scale(void* out, int64_t at, const BlockScal
     static_cast<float*>(out)[at] = s.scale;
 }
 
+// The 8 x 8 values of a thread.  16-bit values without an activation stay in
+// pairs: sizes are compared as whole numbers, two at a time, and with powers of
+// two the conversion takes pairs and divides them itself (exactly).  Three
+// operations a value for both directions, where single floats take thirteen,
+// which the passes are bound by (33.5 M values both ways: MEASURE).
+template <typename T, int FMT, bool ACT, bool POW2>
+struct Values {
+  static constexpr bool PAIRS = sizeof(T) == 2 && !ACT && POW2;
+  typedef T T2 __attribute__((ext_vector_type(2)));
+  typedef short S2 __attribute__((ext_vector_type(2)));
+  typedef unsigned short U2 __attribute__((ext_vector_type(2)));
+  unsigned p[PAIRS ? 8 : 1][4];  // two values each
+  float f[PAIRS ? 1 : 8][8];
+
+  __device__ __forceinline__ void set(int i, const T (&t)[8], int act) {
+    if constexpr (PAIRS) {
+      __builtin_memcpy(p[i], t, sizeof(t));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = ACT ? act_any<T>((float)t[j], act) : (float)t[j];
+    }
+  }
+  __device__ __forceinline__ float at(int i, int j) const {
+    if constexpr (PAIRS)
+      return number((unsigned short)(j & 1 ? p[i][j / 2] >> 16 : p[i][j / 2] & 0xffffu));
+    else
+      return f[i][j];
+  }
+  // The same values, of which the compiler does not know that: what is formed from
+  // them on a rare path is not formed before it, and not kept behind it.
+  __device__ __forceinline__ Values apart() const {
+    Values v = *this;
+    if constexpr (PAIRS) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(v.p[i][j]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(v.f[i][j]));
+    }
+    return v;
+  }
+  // Largest finite sizes.
+  static constexpr unsigned short INF16 = std::is_same_v<T, _Float16> ? 0x7c00 : 0x7f80;
+  static __device__ __forceinline__ U2 size2(unsigned v) { return __builtin_bit_cast(U2, v & 0x7fff7fffu); }
+  static __device__ __forceinline__ float number(unsigned short bits) {
+    T v;
+    __builtin_memcpy(&v, &bits, 2);
+    return (float)v;
+  }
+  __device__ __forceinline__ float row_top(int i) const {
+    float m = 0.0f;
+    bool odd;
+    if constexpr (PAIRS) {
+      const U2 a = __builtin_elementwise_max(__builtin_elementwise_max(size2(p[i][0]), size2(p[i][1])),
+                                             __builtin_elementwise_max(size2(p[i][2]), size2(p[i][3])));
+      const unsigned short b = a[0] > a[1] ? a[0] : a[1];
+      odd = b >= INF16;
+      m = number(b);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, __builtin_fabsf(f[i][j]));
+      odd = !(m <= 3.402823466e+38f);
+    }
+    if (odd) {
+      const Values v = apart();
+      m = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, finite_size(v.at(i, j)));
+    }
+    return m;
+  }
+  __device__ __forceinline__ void col_tops(float (&m)[8]) const {
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      if constexpr (PAIRS) {
+        U2 a = size2(p[0][j / 2]);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) a = __builtin_elementwise_max(a, size2(p[i][j / 2]));
+        odd |= a[0] >= INF16 || a[1] >= INF16;
+        m[j] = number(a[0]);
+        m[j + 1] = number(a[1]);
+      } else {
+        m[j] = m[j + 1] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          m[j] = __builtin_fmaxf(m[j], __builtin_fabsf(f[i][j]));
+          m[j + 1] = __builtin_fmaxf(m[j + 1], __builtin_fabsf(f[i][j + 1]));
+        }
+        odd |= !(m[j] <= 3.402823466e+38f) || !(m[j + 1] <= 3.402823466e+38f);
+      }
+    }
+    if (odd) {
+      const Values v = apart();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[j] = __builtin_fmaxf(m[j], finite_size(v.at(i, j)));
+      }
+    }
+  }
+  // Two pairs to four codes, divided by 2^e.
+  static __device__ __forceinline__ unsigned four(unsigned pa, unsigned pb, float by) {
+    T2 a, b;
+    __builtin_memcpy(&a, &pa, 4);
+    __builtin_memcpy(&b, &pb, 4);
+    S2 r = {0, 0};
+    if constexpr (std::is_same_v<T, _Float16>) {
+      if constexpr (FMT == FNO_FP8_E4M3) {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, a, by, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, b, by, true);
+      } else {
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f16(r, a, by, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f16(r, b, by, true);
+      }
+    } else if constexpr (sizeof(T) == 2) {
+      if constexpr (FMT == FNO_FP8_E4M3) {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, a, by, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, b, by, true);
+      } else {
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, a, by, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, b, by, true);
+      }
+    }
+    return __builtin_bit_cast(unsigned, r);
+  }
+  __device__ __forceinline__ uint2 row_codes(int i, const BlockScale& s) const {
+    if constexpr (PAIRS) {
+      const float by = __builtin_bit_cast(float, s.byte << 23);
+      return uint2{four(p[i][0], p[i][1], by), four(p[i][2], p[i][3], by)};
+    }
+    return uint2{pack4<FMT>(at(i, 0) * s.inv, at(i, 1) * s.inv, at(i, 2) * s.inv, at(i, 3) * s.inv),
+                 pack4<FMT>(at(i, 4) * s.inv, at(i, 5) * s.inv, at(i, 6) * s.inv, at(i, 7) * s.inv)};
+  }
+  __device__ __forceinline__ unsigned column2(int i, int j) const {  // rows i and i + 1
+    return __builtin_amdgcn_perm(p[i + 1][j / 2], p[i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+  }
+  __device__ __forceinline__ uint2 col_codes(int j, const BlockScale& s) const {
+    if constexpr (PAIRS) {
+      const float by = __builtin_bit_cast(float, s.byte << 23);
+      return uint2{four(column2(0, j), column2(2, j), by), four(column2(4, j), column2(6, j), by)};
+    }
+    return uint2{pack4<FMT>(at(0, j) * s.inv, at(1, j) * s.inv, at(2, j) * s.inv, at(3, j) * s.inv),
+                 pack4<FMT>(at(4, j) * s.inv, at(5, j) * s.inv, at(6, j) * s.inv, at(7, j) * s.inv)};
+  }
+};
+
 // A work-group takes CG x 8 columns of 2048 / CG rows, a thread 8 x 8 of them:
 // lanes next to each other hold neighbouring columns of the same rows.  A row's
 // blocks are joined within a wave; a column's blocks of 128 rows are 16 threads,
-// within a wave up to CG = 4, over two or four waves beyond.
-template <typename T, int FMT, int CG>
+// within a wave up to CG = 4, over two or four waves beyond.  CG = 64, whose waves
+// read 1 KB of a row at a time, is for codes of rows alone.
+template <typename T, int FMT, int CG, bool ACT, bool POW2>
 __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
   constexpr int RG = QT / CG;                    // row groups of 8
-  constexpr int BLOCKS = RG / 16;                // blocks of 128 rows
+  constexpr bool COLUMNS = CG <= 16;
+  constexpr int BLOCKS = COLUMNS ? RG / 16 : 1;  // blocks of 128 rows
   constexpr int WAVES = CG <= 4 ? 1 : CG / 4;    // waves of a column's block
-  __shared__ float red[2][4][CG * 8];
+  constexpr int BL = CG < 16 ? CG : 16;          // lanes of a row's block
+  __shared__ float red[2][4][COLUMNS ? CG * 8 : 1];
+  __shared__ __attribute__((aligned(16))) uint8_t turned[COLUMNS ? BLOCKS * CG * 8 * kBlock : 16];
   const int cg = threadIdx.x % CG, rg = threadIdx.x / CG, wave = threadIdx.x >> 6;
   const int64_t tiles_c = (a.cols + CG * 8 - 1) / (CG * 8);
-  const int64_t tr = blockIdx.x / tiles_c;
-  const int c0 = (int)(blockIdx.x - tr * tiles_c) * (CG * 8) + cg * 8;
+  // A die's work-groups (every eighth) take consecutive tiles: what they write of a
+  // line of memory meets in one cache.
+  const int64_t each = gridDim.x >> 3;
+  const int64_t id = blockIdx.x < each * 8 ? (blockIdx.x & 7) * each + (blockIdx.x >> 3) : blockIdx.x;
+  const int64_t tr = id / tiles_c;
+  const int c0 = (int)(id - tr * tiles_c) * (CG * 8) + cg * 8;
   const int64_t r0 = tr * (RG * 8) + rg * 8;
-  const bool pow2 = a.pow2;
-  float v[8][8];
+  constexpr bool pow2 = POW2;
+  Values<T, FMT, ACT, POW2> v;
   const T* x = static_cast<const T*>(a.x);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const bool on = r0 + i < a.rows;
     const T* row = x + (r0 + i) * a.cols;
+    T t[8];
     if (on && c0 + 8 <= a.cols) {
-      T t[8];
       __builtin_memcpy(t, __builtin_assume_aligned(row + c0, sizeof(T)), sizeof(t));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = (float)t[j];
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = on && c0 + j < a.cols ? (float)row[c0 + j] : 0.0f;
+      for (int j = 0; j < 8; ++j) {
+        t[j] = (T)0.0f;  // as behind an activation
+        if (on && c0 + j < a.cols) t[j] = row[c0 + j];
+      }
     }
-  }
-  if (a.act != FNO_NORM_ACT_NONE) {  // both are 0 at 0
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = act_any<T>(v[i][j], a.act);
+    v.set(i, t, a.act);
   }
   const int64_t block_r = (r0 >> 7), block_c = c0 >> 7;
   // Largest sizes and sums of the columns' blocks.
   float top[8];
-  if (a.codes_t || a.tile || a.part) {
+  if (COLUMNS && (a.codes_t || a.tile || a.part)) {
     float sum[8];
+    v.col_tops(top);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float m = 0.0f, s = 0.0f;
+    for (int j = 0; j < 8; ++j) top[j] = far_join<CG>(top[j], false);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        m = __builtin_fmaxf(m, finite_size(v[i][j]));
-        s += v[i][j];
+    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    if (a.part) {
+      const auto w = v.apart();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[j] += w.at(i, j);
+        sum[j] = far_join<CG>(sum[j], true);
       }
-      top[j] = far_join<CG>(m, false);
-      sum[j] = a.part ? far_join<CG>(s, true) : 0.0f;
     }
     if constexpr (WAVES > 1) {
       if ((threadIdx.x & 63) < CG) {
@@ -147,69 +307,102 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
     float m = top[0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) m = __builtin_fmaxf(m, top[j]);
-    one = block_scale<FMT>(near_max<CG>(m), pow2);
+    one = block_scale<FMT>(near_max<BL>(m), pow2);
     if (threadIdx.x == 0) {
       if (a.codes) put_scale(a.scale, block_c * a.blocks_r + block_r, one, pow2);
       if (a.codes_t) put_scale(a.scale_t, block_r * a.blocks_c + block_c, one, pow2);
     }
   }
   if (a.codes) {
+    // each lane stores 8 / CG (at least one) of its rows' scales
+    constexpr int EACH = CG >= 8 ? 1 : 8 / CG;
+    BlockScale mine[EACH];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       BlockScale s = one;
       if (!a.tile) {
-        float m = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = __builtin_fmaxf(m, finite_size(v[i][j]));
-        s = block_scale<FMT>(near_max<CG>(m), pow2);
+        s = block_scale<FMT>(near_max<BL>(v.row_top(i)), pow2);
+        if (EACH == 1 ? cg % BL == i : cg == i / EACH) mine[i % EACH] = s;
       }
-      if (r0 + i < a.rows) {
-        if (!a.tile && cg == 0) put_scale(a.scale, block_c * a.rows + r0 + i, s, pow2);
-        if (c0 < a.pitch) {
-          uint2 q;
-          q.x = pack4<FMT>(v[i][0] * s.inv, v[i][1] * s.inv, v[i][2] * s.inv, v[i][3] * s.inv);
-          q.y = pack4<FMT>(v[i][4] * s.inv, v[i][5] * s.inv, v[i][6] * s.inv, v[i][7] * s.inv);
-          *reinterpret_cast<uint2*>(a.codes + (r0 + i) * a.pitch + c0) = q;
-        }
+      if (r0 + i < a.rows && c0 < a.pitch) {
+        *reinterpret_cast<uint2*>(a.codes + (r0 + i) * a.pitch + c0) = v.row_codes(i, s);
+      }
+    }
+    if (!a.tile && cg % BL < 8) {
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) {
+        const int64_t row = r0 + cg % BL * EACH + k;
+        if (row < a.rows && block_c < a.blocks_c) put_scale(a.scale, block_c * a.rows + row, mine[k], pow2);
       }
     }
   }
-  if (a.codes_t && r0 < a.pitch_t) {
+  if (COLUMNS && a.codes_t) {
+    // Through LDS, so that 128 codes of a column leave as one run.  A column's
+    // pieces of 8 are exchanged by the bits of its group of columns (banks).
+    const int block = rg / 16, piece = rg % 16;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const BlockScale s = a.tile ? one : block_scale<FMT>(top[j], pow2);
-      if (c0 + j < a.cols) {
-        if (!a.tile && rg % 16 == 0 && r0 < a.rows)
-          put_scale(a.scale_t, block_r * a.cols + c0 + j, s, pow2);
-        uint2 q;
-        q.x = pack4<FMT>(v[0][j] * s.inv, v[1][j] * s.inv, v[2][j] * s.inv, v[3][j] * s.inv);
-        q.y = pack4<FMT>(v[4][j] * s.inv, v[5][j] * s.inv, v[6][j] * s.inv, v[7][j] * s.inv);
-        *reinterpret_cast<uint2*>(a.codes_t + (int64_t)(c0 + j) * a.pitch_t + r0) = q;
+      if (!a.tile && piece == 0 && r0 < a.rows && c0 + j < a.cols)
+        put_scale(a.scale_t, block_r * a.cols + c0 + j, s, pow2);
+      *reinterpret_cast<uint2*>(turned + ((block * CG + cg) * 8 + j) * kBlock + (piece ^ cg) * 8) =
+          v.col_codes(j, s);
+    }
+    __syncthreads();
+    const int64_t first = tr * (RG * 8);
+    const int cfirst = c0 - cg * 8;
+#pragma unroll
+    for (int i = 0; i < BLOCKS * CG * 8 * 8 / QT; ++i) {
+      const int t = threadIdx.x + i * QT, at = t & 7, line = t >> 3;  // line: block, column
+      const int col = line % (CG * 8), of = col >> 3;
+      const int64_t row = first + (line / (CG * 8)) * kBlock + at * 16;
+      if (cfirst + col < a.cols && row < a.pitch_t) {
+        uint4 q = *reinterpret_cast<const uint4*>(turned + line * kBlock + ((2 * at ^ of) & 14) * 8);
+        if (of & 1) q = uint4{q.z, q.w, q.x, q.y};
+        *reinterpret_cast<uint4*>(a.codes_t + (int64_t)(cfirst + col) * a.pitch_t + row) = q;
       }
     }
   }
 }
 
 // Sums of the units' column sums, in double.
-constexpr int kSumCols = 16, kSumRows = 64;
-__global__ __launch_bounds__(kSumCols* kSumRows) void col_sum_kernel(const float* part, float* out,
-                                                                     int64_t units, int cols) {
-  __shared__ double red[kSumRows][kSumCols + 1];
-  const int col = threadIdx.x % kSumCols, lane = threadIdx.x / kSumCols;
-  const int64_t c = (int64_t)blockIdx.x * kSumCols + col;
-  double s = 0.0;
-  if (c < cols) {
+constexpr int kSumCols = 16, kSumLanes = 256;  // four columns a thread
+__global__ __launch_bounds__(kSumCols / 4 * kSumLanes) void col_sum_kernel(const float* part, float* out,
+                                                                           int64_t units, int cols) {
+  __shared__ double red[kSumLanes / 16][kSumCols];
+  const int quad = threadIdx.x % (kSumCols / 4), lane = threadIdx.x / (kSumCols / 4);
+  const int64_t c = (int64_t)blockIdx.x * kSumCols + quad * 4;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  if (c + 4 <= cols) {
 #pragma unroll 4
-    for (int64_t i = lane; i < units; i += kSumRows) s += (double)part[i * cols + c];
-  }
-  red[lane][col] = s;
-  __syncthreads();
+    for (int64_t i = lane; i < units; i += kSumLanes) {
+      float t[4];
+      __builtin_memcpy(t, __builtin_assume_aligned(part + i * cols + c, 4), sizeof(t));
 #pragma unroll
-  for (int d = kSumRows / 2; d > 0; d >>= 1) {
-    if (lane < d) red[lane][col] += red[lane + d][col];
-    __syncthreads();
+      for (int j = 0; j < 4; ++j) s[j] += (double)t[j];
+    }
+  } else {
+    for (int64_t i = lane; i < units; i += kSumLanes)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j < cols) s[j] += (double)part[i * cols + c + j];
   }
-  if (lane == 0 && c < cols) out[c] = (float)red[0][col];
+#pragma unroll
+  for (int d = 4; d < 64; d *= 2)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] += __shfl_xor(s[j], d);
+  if (lane % 16 == 0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) red[lane / 16][quad * 4 + j] = s[j];
+  }
+  __syncthreads();
+  const int64_t mine = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
+  if (threadIdx.x < kSumCols && mine < cols) {
+    double t = red[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < kSumLanes / 16; ++w) t += red[w][threadIdx.x];
+    out[mine] = (float)t;
+  }
 }
 
 // --------------------------------------------------------------------------
@@ -240,11 +433,18 @@ struct QuantLaunch {
 template <typename T, int FMT, int CG>
 hipError_t launch_tiles(const QuantLaunch& L) {
   const int64_t grid = fp8_cdiv(L.a.rows, QT / CG * 8) * fp8_cdiv(L.a.cols, CG * 8);
-  quantize_kernel<T, FMT, CG><<<dim3((unsigned)grid), dim3(QT), 0, L.stream>>>(L.a);
+  const dim3 g((unsigned)grid), t(QT);
+  if (L.a.act == FNO_NORM_ACT_NONE)
+    L.a.pow2 ? quantize_kernel<T, FMT, CG, false, true><<<g, t, 0, L.stream>>>(L.a)
+             : quantize_kernel<T, FMT, CG, false, false><<<g, t, 0, L.stream>>>(L.a);
+  else
+    L.a.pow2 ? quantize_kernel<T, FMT, CG, true, true><<<g, t, 0, L.stream>>>(L.a)
+             : quantize_kernel<T, FMT, CG, true, false><<<g, t, 0, L.stream>>>(L.a);
   return hipGetLastError();
 }
 template <typename T, int FMT>
 hipError_t launch_width(const QuantLaunch& L) {
+  if (!L.a.tile && !L.a.codes_t && !L.a.part && L.a.cols >= 512) return launch_tiles<T, FMT, 64>(L);
   if (L.a.tile || L.a.cols > 64) return launch_tiles<T, FMT, 16>(L);
   if (L.a.cols > 32) return launch_tiles<T, FMT, 8>(L);
   if (L.a.cols > 16) return launch_tiles<T, FMT, 4>(L);
@@ -261,7 +461,7 @@ hipError_t launch_quantize(void* ctx) {
                        : L.dtype == FNO_DTYPE_F16 ? launch_format<_Float16>(L)
                                                   : launch_format<__bf16>(L);
   if (e != hipSuccess || !L.col_sums) return e;
-  col_sum_kernel<<<dim3((unsigned)fp8_cdiv(L.a.cols, kSumCols)), dim3(kSumCols * kSumRows), 0, L.stream>>>(
+  col_sum_kernel<<<dim3((unsigned)fp8_cdiv(L.a.cols, kSumCols)), dim3(kSumCols / 4 * kSumLanes), 0, L.stream>>>(
       L.a.part, L.col_sums, L.a.blocks_r, L.a.cols);
   return hipGetLastError();
 }
