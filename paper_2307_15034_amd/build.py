@@ -21,7 +21,8 @@ OBJ = os.path.join(HERE, "_build")
 SOURCES = ["fno_kernels.hip", "fno_fast.hip", "fno_chain.hip", "fno_slab.hip", "fno_gemm.hip",
            "fno_wide2.hip", "fno_line.hip", "fno_any.hip", "fno_any32.hip", "fno_noalloc.hip", "fno_block.hip", "fno_norm.hip",
            "fno_norm_res.hip", "fno_adamw.hip", "fno_rownorm.hip", "fno_rownorm_fwd.hip",
-           "fno_rownorm_bwd.hip", "fno_fp8_quant.hip", "fno_fp8_gemm.hip", "fno_plan.cpp"]
+           "fno_rownorm_bwd_f32.hip", "fno_rownorm_bwd_f16.hip", "fno_rownorm_bwd_bf16.hip",
+           "fno_fp8_quant.hip", "fno_fp8_gemm.hip", "fno_plan.cpp"]
 ARCH = "gfx950"
 
 

@@ -246,15 +246,15 @@ __device__ __forceinline__ float scale_of(int four, int m) {
   return __builtin_bit_cast(float, b == 255u ? 0x7fc00000u : b ? b << 23 : 0x00400000u);
 }
 
-template <int FA, int FB, bool F32S, bool WIDE, int BM, int BN, int WGM, int WGN>
-__global__ __launch_bounds__(64 * WGM * WGN) void gemm_kernel(MatmulArgs g) {
+template <int FA, int FB, bool F32S, bool WIDE, int BM, int BN, int WGM, int WGN, int STAGES = 2>
+__global__ __launch_bounds__(64 * WGM * WGN, STAGES == 1 ? 3 : 1) void gemm_kernel(MatmulArgs g) {
   constexpr int THREADS = 64 * WGM * WGN;
   constexpr int TM = BM / WGM, TN = BN / WGN;  // a wave's part
   constexpr int HM = TM / 64, HN = TN / 64;
-  __shared__ __attribute__((aligned(16))) uint8_t tile_a[2][BM * kBlock], tile_b[2][BN * kBlock];
+  __shared__ __attribute__((aligned(16))) uint8_t tile_a[STAGES][BM * kBlock], tile_b[STAGES][BN * kBlock];
   using S = std::conditional_t<F32S, float, uint8_t>;
-  static_assert(BM + BN == THREADS, "a scale for each thread");
-  __shared__ __attribute__((aligned(16))) S scales[2][BM + BN];
+  constexpr int SN = (BM + BN + THREADS - 1) / THREADS;  // scales a thread brings
+  __shared__ __attribute__((aligned(16))) S scales[STAGES][BM + BN];
   const int lane = threadIdx.x & 63, i16 = lane & 15, kg = lane >> 4;
   const int wave = threadIdx.x >> 6, wm = wave / WGN, wn = wave % WGN;
   int64_t tm, tn;
@@ -269,20 +269,29 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_kernel(MatmulArgs g) {
 #pragma unroll
     for (int j = 0; j < HN * 4; ++j) acc[i][j] = V4F{0.0f, 0.0f, 0.0f, 0.0f};
 
-  // Thread t brings the scales of row t of A's tile, or row t - BM of B's.
-  const bool of_a = threadIdx.x < BM;
-  int64_t srow = of_a ? m0 + threadIdx.x : n0 + threadIdx.x - BM;
-  const int64_t most = (of_a ? g.M : g.N) - 1;
-  srow = (srow < most ? srow : most) >> (of_a ? g.shift_a : g.shift_b);
-  const uint64_t sbase = of_a ? (uint64_t)g.scale_a : (uint64_t)g.scale_b;
-  const int64_t sstep = of_a ? g.scales_a : g.scales_b;
-  uint64_t sat = sbase + (uint64_t)(srow + first * sstep) * sizeof(S);
+  // Thread t brings the scales of rows t, t + THREADS, ... of A's tile and then B's.
+  uint64_t sat[SN];
+  int64_t sstep[SN];
+  S next_s[SN];
+#pragma unroll
+  for (int i = 0; i < SN; ++i) {
+    const int t = threadIdx.x + i * THREADS;
+    const bool of_a = t < BM;
+    int64_t row = of_a ? m0 + t : n0 + t - BM;
+    const int64_t most = (of_a ? g.M : g.N) - 1;
+    row = (row < most ? row : most) >> (of_a ? g.shift_a : g.shift_b);
+    sstep[i] = of_a ? g.scales_a : g.scales_b;
+    sat[i] = (of_a ? (uint64_t)g.scale_a : (uint64_t)g.scale_b) +
+             (uint64_t)(row + first * sstep[i]) * sizeof(S);
+  }
   const TileLoad<BM, THREADS> from_a(g.a, m0, g.M, g.pitch);
   const TileLoad<BN, THREADS> from_b(g.b, n0, g.N, g.pitch);
-  S next_s;
   auto fetch = [&](int kb, uint8_t* a, uint8_t* b) {
-    next_s = *reinterpret_cast<const __attribute__((address_space(1))) S*>(sat);
-    sat += (uint64_t)sstep * sizeof(S);
+#pragma unroll
+    for (int i = 0; i < SN; ++i) {
+      next_s[i] = *reinterpret_cast<const __attribute__((address_space(1))) S*>(sat[i]);
+      sat[i] += (uint64_t)sstep[i] * sizeof(S);
+    }
     from_a.fetch(kb, a);
     from_b.fetch(kb, b);
   };
@@ -387,10 +396,16 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_kernel(MatmulArgs g) {
     });
   };
 
+  auto keep_scales = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < SN; ++i)
+      if ((BM + BN) % THREADS == 0 || threadIdx.x + i * THREADS < BM + BN)
+        scales[buf][threadIdx.x + i * THREADS] = next_s[i];
+  };
   fetch(first, tile_a[0], tile_b[0]);
-  scales[0][threadIdx.x] = next_s;
+  keep_scales(0);
   all_arrived();
-  if (first + 1 < last) fetch(first + 1, tile_a[1], tile_b[1]);
+  if (STAGES > 1 && first + 1 < last) fetch(first + 1, tile_a[STAGES - 1], tile_b[STAGES - 1]);
   read_scales(0);
   if constexpr (WIDE) {
     widen_b(0);
@@ -400,11 +415,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_kernel(MatmulArgs g) {
   }
   fa = read_a(0, 0);
   multiply_most(0);
-  for (int kb = first + 1; kb < last; ++kb) {
-    const int cur = (kb - first) & 1;
-    scales[cur][threadIdx.x] = next_s;
+  for (int kb = first + 1; STAGES > 1 && kb < last; ++kb) {  // (one stage: one block)
+    const int cur = (kb - first) & (STAGES - 1);
+    keep_scales(cur);
     all_arrived();  // this block's tiles are there, the last one's all read
-    if (kb + 1 < last) fetch(kb + 1, tile_a[cur ^ 1], tile_b[cur ^ 1]);
+    if (kb + 1 < last) fetch(kb + 1, tile_a[cur ^ (STAGES - 1)], tile_b[cur ^ (STAGES - 1)]);
     __builtin_amdgcn_sched_barrier(0);
     const V8I next = read_a(cur, 0);
     multiply(Last{}, std::true_type{}, cur);
@@ -482,9 +497,10 @@ fno_status check_desc(const fno_fp8_matmul_desc* d) {
   return FNO_OK;
 }
 
+enum Tile { TILE_128, TILE_256, TILE_NARROW };
 struct MatmulPlan {
   MatmulArgs g;
-  bool big;
+  Tile tile;
 };
 
 MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
@@ -500,14 +516,21 @@ MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
   g.scales_b = g.shift_b ? fp8_cdiv(g.N, kBlock) : g.N;
   g.act = d.activation;
   g.dtype = d.out_dtype;
-  p.big = d.scale_type == FNO_SCALE_POW2 && fp8_cdiv(g.M, 256) * fp8_cdiv(g.N, 256) >= 192;
-  const int side = p.big ? 256 : 128;
-  g.tiles_m = fp8_cdiv(g.M, side);
-  g.tiles_n = fp8_cdiv(g.N, side);
+  // 256 x 256 where such tiles fill the chip's 256 compute units; 256 x 64 of one
+  // stage where a row of codes is one block and columns are few (the work is in
+  // the rows' bytes: more work-groups at a time); else 128 x 128.
+  const bool pow2 = d.scale_type == FNO_SCALE_POW2;
+  const int64_t of256 = fp8_cdiv(g.M, 256) * fp8_cdiv(g.N, 256);
+  p.tile = g.kb == 1 && g.N <= 64 && g.M > 128 ? TILE_NARROW
+           : pow2 && of256 >= 192 && g.N > 128 ? TILE_256
+                                               : TILE_128;
+  const int bm = p.tile == TILE_128 ? 128 : 256, bn = p.tile == TILE_256 ? 256 : p.tile == TILE_NARROW ? 64 : 128;
+  g.tiles_m = fp8_cdiv(g.M, bm);
+  g.tiles_n = fp8_cdiv(g.N, bn);
   // Few tiles of a long inner axis: split along it, down to four blocks each.
   const int64_t tiles = g.tiles_m * g.tiles_n;
   g.splits = 1;
-  const int64_t fill = p.big ? 256 : 512;  // work-groups that the chip holds at a time
+  const int64_t fill = p.tile == TILE_256 ? 256 : 512;  // work-groups that the chip holds at a time
   if (tiles <= fill / 2 && g.kb >= 8)
     g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(fill / tiles, g.kb / 4));
   g.kb_per_split = (int)fp8_cdiv(g.kb, g.splits);
@@ -522,20 +545,25 @@ struct MatmulLaunch {
   hipStream_t stream;
 };
 
+template <int FA, int FB, bool F32S, bool WIDE>
+void launch_tile(const MatmulLaunch& L, dim3 grid) {
+  const MatmulArgs& g = L.p.g;
+  if (L.p.tile == TILE_NARROW) {
+    gemm_kernel<FA, FB, F32S, WIDE, 256, 64, 4, 1, 1><<<grid, dim3(256), 0, L.stream>>>(g);
+  } else if (L.p.tile == TILE_256) {
+    if constexpr (!F32S) gemm_kernel<FA, FB, F32S, WIDE, 256, 256, 2, 4><<<grid, dim3(512), 0, L.stream>>>(g);
+  } else {
+    gemm_kernel<FA, FB, F32S, WIDE, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g);
+  }
+}
 template <int FA, int FB>
 void launch_formats(const MatmulLaunch& L) {
   const MatmulArgs& g = L.p.g;
   const dim3 grid((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits);
-  const bool wide = g.dtype == FNO_DTYPE_F32;
-  if (L.f32s)
-    wide ? gemm_kernel<FA, FB, true, true, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g)
-         : gemm_kernel<FA, FB, true, false, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g);
-  else if (L.p.big)
-    wide ? gemm_kernel<FA, FB, false, true, 256, 256, 2, 4><<<grid, dim3(512), 0, L.stream>>>(g)
-         : gemm_kernel<FA, FB, false, false, 256, 256, 2, 4><<<grid, dim3(512), 0, L.stream>>>(g);
+  if (g.dtype == FNO_DTYPE_F32)
+    L.f32s ? launch_tile<FA, FB, true, true>(L, grid) : launch_tile<FA, FB, false, true>(L, grid);
   else
-    wide ? gemm_kernel<FA, FB, false, true, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g)
-         : gemm_kernel<FA, FB, false, false, 128, 128, 2, 2><<<grid, dim3(256), 0, L.stream>>>(g);
+    L.f32s ? launch_tile<FA, FB, true, false>(L, grid) : launch_tile<FA, FB, false, false>(L, grid);
 }
 
 hipError_t launch_matmul(void* ctx) {

@@ -36,12 +36,26 @@ struct RowNormArgs {
 
 // Threads of a team (a row's) and the vectors that each holds.  Teams of up to a
 // wave share work-groups of 256, larger ones are a work-group each.
-constexpr int row_threads(int team) { return team < 256 ? 256 : team; }
+constexpr int row_threads(int team) { return team <= 64 ? 256 : team; }
+// Work-groups of 1024 threads have 128 registers a thread: parameters are read
+// again for each row there, and no row is loaded ahead.
+constexpr bool row_lean(int team) { return team >= 1024; }
+#define FNO_ROW_TEAMS(DO) \
+  DO(4, 1) DO(8, 1) DO(16, 1) DO(32, 1) DO(64, 1) DO(128, 1) DO(256, 1) DO(512, 1) DO(1024, 1) \
+  DO(1024, 2) DO(1024, 4)
 
-hipError_t launch_row_norm_fwd(const RowNormArgs& a, int dtype, int team, int vecs, unsigned grid,
-                               hipStream_t s);
-hipError_t launch_row_norm_bwd(const RowNormArgs& a, int dtype, bool post, bool pre, int team,
-                               int vecs, unsigned grid, hipStream_t s);
+struct RowLaunchSize {
+  int team, vecs, mode;  // mode: RowMode
+  unsigned grid;
+};
+hipError_t launch_row_norm_fwd(const RowNormArgs& a, int dtype, const RowLaunchSize& l, hipStream_t s);
+// The backward's kernels, by type (one source each: they are many).
+hipError_t launch_row_norm_bwd_f32(const RowNormArgs& a, bool post, bool pre, const RowLaunchSize& l,
+                                   hipStream_t s);
+hipError_t launch_row_norm_bwd_f16(const RowNormArgs& a, bool post, bool pre, const RowLaunchSize& l,
+                                   hipStream_t s);
+hipError_t launch_row_norm_bwd_bf16(const RowNormArgs& a, bool post, bool pre, const RowLaunchSize& l,
+                                    hipStream_t s);
 
 // --------------------------------------------------------------------------
 // Device code
@@ -54,27 +68,48 @@ struct RowVec {
   T e[kRowVec<T>];
 };
 
-// Vector v of a row of C values at `row`; zeros behind the row's end and where
-// `on` is false.  Rows start at any element.
-template <typename T>
-__device__ __forceinline__ RowVec<T> load_row_vec(const T* row, int v, int C, bool on) {
+// How a row's vectors lie: all whole, the last one short, or the row shorter than
+// a vector.
+enum RowMode { ROW_WHOLE, ROW_TAIL, ROW_SHORT };
+
+// Vector v (of the row's values from v V on) of a row of C values at `row`; zeros
+// behind the row's end.  Rows start at any element.  A short last vector is read
+// as the row's last V values and shifted, so that loads need no branch: they are
+// issued a row ahead, and a branch would wait for them.
+template <typename T, int MODE>
+__device__ __forceinline__ RowVec<T> load_row_vec(const T* row, int v, int C, int valid) {
   constexpr int V = kRowVec<T>;
   RowVec<T> r;
-  if (on && (v + 1) * V <= C) {
-    __builtin_memcpy(&r, __builtin_assume_aligned(row + v * V, sizeof(T)), sizeof(r));
+  if constexpr (MODE == ROW_WHOLE) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.e[j] = (T)0.0f;
+    if (valid) __builtin_memcpy(&r, __builtin_assume_aligned(row + v * V, sizeof(T)), sizeof(r));
+  } else if constexpr (MODE == ROW_TAIL) {
+    const int at = v * V < C - V ? v * V : C - V;
+    const int cut = (V - valid) * (int)sizeof(T) * 8;  // bits in front of the vector's own
+    struct {
+      uint64_t lo, hi;
+    } w;
+    __builtin_memcpy(&w, __builtin_assume_aligned(row + at, sizeof(T)), sizeof(w));
+    const int s = cut & 63;
+    const uint64_t up = (w.hi << 1) << (63 - s);
+    const uint64_t lo = cut >= 64 ? w.hi >> s : (w.lo >> s) | up, hi = cut >= 64 ? 0 : w.hi >> s;
+    w.lo = cut >= 128 ? 0 : lo;
+    w.hi = hi;
+    __builtin_memcpy(&r, &w, sizeof(r));
   } else {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       r.e[j] = (T)0.0f;
-      if (on && v * V + j < C) r.e[j] = row[v * V + j];
+      if (v * V + j < C) r.e[j] = row[v * V + j];
     }
   }
   return r;
 }
-template <typename T>
+template <typename T, int MODE>
 __device__ __forceinline__ void store_row_vec(T* row, int v, int C, const RowVec<T>& r) {
   constexpr int V = kRowVec<T>;
-  if ((v + 1) * V <= C) {
+  if (MODE == ROW_WHOLE || (v + 1) * V <= C) {
     __builtin_memcpy(__builtin_assume_aligned(row + v * V, sizeof(T)), &r, sizeof(r));
   } else {
 #pragma unroll
@@ -88,6 +123,10 @@ __device__ __forceinline__ void store_row_vec(T* row, int v, int C, const RowVec
 template <int V>
 __device__ __forceinline__ void load_param(float (&out)[V], const float* p, int v, int C,
                                            float other) {
+  if (p && (v + 1) * V <= C) {
+    __builtin_memcpy(out, __builtin_assume_aligned(p + v * V, 4), sizeof(out));
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < V; ++j) out[j] = v * V + j < C ? (p ? p[v * V + j] : other) : 0.0f;
 }
@@ -216,7 +255,7 @@ __device__ __forceinline__ void row_stats(Team<TEAM>& team, const float (&v)[K][
                       : __builtin_nanf("");  // a value that is not finite
       }
       if (s[k] < 0x1p-70f && a.eps < 0x1p-90f)
-        st[k].r = (float)(1.0 / sqrt((double)q[2 * k + 1] * a.inv_c * 0x1p-144 + (double)a.eps));
+        st[k].r = __builtin_amdgcn_rsqf(__builtin_fmaf(q[2 * k + 1], a.inv_c, a.eps * 0x1p72f * 0x1p72f)) * 0x1p72f;
     }
   }
 }
@@ -236,18 +275,25 @@ struct RowPlace {
   }
 };
 
-template <typename T, int VPT>
-__device__ __forceinline__ void load_row(float (&out)[VPT][kRowVec<T>], const void* base,
-                                         int64_t at, const int (&vec)[VPT],
-                                         const int (&valid)[VPT], int C) {
+// A thread's vectors of a row as they are in memory.
+template <typename T, int VPT, int MODE>
+struct RawRow {
+  RowVec<T> v[VPT];
+  __device__ __forceinline__ void load(const void* base, int64_t at, const int (&vec)[VPT],
+                                       const int (&valid)[VPT], int C) {
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const RowVec<T> r = load_row_vec<T>(static_cast<const T*>(base) + at, vec[i], C, valid[i] > 0);
-#pragma unroll
-    for (int j = 0; j < kRowVec<T>; ++j) out[i][j] = (float)r.e[j];
+    for (int i = 0; i < VPT; ++i)
+      v[i] = load_row_vec<T, MODE>(static_cast<const T*>(base) + at, vec[i], C, valid[i]);
   }
-}
-template <typename T, int VPT>
+  __device__ __forceinline__ void widen(float (&out)[VPT][kRowVec<T>]) const {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j < kRowVec<T>; ++j) out[i][j] = (float)v[i].e[j];
+  }
+};
+
+template <typename T, int VPT, int MODE>
 __device__ __forceinline__ void store_row(void* base, int64_t at, const int (&vec)[VPT],
                                           const int (&valid)[VPT], int C,
                                           const float (&v)[VPT][kRowVec<T>]) {
@@ -257,13 +303,13 @@ __device__ __forceinline__ void store_row(void* base, int64_t at, const int (&ve
       RowVec<T> r;
 #pragma unroll
       for (int j = 0; j < kRowVec<T>; ++j) r.e[j] = (T)v[i][j];
-      store_row_vec<T>(static_cast<T*>(base) + at, vec[i], C, r);
+      store_row_vec<T, MODE>(static_cast<T*>(base) + at, vec[i], C, r);
     }
 }
-// A row's gate (1 without one).
-template <typename T, int VPT>
+// A row of the gate (ones without it).
+template <typename T, int VPT, int MODE>
 __device__ __forceinline__ void load_gate(float (&out)[VPT][kRowVec<T>], const RowNormArgs& a,
-                                          int64_t row, const int (&vec)[VPT],
+                                          int64_t gate_row, const int (&vec)[VPT],
                                           const int (&valid)[VPT]) {
   constexpr int V = kRowVec<T>;
   if (!a.gate) {
@@ -273,21 +319,49 @@ __device__ __forceinline__ void load_gate(float (&out)[VPT][kRowVec<T>], const R
       for (int j = 0; j < V; ++j) out[i][j] = 1.0f;
     return;
   }
-  const int64_t at = (a.per_gate == 1 ? row : row / a.per_gate) * a.C;
+  const int64_t at = gate_row * a.C;
   if (a.gate_f32) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-      for (int q = 0; q < V / 4; ++q) {
-        const int v = vec[i] * (V / 4) + q;
-        const RowVec<float> r = load_row_vec<float>(static_cast<const float*>(a.gate) + at, v, a.C,
-                                                    valid[i] > 4 * q);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) out[i][4 * q + j] = r.e[j];
-      }
+    for (int i = 0; i < VPT; ++i) load_param<V>(out[i], static_cast<const float*>(a.gate) + at, vec[i], a.C, 0.0f);
   } else {
-    load_row<T, VPT>(out, a.gate, at, vec, valid, a.C);
+    RawRow<T, VPT, MODE> r;
+    r.load(a.gate, at, vec, valid, a.C);
+    r.widen(out);
   }
 }
+
+// A parameter's values for a thread, kept over the rows, or read where they are used.
+template <bool KEPT, int VPT, int V>
+struct Param {
+  float kept[KEPT ? VPT : 1][V];
+  const float* from;
+  float other;
+  __device__ __forceinline__ Param(const float* p, float none, const int (&vec)[VPT], int C)
+      : from(p), other(none) {
+    if constexpr (KEPT) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) load_param<V>(kept[i], p, vec[i], C, none);
+    }
+  }
+  __device__ __forceinline__ void get(float (&out)[V], int i, const int (&vec)[VPT], int C) const {
+    if constexpr (KEPT) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) out[j] = kept[i][j];
+    } else {
+      load_param<V>(out, from, vec[i], C, other);
+    }
+  }
+};
+
+// The rows of a unit: a piece of one span.
+struct UnitRows {
+  int64_t span, first, end;
+  __device__ __forceinline__ explicit UnitRows(const RowNormArgs& a) {
+    span = (int64_t)blockIdx.x / a.units_per_gate;
+    first = span * a.span + ((int64_t)blockIdx.x - span * a.units_per_gate) * a.per_unit;
+    const int64_t last = (span + 1) * a.span;
+    end = first + a.per_unit < last ? first + a.per_unit : last;
+  }
+};
 
 }  // namespace fno

@@ -92,14 +92,14 @@ fno_status check_desc(const fno_residual_norm_desc* d) {
 struct RowPlan {
   RowNormArgs a;
   int team, vecs;
-  int64_t units;  // of the backward
+  int64_t units;
 };
 
-// A row's team: the fewest threads that hold it, a vector each, up to a wave;
-// then two vectors a lane, then work-groups.
+// A row's team: the fewest threads that hold it, a vector each, then two and four.
 void team_of(int nvec, int* team, int* vecs) {
-  static const int kTeams[][2] = {{4, 1},   {8, 1},   {16, 1},  {32, 1},   {64, 1},  {64, 2},
-                                  {256, 1}, {256, 2}, {512, 2}, {1024, 2}, {1024, 4}};
+#define FNO_ROW(T_, V_) {T_, V_},
+  static const int kTeams[][2] = {FNO_ROW_TEAMS(FNO_ROW)};
+#undef FNO_ROW
   for (const auto& t : kTeams) {
     *team = t[0];
     *vecs = t[1];
@@ -107,7 +107,7 @@ void team_of(int nvec, int* team, int* vecs) {
   }
 }
 
-RowPlan plan_of(const fno_residual_norm_desc& d) {
+RowPlan plan_of(const fno_residual_norm_desc& d, bool bwd) {
   RowPlan p{};
   RowNormArgs& a = p.a;
   const int V = d.dtype == FNO_DTYPE_F32 ? 4 : 8;
@@ -124,13 +124,15 @@ RowPlan plan_of(const fno_residual_norm_desc& d) {
   a.inv_c = (float)(1.0 / a.C);
   a.per_gate = d.gate_rows ? d.rows / d.gate_rows : d.rows;
   team_of(a.nvec, &p.team, &p.vecs);
-  // A unit is rows of one gate row's share, at most 128 for a thread; one gate
-  // per row needs no sums by gate row, so its units take any rows.
+  // A unit is rows of one gate row's share, in the backward at most 128 for a
+  // thread (its chain of additions); one gate per row needs no sums by gate row,
+  // so its units take any rows.
   const int64_t slots = row_threads(p.team) / p.team;
   a.span = a.per_gate == 1 ? d.rows : a.per_gate;
   const int64_t span = a.span, spans = d.rows / span;
-  const int64_t fill = p.team <= 64 ? 1024 : 512;
-  a.units_per_gate = std::max(std::min(cdiv(fill, spans), cdiv(span, slots)), cdiv(span, 128 * slots));
+  const int64_t fill = p.team <= 64 ? (bwd ? 1024 : 2048) : 131072 / p.team * (bwd ? 1 : 2);
+  a.units_per_gate = std::max(std::min(cdiv(fill, spans), cdiv(span, slots)),
+                              bwd ? cdiv(span, 128 * slots) : 1);
   a.per_unit = cdiv(span, a.units_per_gate);
   a.units_per_gate = cdiv(span, a.per_unit);
   p.units = a.units_per_gate * spans;
@@ -165,17 +167,23 @@ struct RowLaunch {
   hipStream_t stream;
 };
 
+RowLaunchSize size_of(const RowLaunch& L) {
+  const int V = L.dtype == FNO_DTYPE_F32 ? 4 : 8, C = L.p.a.C;
+  return RowLaunchSize{L.p.team, L.p.vecs, C % V == 0 ? ROW_WHOLE : C > V ? ROW_TAIL : ROW_SHORT,
+                       (unsigned)L.p.units};
+}
+
 hipError_t launch_fwd(void* ctx) {
   const RowLaunch& L = *static_cast<RowLaunch*>(ctx);
-  const int64_t slots = row_threads(L.p.team) / L.p.team;
-  const int64_t grid = std::min<int64_t>(cdiv(L.p.a.rows, slots), L.p.team <= 64 ? 2048 : 1024);
-  return launch_row_norm_fwd(L.p.a, L.dtype, L.p.team, L.p.vecs, (unsigned)grid, L.stream);
+  return launch_row_norm_fwd(L.p.a, L.dtype, size_of(L), L.stream);
 }
 
 hipError_t launch_bwd(void* ctx) {
   const RowLaunch& L = *static_cast<RowLaunch*>(ctx);
-  const hipError_t e = launch_row_norm_bwd(L.p.a, L.dtype, L.post, L.pre, L.p.team, L.p.vecs,
-                                           (unsigned)L.p.units, L.stream);
+  const auto launch = L.dtype == FNO_DTYPE_F32   ? launch_row_norm_bwd_f32
+                      : L.dtype == FNO_DTYPE_F16 ? launch_row_norm_bwd_f16
+                                                 : launch_row_norm_bwd_bf16;
+  const hipError_t e = launch(L.p.a, L.post, L.pre, size_of(L), L.stream);
   if (e != hipSuccess || !L.p.a.sums) return e;
   const int64_t jobs = cdiv(L.p.a.C, kJoinCols) *
                        (L.p.a.sums - (L.join.gate_slot >= 0) +
@@ -200,7 +208,7 @@ extern "C" fno_status fno_residual_norm_workspace_size(const fno_residual_norm_d
   const fno_status st = check_desc(d);
   if (st != FNO_OK) return st;
   if (!bytes) return FNO_ERR_INVALID_ARGUMENT;
-  const RowPlan p = plan_of(*d);
+  const RowPlan p = plan_of(*d, true);
   if (p.units > INT32_MAX) return FNO_ERR_UNSUPPORTED;
   *bytes = (size_t)ws_bytes(*d, p);
   return FNO_OK;
@@ -213,9 +221,10 @@ extern "C" fno_status fno_residual_norm_fwd(const fno_residual_norm_desc* d,
   if (st != FNO_OK) return st;
   if (!ok16(x) || !null_or16(u) || !null_or16(y) || !null_or16(h)) return FNO_ERR_INVALID_ARGUMENT;
   if ((u != nullptr) != (y != nullptr) || (!u && !h) || (y && y == h)) return FNO_ERR_INVALID_ARGUMENT;
-  RowLaunch L{plan_of(*d), d->dtype, u != nullptr, h != nullptr, {}, stream};
+  RowLaunch L{plan_of(*d, false), d->dtype, u != nullptr, h != nullptr, {}, stream};
   st = set_params(&L.p.a, *d, params, L.post, L.pre);
   if (st != FNO_OK) return st;
+  if (L.p.units > INT32_MAX) return FNO_ERR_UNSUPPORTED;
   L.p.a.x = x;
   L.p.a.u = u;
   L.p.a.y = y;
@@ -246,7 +255,7 @@ extern "C" fno_status fno_residual_norm_bwd(const fno_residual_norm_desc* d,
   if (post && ((pre && !y) || (grads->scale && !x) || (grads->gate && !d->gate_rows)))
     return FNO_ERR_INVALID_ARGUMENT;
   if (!pre && (grads->pre_w || grads->pre_b)) return FNO_ERR_INVALID_ARGUMENT;
-  RowLaunch L{plan_of(*d), d->dtype, post, pre, {}, stream};
+  RowLaunch L{plan_of(*d, true), d->dtype, post, pre, {}, stream};
   st = set_params(&L.p.a, *d, params, post, pre);
   if (st != FNO_OK) return st;
   if (L.p.units > INT32_MAX) return FNO_ERR_UNSUPPORTED;

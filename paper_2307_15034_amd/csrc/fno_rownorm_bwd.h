@@ -4,6 +4,8 @@
 // Both rows' statistics are formed again from the rows, which a team of threads
 // holds whole; the parameters' sums stay in registers over a unit's rows and
 // leave as one partial row a unit.
+#pragma once
+
 #include "fno_rownorm.h"
 
 namespace fno {
@@ -68,60 +70,75 @@ __device__ __forceinline__ void write_sums(const RowNormArgs& a, int which, floa
   }
 }
 
-template <typename T, int TEAM, int VPT, bool POST, bool PRE>
+template <typename T, int TEAM, int VPT, int MODE, bool POST, bool PRE>
 __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNormArgs a) {
   constexpr int V = kRowVec<T>, SLOTS = row_threads(TEAM) / TEAM;
   constexpr int K = (POST ? 1 : 0) + (PRE ? 1 : 0);  // rows with statistics
   __shared__ float lds[TEAM > 64 ? 1 : row_threads(TEAM) / 64 * TEAM * VPT * V];
+  constexpr bool KEPT = !row_lean(TEAM);
   const RowPlace<T, TEAM, VPT> at(a);
-  float post_w[VPT][V], post_b[VPT][V], scale[VPT][V], pre_w[VPT][V];
+  const Param<KEPT && POST, VPT, V> post_w(a.post_w, 1.0f, at.vec, a.C), post_b(a.post_b, 0.0f, at.vec, a.C);
+  const Param<KEPT && POST, VPT, V> scale(a.scale, 1.0f, at.vec, a.C);
+  const Param<KEPT && PRE, VPT, V> pre_w(a.pre_w, 1.0f, at.vec, a.C);
   float sums[RS_COUNT][VPT][V];
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    if constexpr (POST) {
-      load_param<V>(post_w[i], a.post_w, at.vec[i], a.C, 1.0f);
-      load_param<V>(post_b[i], a.post_b, at.vec[i], a.C, 0.0f);
-      load_param<V>(scale[i], a.scale, at.vec[i], a.C, 1.0f);
-    }
-    if constexpr (PRE) load_param<V>(pre_w[i], a.pre_w, at.vec[i], a.C, 1.0f);
+  for (int i = 0; i < VPT; ++i)
 #pragma unroll
     for (int q = 0; q < RS_COUNT; ++q)
 #pragma unroll
       for (int j = 0; j < V; ++j) sums[q][i][j] = 0.0f;
-  }
   Team<TEAM> team;
-  // the unit's rows: a piece of one span
-  const int64_t g = (int64_t)blockIdx.x / a.units_per_gate;
-  const int64_t first = g * a.span + ((int64_t)blockIdx.x - g * a.units_per_gate) * a.per_unit;
-  const int64_t end = first + a.per_unit < (g + 1) * a.span ? first + a.per_unit : (g + 1) * a.span;
-  for (int64_t row = first + threadIdx.x / TEAM; row < end; row += SLOTS) {
+  const UnitRows unit(a);
+  float gate[VPT][V];
+  if (POST && a.per_gate > 1) load_gate<T, VPT, MODE>(gate, a, unit.span, at.vec, at.valid);
+  const bool with_x = POST && a.slot[RS_SCALE] >= 0;
+  RawRow<T, VPT, MODE> ru, ry, rh, rg, rx;
+  auto fetch = [&](int64_t row) {
     const int64_t start = row * a.C;
-    float v[K][VPT][V], G[VPT][V], t[VPT][V], xh[VPT][V];
-    RowStat st[K];
-    if constexpr (POST) load_row<T, VPT>(v[0], a.u, start, at.vec, at.valid, a.C);
+    if constexpr (POST) ru.load(a.u, start, at.vec, at.valid, a.C);
     if constexpr (PRE) {
-      load_row<T, VPT>(v[K - 1], a.y_in, start, at.vec, at.valid, a.C);
-      load_row<T, VPT>(t, a.g_h, start, at.vec, at.valid, a.C);
+      ry.load(a.y_in, start, at.vec, at.valid, a.C);
+      rh.load(a.g_h, start, at.vec, at.valid, a.C);
+    }
+    if (a.g_y) rg.load(a.g_y, start, at.vec, at.valid, a.C);
+    if (with_x) rx.load(a.x, start, at.vec, at.valid, a.C);
+  };
+  int64_t row = unit.first + threadIdx.x / TEAM;
+  if (KEPT && row < unit.end) fetch(row);
+  for (; row < unit.end; row += SLOTS) {
+    const int64_t start = row * a.C;
+    if (!KEPT) fetch(row);
+    float v[K][VPT][V], G[VPT][V], t[VPT][V], xh[VPT][V], x[VPT][V];
+    RowStat st[K];
+    if constexpr (POST) ru.widen(v[0]);
+    if constexpr (PRE) {
+      ry.widen(v[K - 1]);
+      rh.widen(t);
     }
     if (a.g_y) {
-      load_row<T, VPT>(G, a.g_y, start, at.vec, at.valid, a.C);
+      rg.widen(G);
     } else {
 #pragma unroll
       for (int i = 0; i < VPT; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) G[i][j] = 0.0f;
     }
+    if (with_x) rx.widen(x);
+    if (KEPT && row + SLOTS < unit.end) fetch(row + SLOTS);
     row_stats<K, VPT, V, TEAM>(team, v, at.valid, a, st);
     if constexpr (PRE) {
 #pragma unroll
-      for (int i = 0; i < VPT; ++i)
+      for (int i = 0; i < VPT; ++i) {
+        float w[V];
+        pre_w.get(w, i, at.vec, a.C);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           xh[i][j] = (v[K - 1][i][j] - st[K - 1].mean) * st[K - 1].r;
           sums[RS_PRE_W][i][j] = __builtin_fmaf(t[i][j], xh[i][j], sums[RS_PRE_W][i][j]);
           sums[RS_PRE_B][i][j] += t[i][j];
-          t[i][j] *= pre_w[i][j];
+          t[i][j] *= w[j];
         }
+      }
       float d[VPT][V];
       norm_grad<VPT, V, TEAM>(team, t, xh, a, st[K - 1].r, d);
 #pragma unroll
@@ -130,25 +147,26 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
         for (int j = 0; j < V; ++j) G[i][j] += d[i][j];
     }
     if constexpr (POST) {
-      if (a.slot[RS_SCALE] >= 0) {
-        float x[VPT][V];
-        load_row<T, VPT>(x, a.x, start, at.vec, at.valid, a.C);
+      if (with_x) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
           for (int j = 0; j < V; ++j)
             sums[RS_SCALE][i][j] = __builtin_fmaf(G[i][j], x[i][j], sums[RS_SCALE][i][j]);
       }
-      float gate[VPT][V];
-      load_gate<T, VPT>(gate, a, row, at.vec, at.valid);
+      if (a.per_gate == 1) load_gate<T, VPT, MODE>(gate, a, row, at.vec, at.valid);
 #pragma unroll
-      for (int i = 0; i < VPT; ++i)
+      for (int i = 0; i < VPT; ++i) {
+        float w[V], b[V];
+        post_w.get(w, i, at.vec, a.C);
+        post_b.get(b, i, at.vec, a.C);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           xh[i][j] = (v[0][i][j] - st[0].mean) * st[0].r;
-          t[i][j] = G[i][j] * __builtin_fmaf(xh[i][j], post_w[i][j], post_b[i][j]);
+          t[i][j] = G[i][j] * __builtin_fmaf(xh[i][j], w[j], b[j]);
           sums[RS_GATE][i][j] += t[i][j];
         }
+      }
       if (a.g_gate) {
         if (a.gate_f32) {
 #pragma unroll
@@ -159,27 +177,31 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
 #pragma unroll
               for (int j = 0; j < 4; ++j) r.e[j] = t[i][4 * q + j];
               if (at.valid[i] > 4 * q)
-                store_row_vec<float>(static_cast<float*>(a.g_gate) + start, at.vec[i] * (V / 4) + q, a.C, r);
+                store_row_vec<float, ROW_TAIL>(static_cast<float*>(a.g_gate) + start, at.vec[i] * (V / 4) + q, a.C, r);
             }
         } else {
-          store_row<T, VPT>(a.g_gate, start, at.vec, at.valid, a.C, t);
+          store_row<T, VPT, MODE>(a.g_gate, start, at.vec, at.valid, a.C, t);
         }
       }
 #pragma unroll
-      for (int i = 0; i < VPT; ++i)
+      for (int i = 0; i < VPT; ++i) {
+        float w[V], c[V];
+        post_w.get(w, i, at.vec, a.C);
+        scale.get(c, i, at.vec, a.C);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           t[i][j] = G[i][j] * gate[i][j];
-          G[i][j] *= scale[i][j];
+          G[i][j] *= c[j];
           sums[RS_POST_W][i][j] = __builtin_fmaf(t[i][j], xh[i][j], sums[RS_POST_W][i][j]);
           sums[RS_POST_B][i][j] += t[i][j];
-          t[i][j] *= post_w[i][j];
+          t[i][j] *= w[j];
         }
+      }
       float d[VPT][V];
       norm_grad<VPT, V, TEAM>(team, t, xh, a, st[0].r, d);
-      store_row<T, VPT>(a.g_u, start, at.vec, at.valid, a.C, d);
+      store_row<T, VPT, MODE>(a.g_u, start, at.vec, at.valid, a.C, d);
     }
-    store_row<T, VPT>(a.g_x, start, at.vec, at.valid, a.C, G);
+    store_row<T, VPT, MODE>(a.g_x, start, at.vec, at.valid, a.C, G);
   }
   if (a.sums) {
     if constexpr (POST) {
@@ -195,43 +217,32 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
   }
 }
 
-template <typename T, bool POST, bool PRE>
-hipError_t launch_of(const RowNormArgs& a, int team, int vecs, unsigned grid, hipStream_t s) {
-#define FNO_ROW(T_, V_)                                                                          \
-  if (team == T_ && vecs == V_) {                                                                \
-    row_norm_bwd_kernel<T, T_, V_, POST, PRE><<<dim3(grid), dim3(row_threads(T_)), 0, s>>>(a);   \
-    return hipGetLastError();                                                                    \
+template <typename T, bool POST, bool PRE, int MODE>
+hipError_t launch_mode(const RowNormArgs& a, const RowLaunchSize& l, hipStream_t s) {
+#define FNO_ROW(T_, V_)                                                                        \
+  if (l.team == T_ && l.vecs == V_) {                                                          \
+    row_norm_bwd_kernel<T, T_, V_, MODE, POST, PRE><<<dim3(l.grid), dim3(row_threads(T_)), 0, s>>>(a); \
+    return hipGetLastError();                                                                  \
   }
-  FNO_ROW(4, 1)
-  FNO_ROW(8, 1)
-  FNO_ROW(16, 1)
-  FNO_ROW(32, 1)
-  FNO_ROW(64, 1)
-  FNO_ROW(64, 2)
-  FNO_ROW(256, 1)
-  FNO_ROW(256, 2)
-  FNO_ROW(512, 2)
-  FNO_ROW(1024, 2)
-  FNO_ROW(1024, 4)
+  if constexpr (MODE == ROW_SHORT) {  // one vector
+    FNO_ROW(4, 1)
+  } else {
+    FNO_ROW_TEAMS(FNO_ROW)
+  }
 #undef FNO_ROW
   return hipErrorInvalidValue;
 }
-
+template <typename T, bool POST, bool PRE>
+hipError_t launch_of(const RowNormArgs& a, const RowLaunchSize& l, hipStream_t s) {
+  if (l.mode == ROW_WHOLE) return launch_mode<T, POST, PRE, ROW_WHOLE>(a, l, s);
+  return l.mode == ROW_TAIL ? launch_mode<T, POST, PRE, ROW_TAIL>(a, l, s)
+                            : launch_mode<T, POST, PRE, ROW_SHORT>(a, l, s);
+}
 template <typename T>
-hipError_t launch_form(const RowNormArgs& a, bool post, bool pre, int team, int vecs, unsigned grid,
-                       hipStream_t s) {
-  if (post && pre) return launch_of<T, true, true>(a, team, vecs, grid, s);
-  if (post) return launch_of<T, true, false>(a, team, vecs, grid, s);
-  return launch_of<T, false, true>(a, team, vecs, grid, s);
+hipError_t launch_form(const RowNormArgs& a, bool post, bool pre, const RowLaunchSize& l, hipStream_t s) {
+  if (post && pre) return launch_of<T, true, true>(a, l, s);
+  return post ? launch_of<T, true, false>(a, l, s) : launch_of<T, false, true>(a, l, s);
 }
 
 }  // namespace
-
-hipError_t launch_row_norm_bwd(const RowNormArgs& a, int dtype, bool post, bool pre, int team,
-                               int vecs, unsigned grid, hipStream_t s) {
-  if (dtype == FNO_DTYPE_F32) return launch_form<float>(a, post, pre, team, vecs, grid, s);
-  if (dtype == FNO_DTYPE_F16) return launch_form<_Float16>(a, post, pre, team, vecs, grid, s);
-  return launch_form<__bf16>(a, post, pre, team, vecs, grid, s);
-}
-
 }  // namespace fno
