@@ -147,6 +147,13 @@ __device__ __forceinline__ void finish4(const MatmulArgs& g, int64_t row, int64_
       if (col + j < g.N) out[j] = r[j];
   }
 }
+template <typename T>
+__device__ __forceinline__ void finish1(const MatmulArgs& g, int64_t row, int64_t col, float v) {
+  const int64_t at = row * g.N + col;
+  if (g.z) v *= act_grad_any<T>((float)static_cast<const T*>(g.z)[at], g.act);
+  if (g.bias) v += g.bias[col];
+  static_cast<T*>(g.out)[at] = (T)v;
+}
 // A wave's part of the tile: four columns at a time of the rows that a lane holds,
 // rows and columns behind the last left out.
 template <typename T, int RM, int RN>
@@ -446,6 +453,91 @@ __global__ __launch_bounds__(64 * WGM * WGN, STAGES == 1 ? 3 : 1) void gemm_kern
   }
 }
 
+// Few rows: the work is in reading B.  A work-group takes 16 of its rows, a wave
+// every eighth block of them, straight from memory into the operands (row i of A
+// and B: lanes i, i + 16, ..); the waves' sums meet in LDS, in their order.  One
+// row of 4096 by 4096 x 4096: MEASURE.
+constexpr int kRowWaves = 8;
+template <int FA, int FB, bool F32S, bool WIDE, int MT>
+__global__ __launch_bounds__(64 * kRowWaves) void few_rows_kernel(MatmulArgs g) {
+  __shared__ V4F sums[kRowWaves][MT][64];
+  const int lane = threadIdx.x & 63, i16 = lane & 15, kg = lane >> 4, wave = threadIdx.x >> 6;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t bn = n0 + i16 < g.N ? n0 + i16 : g.N - 1;
+  const uint8_t* b = g.b + bn * g.pitch;
+  using S = std::conditional_t<F32S, float, uint8_t>;
+  const S* sa = static_cast<const S*>(g.scale_a);
+  const S* sb = static_cast<const S*>(g.scale_b) + (bn >> g.shift_b);
+  const uint8_t* a[MT];
+  int64_t am[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    am[t] = t * 16 + i16 < g.M ? t * 16 + i16 : g.M - 1;
+    a[t] = g.a + am[t] * g.pitch;
+  }
+  auto operand = [&](const uint8_t* row, int kb) {
+    const int64_t at = (int64_t)kb * kBlock + kg * 16;
+    V4I lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+    if (at < g.pitch) lo = *reinterpret_cast<const V4I*>(row + at);
+    if (at + 64 < g.pitch) hi = *reinterpret_cast<const V4I*>(row + at + 64);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  V4F acc[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) acc[t] = V4F{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll(MT == 1 ? 4 : 2)
+  for (int kb = wave; kb < g.kb; kb += kRowWaves) {
+    const V8I fb = operand(b, kb);
+    const S ub = sb[kb * g.scales_b];
+    V8B wb[4];
+    if constexpr (WIDE) widen<FB>(fb, F32S ? 1.0f : scale_of((int)ub, 0), wb);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const V8I fa = operand(a[t], kb);
+      V4F p = F32S ? V4F{0.0f, 0.0f, 0.0f, 0.0f} : acc[t];
+      S ua = 0;
+      if constexpr (!F32S) ua = sa[kb * g.scales_a + (am[t] >> g.shift_a)];
+      if constexpr (WIDE) {
+        V8B wa[4];
+        widen<FA>(fa, F32S ? 1.0f : scale_of((int)ua, 0), wa);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[i], wb[i], p, 0, 0, 0);
+      } else if constexpr (F32S) {
+        p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, p, FA, FB, 0, 0, 0, 0);
+      } else {
+        p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, p, FA, FB, 0, (int)ua, 0, (int)ub);
+      }
+      if constexpr (F32S) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t m = t * 16 + kg * 4 + r < g.M ? t * 16 + kg * 4 + r : g.M - 1;
+          acc[t][r] = __builtin_fmaf(p[r], sa[kb * g.scales_a + (m >> g.shift_a)] * ub, acc[t][r]);
+        }
+      } else {
+        acc[t] = p;
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) sums[wave][t][lane] = acc[t];
+  __syncthreads();
+  // a thread for a result: row 4 q + r of its 16, column i
+  for (int o = threadIdx.x; o < MT * 256; o += 64 * kRowWaves) {
+    const int t = o >> 8, row16 = (o >> 4) & 15, col16 = o & 15;
+    const int64_t row = t * 16 + row16, col = n0 + col16;
+    if (row >= g.M || col >= g.N) continue;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w) v += sums[w][t][(row16 >> 2) * 16 + col16][row16 & 3];
+    if (g.dtype == FNO_DTYPE_F32)
+      finish1<float>(g, row, col, v);
+    else if (g.dtype == FNO_DTYPE_F16)
+      finish1<_Float16>(g, row, col, v);
+    else
+      finish1<__bf16>(g, row, col, v);
+  }
+}
+
 // Joins the splits' sums: four columns for `lanes` threads (a power of two up to
 // 64), each of which adds every lanes-th split; a fixed order.
 __global__ __launch_bounds__(256) void join_splits_kernel(MatmulArgs g, int lanes) {
@@ -497,7 +589,7 @@ fno_status check_desc(const fno_fp8_matmul_desc* d) {
   return FNO_OK;
 }
 
-enum Tile { TILE_128, TILE_256, TILE_NARROW };
+enum Tile { TILE_128, TILE_256, TILE_NARROW, FEW_ROWS };
 struct MatmulPlan {
   MatmulArgs g;
   Tile tile;
@@ -521,17 +613,21 @@ MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
   // the rows' bytes: more work-groups at a time); else 128 x 128.
   const bool pow2 = d.scale_type == FNO_SCALE_POW2;
   const int64_t of256 = fp8_cdiv(g.M, 256) * fp8_cdiv(g.N, 256);
-  p.tile = g.kb == 1 && g.N <= 64 && g.M > 128 ? TILE_NARROW
+  // Few rows of B's worth: up to 64 rows, while a wave's share of the inner axis
+  // stays short (products of weights' gradients have few rows and a long one).
+  p.tile = g.M <= 64 && g.kb <= 256 ? FEW_ROWS
+           : g.kb == 1 && g.N <= 64 && g.M > 128 ? TILE_NARROW
            : pow2 && of256 >= 192 && g.N > 128 ? TILE_256
                                                : TILE_128;
-  const int bm = p.tile == TILE_128 ? 128 : 256, bn = p.tile == TILE_256 ? 256 : p.tile == TILE_NARROW ? 64 : 128;
+  const int bm = p.tile == FEW_ROWS ? 64 : p.tile == TILE_128 ? 128 : 256;
+  const int bn = p.tile == FEW_ROWS ? 16 : p.tile == TILE_256 ? 256 : p.tile == TILE_NARROW ? 64 : 128;
   g.tiles_m = fp8_cdiv(g.M, bm);
   g.tiles_n = fp8_cdiv(g.N, bn);
   // Few tiles of a long inner axis: split along it, down to four blocks each.
   const int64_t tiles = g.tiles_m * g.tiles_n;
   g.splits = 1;
   const int64_t fill = p.tile == TILE_256 ? 256 : 512;  // work-groups that the chip holds at a time
-  if (tiles <= fill / 2 && g.kb >= 8)
+  if (p.tile != FEW_ROWS && tiles <= fill / 2 && g.kb >= 8)
     g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(fill / tiles, g.kb / 4));
   g.kb_per_split = (int)fp8_cdiv(g.kb, g.splits);
   g.splits = (int)fp8_cdiv(g.kb, g.kb_per_split);
@@ -548,7 +644,10 @@ struct MatmulLaunch {
 template <int FA, int FB, bool F32S, bool WIDE>
 void launch_tile(const MatmulLaunch& L, dim3 grid) {
   const MatmulArgs& g = L.p.g;
-  if (L.p.tile == TILE_NARROW) {
+  if (L.p.tile == FEW_ROWS) {
+    g.M <= 16 ? few_rows_kernel<FA, FB, F32S, WIDE, 1><<<grid, dim3(64 * kRowWaves), 0, L.stream>>>(g)
+              : few_rows_kernel<FA, FB, F32S, WIDE, 4><<<grid, dim3(64 * kRowWaves), 0, L.stream>>>(g);
+  } else if (L.p.tile == TILE_NARROW) {
     gemm_kernel<FA, FB, F32S, WIDE, 256, 64, 4, 1, 1><<<grid, dim3(256), 0, L.stream>>>(g);
   } else if (L.p.tile == TILE_256) {
     if constexpr (!F32S) gemm_kernel<FA, FB, F32S, WIDE, 256, 256, 2, 4><<<grid, dim3(512), 0, L.stream>>>(g);

@@ -24,7 +24,7 @@ def _addr(t: Optional[torch.Tensor], shape=None, dtype=None, name: str = "tensor
         raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != tuple(shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if min_bytes is not None and t.numel() * t.element_size() < min_bytes:
         raise ValueError(f"{name}: {t.numel() * t.element_size()} bytes, "
@@ -321,10 +321,10 @@ def _stream_of(device: torch.device, stream: Optional[int]) -> int:
     """The stream a call runs on: `stream`, or torch's current one on
     `device`, which has to be the current device (the library launches
     there)."""
-    current = torch.cuda.current_device()
+    current = torch._C._cuda_getDevice()
     if device.index != current:
         raise ValueError(f"the current device is cuda:{current}, the tensors live on {device}")
-    return torch.cuda.current_stream(current).cuda_stream if stream is None else stream
+    return torch._C._cuda_getCurrentRawStream(current) if stream is None else stream
 
 
 def _external(device: torch.device, stream: int) -> torch.cuda.Stream:
@@ -538,21 +538,20 @@ class ResidualNorm:
         return a
 
     def _params(self, p, device):
-        s = B.FnoResidualNormParams()
-        for k, t in p.items():
-            if t is not None and k != "gate":
-                setattr(s, k, _addr(t, (self.channels,), torch.float32, k, device))
-        gate = p["gate"]
+        """(addresses, (descriptor, workspace bytes)) of parameters in their order."""
+        shape, gate = (self.channels,), p[2]
+        at = [0 if t is None or t is gate else _addr(t, shape, torch.float32, k, device)
+              for k, t in zip(self.PARAMS, p)]
         if gate is None:
-            return s, self._desc(0, torch.float32)
+            return B.FnoResidualNormParams(*at), self._desc(0, torch.float32)
         if gate.dtype not in (torch.float32, self.dtype):
             raise ValueError(f"gate: dtype {gate.dtype}, expected float32 or {self.dtype}")
         if gate.dim() != 2 or gate.shape[1] != self.channels or not 0 < gate.shape[0] <= self.rows \
                 or self.rows % gate.shape[0]:
             raise ValueError(f"gate: shape {tuple(gate.shape)}, expected [gate_rows, "
                              f"{self.channels}], gate_rows a divisor of {self.rows}")
-        s.gate = _addr(gate, None, None, "gate", device)
-        return s, self._desc(gate.shape[0], gate.dtype)
+        at[2] = _addr(gate, None, None, "gate", device)
+        return B.FnoResidualNormParams(*at), self._desc(gate.shape[0], gate.dtype)
 
     @staticmethod
     def _new(like, stream, name):
@@ -571,8 +570,7 @@ class ResidualNorm:
             raise ValueError("h is given, but pre is False")
         ax, dev = self._t(x, "x", self.device), x.device
         au, ay, ah = self._t(u, "u", dev), self._t(y, "y", dev), self._t(h, "h", dev)
-        par, (desc, _) = self._params(dict(post_w=post_w, post_b=post_b, gate=gate, scale=scale,
-                                           pre_w=pre_w, pre_b=pre_b), dev)
+        par, (desc, _) = self._params((post_w, post_b, gate, scale, pre_w, pre_b), dev)
         s = _stream_of(dev, stream)
         if u is not None and y is None:
             y = self._new(x, stream, "y")
@@ -611,7 +609,7 @@ class ResidualNorm:
         dev = first.device
         ax, au, ay = self._t(x, "x", dev), self._t(u, "u", dev), self._t(y, "y", dev)
         agy, agh = self._t(g_y, "g_y", dev), self._t(g_h, "g_h", dev)
-        par, (desc, nbytes) = self._params(params, dev)
+        par, (desc, nbytes) = self._params(tuple(params.values()), dev)
         got: Dict[str, Optional[torch.Tensor]] = {}
         grads = B.FnoResidualNormParams()
         for k, t in params.items():  # checked whole before anything is allocated
