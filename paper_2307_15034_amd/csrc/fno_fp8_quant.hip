@@ -214,6 +214,15 @@ struct Values {
   }
 };
 
+// Elements `by` to 7 to the front, zeros behind them (by 0 to 8).
+template <typename T>
+__device__ __forceinline__ void move_down(T (&t)[8], int by) {
+#pragma unroll
+  for (int d = 8; d > 0; d /= 2)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = by & d ? (j + d < 8 ? t[j + d] : (T)0.0f) : t[j];
+}
+
 // A work-group takes CG x 8 columns of 2048 / CG rows, a thread 8 x 8 of them:
 // lanes next to each other hold neighbouring columns of the same rows.  A row's
 // blocks are joined within a wave; a column's blocks of 128 rows are 16 threads,
@@ -240,21 +249,38 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
   constexpr bool pow2 = POW2;
   Values<T, FMT, ACT, POW2> v;
   const T* x = static_cast<const T*>(a.x);
+  // All eight rows' loads before any is used, so none has a branch of its own: rows
+  // behind the last repeat it and are zeroed, and where a row ends inside the eight
+  // columns its last eight are read and moved down.
+  T t[8][8];
+  const int cols = a.cols, left = cols - c0;  // columns from c0 on
+  const bool whole = (cols & 7) == 0;
+  if (cols >= 8) {
+    const int at = left >= 8 ? c0 : cols - 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = r0 + i < a.rows ? r0 + i : a.rows - 1;
+      __builtin_memcpy(t[i], __builtin_assume_aligned(x + row * cols + at, sizeof(T)), sizeof(t[i]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = r0 + i < a.rows ? r0 + i : a.rows - 1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[i][j] = j < left ? x[row * cols + c0 + j] : (T)0.0f;
+    }
+  }
+  const int off = !whole && cols >= 8 && left < 8 ? (left > 0 ? 8 - left : 8) : 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const bool on = r0 + i < a.rows;
-    const T* row = x + (r0 + i) * a.cols;
-    T t[8];
-    if (on && c0 + 8 <= a.cols) {
-      __builtin_memcpy(t, __builtin_assume_aligned(row + c0, sizeof(T)), sizeof(t));
-    } else {
+    if (!whole) move_down(t[i], off);
+    const bool on = r0 + i < a.rows && left > 0;
+    uint32_t w[sizeof(t[i]) / 4];
+    __builtin_memcpy(w, t[i], sizeof(w));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        t[j] = (T)0.0f;  // as behind an activation
-        if (on && c0 + j < a.cols) t[j] = row[c0 + j];
-      }
-    }
-    v.set(i, t, a.act);
+    for (uint32_t& e : w) e = on ? e : 0u;  // 0 as behind an activation
+    __builtin_memcpy(t[i], w, sizeof(w));
+    v.set(i, t[i], a.act);
   }
   const int64_t block_r = (r0 >> 7), block_c = c0 >> 7;
   // Largest sizes and sums of the columns' blocks.
