@@ -162,30 +162,48 @@ __device__ __forceinline__ void finish_tile(const MatmulArgs& g, const V4F (&acc
 #pragma unroll
   for (int q = 0; q < RN / 4; ++q) {
     const int64_t col = col0 + q * 64;
-    const bool whole = col + 4 <= g.N;
+    const bool whole = col + 4 <= g.N && row0 < g.M;
     if (whole) {
       V4F bias = {0.0f, 0.0f, 0.0f, 0.0f};
       if (g.bias) __builtin_memcpy(&bias, __builtin_assume_aligned(g.bias + col, 4), 16);
       T* out = static_cast<T*>(g.out) + row0 * g.N + col;
       const T* z = static_cast<const T*>(g.z) + row0 * g.N + col;
+      const int64_t left = g.M - row0;  // rows from row0 on
+      struct T4 {
+        T e[4];
+      };
 #pragma unroll
-      for (int i = 0; i < RM; ++i)
+      for (int i = 0; i < RM; i += 2) {
+        // eight rows of z at a time, all asked for before the first is used
+        T4 t[2][4];
+        if (g.z) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t row = (i >> 2) * 64 + r * 4 + (i & 3);
-          if (row0 + row >= g.M) continue;
-          V4F v = {acc[i][q * 4][r], acc[i][q * 4 + 1][r], acc[i][q * 4 + 2][r], acc[i][q * 4 + 3][r]};
-          T t[4];
-          if (g.z) {
-            __builtin_memcpy(t, __builtin_assume_aligned(z + row * g.N, sizeof(T)), sizeof(t));
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] *= act_grad_any<T>((float)t[j], g.act);
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) t[j] = (T)(v[j] + bias[j]);
-          __builtin_memcpy(__builtin_assume_aligned(out + row * g.N, sizeof(T)), t, sizeof(t));
+            for (int r = 0; r < 4; ++r) {
+              const int64_t row = ((i + h) >> 2) * 64 + r * 4 + ((i + h) & 3);
+              __builtin_memcpy(&t[h][r], __builtin_assume_aligned(z + (row < left ? row : 0) * g.N, sizeof(T)),
+                               sizeof(T4));
+            }
         }
-    } else if (col < g.N) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int64_t row = ((i + h) >> 2) * 64 + r * 4 + ((i + h) & 3);
+            V4F v = {acc[i + h][q * 4][r], acc[i + h][q * 4 + 1][r], acc[i + h][q * 4 + 2][r],
+                     acc[i + h][q * 4 + 3][r]};
+            if (g.z) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) v[j] *= act_grad_any<T>((float)t[h][r].e[j], g.act);
+            }
+            T4 o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o.e[j] = (T)(v[j] + bias[j]);
+            if (row < left) __builtin_memcpy(__builtin_assume_aligned(out + row * g.N, sizeof(T)), &o, sizeof(o));
+          }
+      }
+    } else if (col < g.N && row0 < g.M) {
 #pragma unroll
       for (int i = 0; i < RM; ++i)
 #pragma unroll

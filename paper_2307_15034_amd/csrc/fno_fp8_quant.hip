@@ -392,41 +392,43 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
 }
 
 // Sums of the units' column sums, in double.
-constexpr int kSumCols = 16, kSumLanes = 256;  // four columns a thread
-__global__ __launch_bounds__(kSumCols / 4 * kSumLanes) void col_sum_kernel(const float* part, float* out,
-                                                                           int64_t units, int cols) {
-  __shared__ double red[kSumLanes / 16][kSumCols];
-  const int quad = threadIdx.x % (kSumCols / 4), lane = threadIdx.x / (kSumCols / 4);
-  const int64_t c = (int64_t)blockIdx.x * kSumCols + quad * 4;
+// COLS columns for a work-group, four for a thread: few where units are many.
+template <int COLS>
+__global__ __launch_bounds__(1024) void col_sum_kernel(const float* part, float* out, int64_t units,
+                                                       int cols) {
+  constexpr int QUADS = COLS / 4, LANES = 1024 / QUADS;
+  __shared__ double red[16][COLS];
+  const int quad = threadIdx.x % QUADS, lane = threadIdx.x / QUADS;
+  const int64_t c = (int64_t)blockIdx.x * COLS + quad * 4;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
   if (c + 4 <= cols) {
 #pragma unroll 4
-    for (int64_t i = lane; i < units; i += kSumLanes) {
+    for (int64_t i = lane; i < units; i += LANES) {
       float t[4];
       __builtin_memcpy(t, __builtin_assume_aligned(part + i * cols + c, 4), sizeof(t));
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[j] += (double)t[j];
     }
   } else {
-    for (int64_t i = lane; i < units; i += kSumLanes)
+    for (int64_t i = lane; i < units; i += LANES)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (c + j < cols) s[j] += (double)part[i * cols + c + j];
   }
 #pragma unroll
-  for (int d = 4; d < 64; d *= 2)
+  for (int d = QUADS; d < 64; d *= 2)
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[j] += __shfl_xor(s[j], d);
-  if (lane % 16 == 0) {
+  if ((threadIdx.x & 63) < QUADS) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) red[lane / 16][quad * 4 + j] = s[j];
+    for (int j = 0; j < 4; ++j) red[threadIdx.x >> 6][quad * 4 + j] = s[j];
   }
   __syncthreads();
-  const int64_t mine = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
-  if (threadIdx.x < kSumCols && mine < cols) {
+  const int64_t mine = (int64_t)blockIdx.x * COLS + threadIdx.x;
+  if (threadIdx.x < COLS && mine < cols) {
     double t = red[0][threadIdx.x];
 #pragma unroll
-    for (int w = 1; w < kSumLanes / 16; ++w) t += red[w][threadIdx.x];
+    for (int w = 1; w < 16; ++w) t += red[w][threadIdx.x];
     out[mine] = (float)t;
   }
 }
@@ -487,8 +489,12 @@ hipError_t launch_quantize(void* ctx) {
                        : L.dtype == FNO_DTYPE_F16 ? launch_format<_Float16>(L)
                                                   : launch_format<__bf16>(L);
   if (e != hipSuccess || !L.col_sums) return e;
-  col_sum_kernel<<<dim3((unsigned)fp8_cdiv(L.a.cols, kSumCols)), dim3(kSumCols / 4 * kSumLanes), 0, L.stream>>>(
-      L.a.part, L.col_sums, L.a.blocks_r, L.a.cols);
+  if (L.a.blocks_r > 512)
+    col_sum_kernel<4><<<dim3((unsigned)fp8_cdiv(L.a.cols, 4)), dim3(1024), 0, L.stream>>>(
+        L.a.part, L.col_sums, L.a.blocks_r, L.a.cols);
+  else
+    col_sum_kernel<32><<<dim3((unsigned)fp8_cdiv(L.a.cols, 32)), dim3(1024), 0, L.stream>>>(
+        L.a.part, L.col_sums, L.a.blocks_r, L.a.cols);
   return hipGetLastError();
 }
 
