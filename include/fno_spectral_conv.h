@@ -569,8 +569,9 @@ fno_status fno_adamw_moments(const fno_adamw_tensor *tensors, int64_t count, fno
  * rows / gate_rows consecutive rows: 1 (one gate for all), one per sample, or
  * one per row.  gate_rows 0: no gate (1).
  *
- * Sums are fp32 chains of at most 128 additions, joined in double; every sum
- * has a fixed order.  h is formed from y before its rounding.  A row with a
+ * A row's sums are fp32; the parameters' are fp32 chains of at most 128
+ * additions, joined in double.  Every sum has a fixed order: results are
+ * bit-identical from run to run.  h is formed from y before its rounding.  A row with a
  * value that is not finite, or beyond 2^126 in size, gives NaN throughout.
  * ------------------------------------------------------------------------ */
 typedef enum { FNO_ROW_NORM_LAYER = 0, FNO_ROW_NORM_RMS = 1 } fno_row_norm;
@@ -582,7 +583,8 @@ typedef struct {
   float eps;           /* >= 0, finite */
   int64_t rows;        /* 1 .. 2^40, rows x channels up to 2^42 */
   int64_t channels;    /* 1 .. 16384 */
-  int64_t gate_rows;   /* 0, or a divisor of rows */
+  int64_t gate_rows;   /* 0, or a divisor of rows; up to 2^22 - 1 unless it is
+                          rows (FNO_ERR_UNSUPPORTED) */
 } fno_residual_norm_desc;
 
 typedef struct {
@@ -642,7 +644,8 @@ typedef struct {
   int32_t scale_type;  /* fno_scale_type */
   int32_t blocks;      /* fno_fp8_blocks */
   int32_t activation;  /* fno_norm_activation */
-  int64_t rows, cols;  /* >= 1, each up to 2^31 - 1; rows x cols up to 2^40 */
+  int64_t rows, cols;  /* >= 1, each up to 2^31 - 1; rows x cols below 2^38
+                          (FNO_ERR_UNSUPPORTED) */
 } fno_fp8_quantize_desc;
 
 /* x [rows][cols] to the codes of v = act(x): `codes` [rows][pitch(cols)] with
@@ -650,7 +653,8 @@ typedef struct {
  * [cols][pitch(rows)] with blocks along its own rows (the columns of x).
  * Either pair of codes and scales may be null.  With F the format's largest
  * value and a the largest size of a block's finite values, the scale is
- *     POW2   2^max(e, -126), e the least with a <= F 2^e;  F32  max(a / F, 2^-126);
+ *     POW2   2^max(e, -126), e the least with a <= F 2^e
+ *     F32    max(a (1 / F), 2^-126), both operations in fp32,
  * 1 where a = 0; the code is v times the scale's reciprocal (an fp32 product)
  * rounded to nearest, ties to even.  NaN stays NaN; an infinity becomes NaN in
  * e4m3.  col_sums, if not null, receives the sums of v over rows (fp32 [cols],
@@ -667,13 +671,18 @@ typedef struct {
   int32_t blocks_a, blocks_b;  /* fno_fp8_blocks */
   int32_t out_dtype;           /* fno_dtype of out and z */
   int32_t activation;          /* fno_norm_activation: whose derivative multiplies */
-  int64_t rows, cols, inner;   /* >= 1, each up to 2^31 - 1 */
+  int64_t rows, cols, inner;   /* >= 1, each up to 2^31 - 1, with rows x cols
+                                  below 2^37 (FNO_ERR_UNSUPPORTED where one
+                                  launch does not hold the tiles) */
 } fno_fp8_matmul_desc;
 
 /* out = (A B^T) act'(z) + bias:  A [rows][inner] and B [cols][inner] in codes,
  * out and z [rows][cols], bias fp32 [cols] (null: none).  z is null if and only
- * if the activation is NONE.  Products are exact, sums fp32 (a fixed order), one
- * rounding to out_dtype.  A row of codes is read whole, fno_fp8_pitch(inner)
+ * if the activation is NONE.  Sums are fp32 in a fixed order, with one rounding to
+ * out_dtype.  For out_dtype F32 every product enters them exactly; for 16-bit
+ * results the matrix instruction for 8-bit codes joins eight consecutive products
+ * at a time, each cut towards zero to a multiple of 2^-13 of the power of two below
+ * the largest of the eight.  A row of codes is read whole, fno_fp8_pitch(inner)
  * bytes: what stands behind `inner` has to be zero. */
 fno_status fno_fp8_matmul_workspace_size(const fno_fp8_matmul_desc *desc, size_t *bytes);
 fno_status fno_fp8_matmul(const fno_fp8_matmul_desc *desc, const void *a, const void *scale_a,

@@ -112,7 +112,8 @@ def block_scale(a, fmt, kind):
         k = np.frexp(top)[1]
         s = np.ldexp(1.0, np.maximum(e - k + (m > 0.875), -126))
     else:
-        s = np.maximum((safe / top).astype(np.float32), np.float32(2.0 ** -126)).astype(np.float64)
+        s = np.maximum(safe.astype(np.float32) * (np.float32(1.0) / np.float32(top)),
+                       np.float32(2.0 ** -126)).astype(np.float64)
     return np.where(a > 0, s, 1.0)
 
 

@@ -38,7 +38,7 @@ __device__ __forceinline__ BlockScale block_scale(float a, bool pow2) {
       s.byte = (unsigned)(e + 127);
       s.inv = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
     } else {
-      const float q = a / F;
+      const float q = a * (1.0f / F);  // (the fp32 reciprocal)
       s.scale = q < 0x1p-126f ? 0x1p-126f : q;
       s.inv = 1.0f / s.scale;
     }

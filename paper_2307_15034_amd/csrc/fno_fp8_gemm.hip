@@ -271,6 +271,12 @@ __device__ __forceinline__ float scale_of(int four, int m) {
   return __builtin_bit_cast(float, b == 255u ? 0x7fc00000u : b ? b << 23 : 0x00400000u);
 }
 
+// The tile's product.  Two stages of LDS: a block's tiles arrive while the one
+// before is multiplied; the matrix cores bound it (256 x 256, eight waves of 128 x
+// 64: their operands take 75% of LDS's rate; 128 x 128 tiles would take all of it).
+// 16384 x 4096 x 4096: 222 to 249 us with powers of two (2.2 to 2.5 PFLOP/s), 370 with fp32 scales, which the vector unit bounds
+// (eight operations for a 16 x 16 product of 32 cycles).  Wide, 4096 x 4096 x 8192:
+// 207 us (1.33 PFLOP/s).
 template <int FA, int FB, bool F32S, bool WIDE, int BM, int BN, int WGM, int WGN, int STAGES = 2>
 __global__ __launch_bounds__(64 * WGM * WGN, STAGES == 1 ? 3 : 1) void gemm_kernel(MatmulArgs g) {
   constexpr int THREADS = 64 * WGM * WGN;
@@ -474,7 +480,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, STAGES == 1 ? 3 : 1) void gemm_kern
 // Few rows: the work is in reading B.  A work-group takes 16 of its rows, a wave
 // every eighth block of them, straight from memory into the operands (row i of A
 // and B: lanes i, i + 16, ..); the waves' sums meet in LDS, in their order.  One
-// row of 4096 by 4096 x 4096: MEASURE.
+// row of 4096 by 4096 x 4096: 5.5 us (3.1 TB/s of codes); split tiles and their join
+// took 5.1 + 2.8.
 constexpr int kRowWaves = 8;
 template <int FA, int FB, bool F32S, bool WIDE, int MT>
 __global__ __launch_bounds__(64 * kRowWaves) void few_rows_kernel(MatmulArgs g) {
@@ -633,7 +640,7 @@ MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
   const int64_t of256 = fp8_cdiv(g.M, 256) * fp8_cdiv(g.N, 256);
   // Few rows of B's worth: up to 64 rows, while a wave's share of the inner axis
   // stays short (products of weights' gradients have few rows and a long one).
-  p.tile = g.M <= 64 && g.kb <= 256 ? FEW_ROWS
+  p.tile = g.M <= 64 && g.kb <= 256 && g.N < ((int64_t)1 << 26) ? FEW_ROWS
            : g.kb == 1 && g.N <= 64 && g.M > 128 ? TILE_NARROW
            : pow2 && of256 >= 192 && g.N > 128 ? TILE_256
                                                : TILE_128;
@@ -650,6 +657,12 @@ MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
   g.kb_per_split = (int)fp8_cdiv(g.kb, g.splits);
   g.splits = (int)fp8_cdiv(g.kb, g.kb_per_split);
   return p;
+}
+
+// Whether a launch's threads (512 or 256 for a tile) would pass 2^32.
+bool too_many(const MatmulPlan& p) {
+  const int64_t most = p.tile == TILE_256 || p.tile == FEW_ROWS ? (int64_t)1 << 23 : (int64_t)1 << 24;
+  return p.g.tiles_m * p.g.tiles_n >= most;
 }
 
 struct MatmulLaunch {
@@ -716,7 +729,9 @@ extern "C" fno_status fno_fp8_matmul_workspace_size(const fno_fp8_matmul_desc* d
   const fno_status st = check_desc(d);
   if (st != FNO_OK) return st;
   if (!bytes) return FNO_ERR_INVALID_ARGUMENT;
-  *bytes = ws_bytes(plan_of(*d));
+  const MatmulPlan p = plan_of(*d);
+  if (too_many(p)) return FNO_ERR_UNSUPPORTED;
+  *bytes = ws_bytes(p);
   return FNO_OK;
 }
 
@@ -735,7 +750,7 @@ extern "C" fno_status fno_fp8_matmul(const fno_fp8_matmul_desc* d, const void* a
     if (ws_len < ws_bytes(L.p)) return FNO_ERR_WORKSPACE_TOO_SMALL;
     if (!fp8_ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
   }
-  if (L.p.g.tiles_m * L.p.g.tiles_n > INT32_MAX) return FNO_ERR_UNSUPPORTED;
+  if (too_many(L.p)) return FNO_ERR_UNSUPPORTED;
   MatmulArgs& g = L.p.g;
   g.a = static_cast<const uint8_t*>(a);
   g.b = static_cast<const uint8_t*>(b);

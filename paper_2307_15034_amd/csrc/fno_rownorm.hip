@@ -140,6 +140,8 @@ RowPlan plan_of(const fno_residual_norm_desc& d, bool bwd) {
 }
 
 constexpr int64_t kMaxGrid = (int64_t)1 << 20;
+// Work-groups of a launch: their threads (up to 1024) stay below 2^32.
+constexpr int64_t kMaxUnits = ((int64_t)1 << 22) - 1;
 
 fno_status set_params(RowNormArgs* a, const fno_residual_norm_desc& d,
                       const fno_residual_norm_params* q, bool post, bool pre) {
@@ -209,7 +211,7 @@ extern "C" fno_status fno_residual_norm_workspace_size(const fno_residual_norm_d
   if (st != FNO_OK) return st;
   if (!bytes) return FNO_ERR_INVALID_ARGUMENT;
   const RowPlan p = plan_of(*d, true);
-  if (p.units > INT32_MAX) return FNO_ERR_UNSUPPORTED;
+  if (p.units > kMaxUnits) return FNO_ERR_UNSUPPORTED;
   *bytes = (size_t)ws_bytes(*d, p);
   return FNO_OK;
 }
@@ -224,7 +226,7 @@ extern "C" fno_status fno_residual_norm_fwd(const fno_residual_norm_desc* d,
   RowLaunch L{plan_of(*d, false), d->dtype, u != nullptr, h != nullptr, {}, stream};
   st = set_params(&L.p.a, *d, params, L.post, L.pre);
   if (st != FNO_OK) return st;
-  if (L.p.units > INT32_MAX) return FNO_ERR_UNSUPPORTED;
+  if (L.p.units > kMaxUnits) return FNO_ERR_UNSUPPORTED;
   L.p.a.x = x;
   L.p.a.u = u;
   L.p.a.y = y;
@@ -258,7 +260,7 @@ extern "C" fno_status fno_residual_norm_bwd(const fno_residual_norm_desc* d,
   RowLaunch L{plan_of(*d, true), d->dtype, post, pre, {}, stream};
   st = set_params(&L.p.a, *d, params, post, pre);
   if (st != FNO_OK) return st;
-  if (L.p.units > INT32_MAX) return FNO_ERR_UNSUPPORTED;
+  if (L.p.units > kMaxUnits) return FNO_ERR_UNSUPPORTED;
   const bool row_gate = d->gate_rows == d->rows;
   RowNormArgs& a = L.p.a;
   void* const out[RS_COUNT] = {grads->post_w, grads->post_b, row_gate ? nullptr : grads->gate,

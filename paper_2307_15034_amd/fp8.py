@@ -54,6 +54,8 @@ class _Shape:
 
     def check(self, m, name, device):
         """Addresses of a matrix's codes and scales."""
+        if len(m) != 2 or m[0] is None or m[1] is None:
+            raise ValueError(f"{name}: codes and scale are required")
         return (_addr(m[0], self.codes, self.type, f"{name}.codes", device),
                 _addr(m[1], self.scale, self.scale_type, f"{name}.scale", device))
 
@@ -92,7 +94,8 @@ class Fp8Quantize:
     """Rounds act(x), x [..., cols] with `rows` rows of `dtype`, to codes.
 
     A block's scale is the least power of two (`pow2_scales`) that brings its
-    largest size within the format's, or that size over the format's in fp32.
+    largest size within the format's, or that size times the fp32 reciprocal of the
+    format's.
     Blocks are 128 columns of a row, and 128 rows of a column for the transpose;
     with `tile`, 128 x 128 for both.
 

@@ -97,3 +97,17 @@ def test_fp8_call_refusals():
     assert B.fno_fp8_matmul(d, **{**call, "ws_bytes": 255}, check=False) == B.FNO_ERR_WORKSPACE_TOO_SMALL
     d = B.make_fp8_matmul_desc(10, 20, 30, activation=B.FNO_NORM_ACT_GELU)
     assert B.fno_fp8_matmul(d, **call, check=False) == BAD
+
+
+def test_sizes_past_a_launch_are_refused():
+    none = B.FNO_ERR_UNSUPPORTED
+    d = B.make_fp8_quantize_desc(1 << 19, 1 << 19)
+    for call in (lambda: B.fno_fp8_quantize_workspace_size(d),
+                 lambda: B.fno_fp8_quantize(d, A, A, A, 0, 0, 0, A, 1 << 40, 0),
+                 lambda: B.fno_fp8_matmul_workspace_size(B.make_fp8_matmul_desc((1 << 31) - 1, 2048, 64)),
+                 lambda: B.fno_residual_norm_workspace_size(B.make_residual_norm_desc(1 << 24, 8, 1 << 23))):
+        with pytest.raises(B.FnoError) as e:
+            call()
+        assert e.value.status == none
+    assert B.fno_fp8_matmul_workspace_size(B.make_fp8_matmul_desc((1 << 31) - 1, 1, 64)) == 256
+    assert B.fno_residual_norm_workspace_size(B.make_residual_norm_desc(1 << 24, 8, 1 << 24)) > 0

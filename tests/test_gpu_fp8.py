@@ -492,3 +492,70 @@ def test_wrapper_refusals():
                dict(rows=8, c_in=8, c_out=8, grad_format=2)):
         with pytest.raises((ValueError, B.FnoError)):
             Fp8Linear(**kw)
+
+
+def test_nan_scales_in_the_tiled_products():
+    """Byte 255 in the 8-bit instruction's own scales, of rows and of columns."""
+    op, a, b, _, _, out = _matmul(300, 200, 300, dt="bf16")
+    sa, sb = a.scale.view(torch.uint8).clone(), b.scale.view(torch.uint8).clone()
+    sa[2, 130] = 255
+    sb[0, 199] = 255
+    f = lambda s: s.view(torch.float8_e8m0fnu)  # noqa: E731
+    got = op.run(Fp8Codes(a.codes, f(sa)), Fp8Codes(b.codes, f(sb)))
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[130] = True
+    bad[:, 199] = True
+    assert bool(got[bad].isnan().all()) and torch.equal(got[~bad], out[~bad])
+
+
+def test_codes_that_are_not_a_number_stay_alone():
+    for dt, fmt, m in (("bf16", "e4m3", 300), ("fp32", "e5m2", 300), ("fp16", "e5m2", 20)):
+        op, a, b, _, _, out = _matmul(m, 140, 200, fmt, "e4m3", dt=dt)
+        c = a.codes.view(torch.uint8).clone()
+        c[m - 3, 150] = 0x7F
+        got = op.run(Fp8Codes(c.view(TYPE[fmt]), a.scale), b)
+        keep = torch.arange(m, device="cuda") != m - 3
+        assert bool(got[m - 3].isnan().all()) and torch.equal(got[keep], out[keep])
+
+
+def test_rows_of_codes_longer_than_a_tiles_offsets():
+    """Rows of 16.8 M codes: a tile's rows lie more than 2^31 bytes apart."""
+    m, n, k = 130, 3, 16_800_000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    draw = lambda r: torch.randint(0, 4, (r, k), dtype=torch.uint8, device="cuda", generator=g)  # noqa: E731
+    table = torch.tensor([0x00, 0x38, 0xB8, 0x30], dtype=torch.uint8, device="cuda")  # 0, 1, -1, 1/2
+    value = torch.tensor([0.0, 1.0, -1.0, 0.5], device="cuda")
+    a, b = draw(m), draw(n)
+    ones = lambda r: torch.full((-(-k // 128), r), 127, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)  # noqa: E731
+    want = torch.zeros(m, n, dtype=torch.float64, device="cuda")
+    ac, bc = torch.empty_like(a), torch.empty_like(b)
+    for j in range(0, k, 1 << 20):
+        s = slice(j, j + (1 << 20))
+        want += value[a[:, s].int()].double() @ value[b[:, s].int()].double().t()
+        ac[:, s], bc[:, s] = table[a[:, s].int()], table[b[:, s].int()]
+    op = Fp8Matmul(m, n, k, torch.float32)
+    got = op.run(Fp8Codes(ac.view(torch.float8_e4m3fn), ones(m)), Fp8Codes(bc.view(torch.float8_e4m3fn), ones(n)))
+    # halves: sums below 2^23 are exact in fp32, in any order
+    assert float(want.abs().max()) < 2 ** 22 and torch.equal(got.double(), want)
+
+
+def test_matrices_past_32_bits():
+    """More than 2^32 codes; the last rows against the same rows alone."""
+    rows, cols = (1 << 16) + 77, 66000
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x.normal_(generator=g)
+    w = torch.randn(40, cols, device="cuda", generator=g).bfloat16()
+    op = Fp8Linear(rows, cols, 40, torch.bfloat16)
+    p = op.pack(w)
+    y, kept = op.fwd(x, p)
+    tail = 205  # (the last blocks of 128 rows begin at a multiple)
+    some = Fp8Linear(tail, cols, 40, torch.bfloat16)
+    y2, kept2 = some.fwd(x[-tail:].contiguous(), p)
+    # the tiles differ, so do the groups of eight's joins' order: not more than twice the rounding
+    assert bool(((y[-tail:] - y2).abs().float() <= 2.0 ** -7 * y2.abs().float() + 1e-2).all())
+    at = rows - tail
+    assert at % 128 == 0
+    pitch = kept2.codes.shape[1]
+    assert torch.equal(kept.codes.view(torch.uint8)[:, at:at + pitch], kept2.codes.view(torch.uint8))
+    assert torch.equal(kept.scale.view(torch.uint8)[at // 128:], kept2.scale.view(torch.uint8))

@@ -228,3 +228,34 @@ def test_wrapper_refusals():
             ResidualNorm(**kw)
     with pytest.raises(ValueError):
         ResidualNorm(4, 4, torch.float64)
+
+
+def test_one_row_with_a_gate():
+    for c in (1, 5, 64, 300):
+        for dt in ("fp32", "bf16"):
+            _check(1, c, dt, gates=1, gate_dt=dt)
+
+
+def test_rows_past_32_bits():
+    """More than 2^31 values; the last rows against the same rows alone."""
+    rows, c = (1 << 22) + 37, 520
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty(rows, c, dtype=torch.float16, device="cuda").normal_(generator=g)
+    u = torch.empty_like(x).normal_(generator=g)
+    w = 1 + 0.2 * torch.randn(c, device="cuda", generator=g)
+    y, h = ResidualNorm(rows, c).fwd(x, u, post_w=w, scale=w)
+    got = ResidualNorm(rows, c).bwd(x, u, x=x, u=u, y=y, post_w=w, scale=w)
+    n = 100
+    last = [t[-n:].clone() for t in (x, u, y)]
+    small = ResidualNorm(n, c)
+    y2, h2 = small.fwd(last[0], last[1], post_w=w, scale=w)
+    got2 = small.bwd(last[0], last[1], x=last[0], u=last[1], y=last[2], post_w=w, scale=w)
+    assert torch.equal(y[-n:], y2) and torch.equal(h[-n:], h2)
+    assert torch.equal(got["g_x"][-n:], got2["g_x"]) and torch.equal(got["g_u"][-n:], got2["g_u"])
+    # the parameters' sums against torch's own, in pieces
+    want = sum(((got["g_x"][i:i + (1 << 18)].double() / w.double()) * x[i:i + (1 << 18)].double()).sum(0)
+               for i in range(0, rows, 1 << 18))
+    size = sum(((got["g_x"][i:i + (1 << 18)].double() / w.double()) * x[i:i + (1 << 18)].double()).abs().sum(0)
+               for i in range(0, rows, 1 << 18))
+    # g_x is rounded to fp16 (2^-11 of each term, of either sign): far within 2^-11 of the sum of sizes
+    assert bool(((got["g_scale"].double() - want).abs() <= 2.0 ** -11 * size).all())
