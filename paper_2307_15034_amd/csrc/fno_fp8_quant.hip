@@ -62,6 +62,25 @@ __device__ __forceinline__ void put_scale(void* out, int64_t at, const BlockScal
     static_cast<float*>(out)[at] = s.scale;
 }
 
+// SiLU as exact as fp32: the exponential of the argument's product with log2 e and
+// that product's own remainder, the reciprocal with one step of Newton's.
+__device__ __forceinline__ float silu32_of(float z) {
+  const float hi = z * -1.44269502f;
+  const float lo = __builtin_fmaf(z, -1.92596299e-08f, __builtin_fmaf(z, -1.44269502f, -hi));
+  float e = __builtin_amdgcn_exp2f(hi);
+  e = __builtin_fmaf(e, lo * 0.693147182f, e);
+  const float d = 1.0f + e;
+  float r = __builtin_amdgcn_rcpf(d);
+  r = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
+  return __builtin_fabsf(z) < 87.0f ? z * r : silu_f(z);
+}
+// What is rounded to eight bits is formed in fp32 as exactly as fp32 tensors are,
+// whatever the type of x: an error beside a border between two codes becomes a
+// whole step of the code.
+__device__ __forceinline__ float act32_of(float z, int act) {
+  return act == FNO_NORM_ACT_GELU ? gelu32_of(z) : act == FNO_NORM_ACT_SILU ? silu32_of(z) : z;
+}
+
 // The 8 x 8 values of a thread.  16-bit values without an activation stay in
 // pairs: sizes are compared as whole numbers, two at a time, and with powers of
 // two the conversion takes pairs and divides them itself (exactly).  Three
@@ -82,7 +101,7 @@ struct Values {
       __builtin_memcpy(p[i], t, sizeof(t));
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[i][j] = ACT ? act_any<T>((float)t[j], act) : (float)t[j];
+      for (int j = 0; j < 8; ++j) f[i][j] = ACT ? act32_of((float)t[j], act) : (float)t[j];
     }
   }
   __device__ __forceinline__ float at(int i, int j) const {

@@ -191,8 +191,8 @@ struct RowStat {
 // Means and 1 / sqrt(var + eps) of K rows at once (v[k]: a thread's values,
 // `valid` of each vector's are the row's).  The mean is of values scaled by a
 // power of two, whose sum stays within fp32; the squares are of distances from
-// it.  Where their sum leaves what fp32 holds exactly enough (rows far larger
-// than 2^45, or as small as eps = 0 would need), they are formed again at
+// it.  Where their sum leaves what fp32 holds exactly enough (rows larger
+// than 2^60 or so, or as small as eps = 0 would need), they are formed again at
 // another power of two.
 template <int K, int VPT, int V, int TEAM>
 __device__ __forceinline__ void row_stats(Team<TEAM>& team, const float (&v)[K][VPT][V],
