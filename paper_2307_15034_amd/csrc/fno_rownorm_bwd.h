@@ -224,7 +224,8 @@ template <typename T, bool POST, bool PRE, int MODE>
 hipError_t launch_mode(const RowNormArgs& a, const RowLaunchSize& l, hipStream_t s) {
 #define FNO_ROW(T_, V_)                                                                        \
   if (l.team == T_ && l.vecs == V_) {                                                          \
-    row_norm_bwd_kernel<T, T_, V_, MODE, POST, PRE><<<dim3(l.grid), dim3(row_threads(T_)), 0, s>>>(a); \
+    if constexpr (T_ * V_ * kRowVec<T> <= 16384) /* the longest row */ \
+      row_norm_bwd_kernel<T, T_, V_, MODE, POST, PRE><<<dim3(l.grid), dim3(row_threads(T_)), 0, s>>>(a); \
     return hipGetLastError();                                                                  \
   }
   if constexpr (MODE == ROW_SHORT) {  // one vector
