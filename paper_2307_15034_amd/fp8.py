@@ -100,8 +100,9 @@ class Fp8Quantize:
     with `tile`, 128 x 128 for both.
 
     An object keeps one workspace, memory of the first call's stream, so its
-    calls belong on one stream (or on streams that wait for each other).  Where
-    `stream` is given, outputs are the caller's too.
+    calls belong on one stream (or on streams that wait for each other), and it
+    outlives the graphs that hold its calls.  Where `stream` is given, outputs are
+    the caller's too.
     """
 
     def __init__(self, rows: int, cols: int, dtype: torch.dtype = torch.float16,

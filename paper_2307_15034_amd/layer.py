@@ -460,16 +460,21 @@ class GroupNormAct:
 class _Workspace:
     """Scratch memory that an object keeps: taken from the memory of the first
     call's stream, taken anew where a call needs more or runs on another device,
-    and kept from others until the work of every stream that used it is done."""
+    and kept from others until the work of every stream that used it is done.
+    What was taken before stays with the object: a captured graph holds its
+    address, which no one else's memory may have while the graph can be replayed."""
 
     def __init__(self):
         self._t: Optional[torch.Tensor] = None
         self._stream = 0
+        self._before: List[torch.Tensor] = []
 
     def get(self, nbytes: int, device: torch.device, s: int):
         """(address, bytes) for a call on stream `s`."""
         t = self._t
         if t is None or t.device != device or t.numel() < nbytes:
+            if t is not None:
+                self._before.append(t)
             if s == torch.cuda.current_stream(device).cuda_stream:
                 t = torch.empty(nbytes, dtype=torch.uint8, device=device)
             else:
@@ -499,9 +504,11 @@ class ResidualNorm:
     gate_rows a divisor of rows: [1, C] for all rows, [batch, C] per sample,
     [rows, C] per row (None: 1).
 
-    The backward keeps one workspace, memory of the first call's stream, so an
-    object's backward calls belong on one stream (or on streams that wait for
-    each other).  Where `stream` is given, outputs are the caller's too.
+    The backward keeps one workspace, memory of the first call's stream (and the
+    smaller ones before it, where a gate of more rows needed more), so an object's
+    backward calls belong on one stream (or on streams that wait for each other),
+    and an object outlives the graphs that hold its calls.  Where `stream` is given,
+    outputs are the caller's too.
     """
 
     PARAMS = ("post_w", "post_b", "gate", "scale", "pre_w", "pre_b")

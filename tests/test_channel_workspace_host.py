@@ -1,0 +1,23 @@
+"""The scratch memory that the operators over channels keep (no GPU needed: the
+memory is the CPU's, and streams are numbers)."""
+import types
+import weakref
+
+import pytest
+
+torch = pytest.importorskip("torch")
+L = pytest.importorskip("paper_2307_15034_amd.layer")
+
+
+def test_a_workspace_that_was_handed_out_stays(monkeypatch):
+    """A captured graph holds the address of the workspace that its calls got.  A
+    later call that needs more gets another one; the first is not given back."""
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: types.SimpleNamespace(cuda_stream=0))
+    ws, cpu = L._Workspace(), torch.device("cpu")
+    seen = []
+    for nbytes in (256, 1024, 512, 4096):
+        at, n = ws.get(nbytes, cpu, 0)
+        assert n >= nbytes and at == ws._t.data_ptr()
+        seen.append((at, weakref.ref(ws._t)))
+    assert all(t() is not None and t().data_ptr() == at for at, t in seen)
+    assert seen[1][0] == seen[2][0] and len({at for at, _ in seen}) == 3
