@@ -547,7 +547,7 @@ class ResidualNorm:
     def _params(self, p, device):
         """(addresses, (descriptor, workspace bytes)) of parameters in their order."""
         shape, gate = (self.channels,), p[2]
-        at = [0 if t is None or t is gate else _addr(t, shape, torch.float32, k, device)
+        at = [0 if t is None or k == "gate" else _addr(t, shape, torch.float32, k, device)
               for k, t in zip(self.PARAMS, p)]
         if gate is None:
             return B.FnoResidualNormParams(*at), self._desc(0, torch.float32)

@@ -1,5 +1,5 @@
-"""The scratch memory that the operators over channels keep (no GPU needed: the
-memory is the CPU's, and streams are numbers)."""
+"""Checks of the wrappers of the operators over channels, and the scratch memory that
+they keep (no GPU needed: the memory is the CPU's, and streams are numbers)."""
 import types
 import weakref
 
@@ -21,3 +21,14 @@ def test_a_workspace_that_was_handed_out_stays(monkeypatch):
         seen.append((at, weakref.ref(ws._t)))
     assert all(t() is not None and t().data_ptr() == at for at, t in seen)
     assert seen[1][0] == seen[2][0] and len({at for at, _ in seen}) == 3
+
+
+def test_a_gate_in_the_place_of_another_parameter_is_refused():
+    """The same tensor as gate and as a parameter of one row: its shape is not the
+    parameter's."""
+    op = L.ResidualNorm(8, 16)
+    one = torch.ones(1, 16)
+    for k in ("post_w", "post_b", "scale", "pre_w", "pre_b"):
+        p = {**dict.fromkeys(op.PARAMS), "gate": one, k: one}
+        with pytest.raises(ValueError, match=k):
+            op._params(tuple(p.values()), False)  # (layout checks alone: no GPU)
