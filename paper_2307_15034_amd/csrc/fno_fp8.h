@@ -69,6 +69,7 @@ struct QuantArgs {
   int cols;
   int act, pow2, tile;
   int64_t blocks_r, blocks_c;  // blocks of 128 along the rows and the columns
+  int64_t groups;              // work-groups of the launch
 };
 
 struct MatmulArgs {

@@ -258,13 +258,16 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
   __shared__ float red[2][4][COLUMNS ? CG * 8 : 1];
   __shared__ __attribute__((aligned(16))) uint8_t turned[COLUMNS ? BLOCKS * CG * 8 * kBlock : 16];
   const int cg = threadIdx.x % CG, rg = threadIdx.x / CG, wave = threadIdx.x >> 6;
-  const int64_t tiles_c = (a.cols + CG * 8 - 1) / (CG * 8);
+  const int64_t tiles_c = ((int64_t)a.cols + CG * 8 - 1) / (CG * 8);
   // A die's work-groups (every eighth) take consecutive tiles: what they write of a
   // line of memory meets in one cache.
-  const int64_t each = gridDim.x >> 3;
-  const int64_t id = blockIdx.x < each * 8 ? (blockIdx.x & 7) * each + (blockIdx.x >> 3) : blockIdx.x;
+  int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (id >= a.groups) return;
+  const int64_t each = a.groups >> 3;
+  if (id < each * 8) id = (id & 7) * each + (id >> 3);
   const int64_t tr = id / tiles_c;
-  const int c0 = (int)(id - tr * tiles_c) * (CG * 8) + cg * 8;
+  // (the last tile's columns may pass 2^31)
+  const unsigned c0 = (unsigned)(id - tr * tiles_c) * (CG * 8) + cg * 8;
   const int64_t r0 = tr * (RG * 8) + rg * 8;
   constexpr bool pow2 = POW2;
   Values<T, FMT, ACT, POW2> v;
@@ -273,10 +276,10 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
   // behind the last repeat it and are zeroed, and where a row ends inside the eight
   // columns its last eight are read and moved down.
   T t[8][8];
-  const int cols = a.cols, left = cols - c0;  // columns from c0 on
+  const int cols = a.cols, left = (int)((unsigned)cols - c0);  // columns from c0 on
   const bool whole = (cols & 7) == 0;
   if (cols >= 8) {
-    const int at = left >= 8 ? c0 : cols - 8;
+    const int at = left >= 8 ? (int)c0 : cols - 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = r0 + i < a.rows ? r0 + i : a.rows - 1;
@@ -345,7 +348,7 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
     if (a.part && rg % 16 == 0 && r0 < a.rows) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (c0 + j < a.cols) a.part[block_r * a.cols + c0 + j] = sum[j];
+        if (j < left) a.part[block_r * a.cols + c0 + j] = sum[j];
     }
   }
   BlockScale one{};
@@ -389,14 +392,14 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const BlockScale s = a.tile ? one : block_scale<FMT>(top[j], pow2);
-      if (!a.tile && piece == 0 && r0 < a.rows && c0 + j < a.cols)
+      if (!a.tile && piece == 0 && r0 < a.rows && j < left)
         put_scale(a.scale_t, block_r * a.cols + c0 + j, s, pow2);
       *reinterpret_cast<uint2*>(turned + ((block * CG + cg) * 8 + j) * kBlock + (piece ^ cg) * 8) =
           v.col_codes(j, s);
     }
     __syncthreads();
     const int64_t first = tr * (RG * 8);
-    const int cfirst = c0 - cg * 8;
+    const int64_t cfirst = c0 - cg * 8;
 #pragma unroll
     for (int i = 0; i < BLOCKS * CG * 8 * 8 / QT; ++i) {
       const int t = threadIdx.x + i * QT, at = t & 7, line = t >> 3;  // line: block, column
@@ -405,7 +408,7 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
       if (cfirst + col < a.cols && row < a.pitch_t) {
         uint4 q = *reinterpret_cast<const uint4*>(turned + line * kBlock + ((2 * at ^ of) & 14) * 8);
         if (of & 1) q = uint4{q.z, q.w, q.x, q.y};
-        *reinterpret_cast<uint4*>(a.codes_t + (int64_t)(cfirst + col) * a.pitch_t + row) = q;
+        *reinterpret_cast<uint4*>(a.codes_t + (cfirst + col) * a.pitch_t + row) = q;
       }
     }
   }
@@ -419,7 +422,8 @@ __global__ __launch_bounds__(1024) void col_sum_kernel(const float* part, float*
   constexpr int QUADS = COLS / 4, LANES = 1024 / QUADS;
   __shared__ double red[16][COLS];
   const int quad = threadIdx.x % QUADS, lane = threadIdx.x / QUADS;
-  const int64_t c = (int64_t)blockIdx.x * COLS + quad * 4;
+  const int64_t group = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int64_t c = group * COLS + quad * 4;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
   if (c + 4 <= cols) {
 #pragma unroll 4
@@ -444,7 +448,7 @@ __global__ __launch_bounds__(1024) void col_sum_kernel(const float* part, float*
     for (int j = 0; j < 4; ++j) red[threadIdx.x >> 6][quad * 4 + j] = s[j];
   }
   __syncthreads();
-  const int64_t mine = (int64_t)blockIdx.x * COLS + threadIdx.x;
+  const int64_t mine = group * COLS + threadIdx.x;
   if (threadIdx.x < COLS && mine < cols) {
     double t = red[0][threadIdx.x];
 #pragma unroll
@@ -478,16 +482,24 @@ struct QuantLaunch {
   hipStream_t stream;
 };
 
+// A launch's threads stay below 2^32 along an axis: more work-groups than a row of
+// the grid holds go on in the next one (the last row's surplus leaves at once).
+dim3 grid_of(int64_t groups) {
+  constexpr int64_t kRow = 1 << 20;
+  return groups <= kRow ? dim3((unsigned)groups) : dim3((unsigned)kRow, (unsigned)fp8_cdiv(groups, kRow));
+}
+
 template <typename T, int FMT, int CG>
 hipError_t launch_tiles(const QuantLaunch& L) {
-  const int64_t grid = fp8_cdiv(L.a.rows, QT / CG * 8) * fp8_cdiv(L.a.cols, CG * 8);
-  const dim3 g((unsigned)grid), t(QT);
-  if (L.a.act == FNO_NORM_ACT_NONE)
-    L.a.pow2 ? quantize_kernel<T, FMT, CG, false, true><<<g, t, 0, L.stream>>>(L.a)
-             : quantize_kernel<T, FMT, CG, false, false><<<g, t, 0, L.stream>>>(L.a);
+  QuantArgs a = L.a;
+  a.groups = fp8_cdiv(a.rows, QT / CG * 8) * fp8_cdiv(a.cols, CG * 8);
+  const dim3 g = grid_of(a.groups), t(QT);
+  if (a.act == FNO_NORM_ACT_NONE)
+    a.pow2 ? quantize_kernel<T, FMT, CG, false, true><<<g, t, 0, L.stream>>>(a)
+           : quantize_kernel<T, FMT, CG, false, false><<<g, t, 0, L.stream>>>(a);
   else
-    L.a.pow2 ? quantize_kernel<T, FMT, CG, true, true><<<g, t, 0, L.stream>>>(L.a)
-             : quantize_kernel<T, FMT, CG, true, false><<<g, t, 0, L.stream>>>(L.a);
+    a.pow2 ? quantize_kernel<T, FMT, CG, true, true><<<g, t, 0, L.stream>>>(a)
+           : quantize_kernel<T, FMT, CG, true, false><<<g, t, 0, L.stream>>>(a);
   return hipGetLastError();
 }
 template <typename T, int FMT>
@@ -510,21 +522,15 @@ hipError_t launch_quantize(void* ctx) {
                                                   : launch_format<__bf16>(L);
   if (e != hipSuccess || !L.col_sums) return e;
   if (L.a.blocks_r > 512)
-    col_sum_kernel<4><<<dim3((unsigned)fp8_cdiv(L.a.cols, 4)), dim3(1024), 0, L.stream>>>(
+    col_sum_kernel<4><<<grid_of(fp8_cdiv(L.a.cols, 4)), dim3(1024), 0, L.stream>>>(
         L.a.part, L.col_sums, L.a.blocks_r, L.a.cols);
   else
-    col_sum_kernel<32><<<dim3((unsigned)fp8_cdiv(L.a.cols, 32)), dim3(1024), 0, L.stream>>>(
+    col_sum_kernel<32><<<grid_of(fp8_cdiv(L.a.cols, 32)), dim3(1024), 0, L.stream>>>(
         L.a.part, L.col_sums, L.a.blocks_r, L.a.cols);
   return hipGetLastError();
 }
 
-// Work-groups of a launch, whose threads have to stay below 2^32; a launch has at
-// most one for each 2048 values and each edge of its tiles.
-bool too_many(const fno_fp8_quantize_desc& d) {
-  const int64_t narrow = fp8_cdiv(d.rows, 32) * fp8_cdiv(d.cols, 512);
-  const int64_t wide = fp8_cdiv(d.rows, 128) * fp8_cdiv(d.cols, 128);
-  return std::max(narrow, wide) >= (int64_t)1 << 24;
-}
+bool too_many(const fno_fp8_quantize_desc& d) { return d.rows > (((int64_t)1 << 38) - 1) / d.cols; }
 
 size_t ws_bytes(const fno_fp8_quantize_desc& d) {
   return (size_t)std::max<int64_t>(256, fp8_cdiv(fp8_cdiv(d.rows, kBlock) * d.cols * 4, 256) * 256);

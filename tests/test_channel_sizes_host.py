@@ -1,0 +1,30 @@
+"""Sizes that the C entry points of the 8-bit codes accept (no GPU needed)."""
+import pytest
+
+B = pytest.importorskip("paper_2307_15034_amd.binding")
+
+MOST = (1 << 31) - 1
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 29, 8), (1 << 30, 1), (1 << 29, 20), (1 << 29, 64), (MOST, 1),
+                                       (MOST, 16), (MOST, 127), (1, MOST), (127, MOST), (1, MOST - 300),
+                                       ((1 << 19) - 1, 1 << 19)])
+def test_codes_of_every_size_below_2_38(rows, cols):
+    for blocks in (B.FNO_BLOCKS_ROW, B.FNO_BLOCKS_TILE):
+        d = B.make_fp8_quantize_desc(rows, cols, blocks=blocks)
+        assert B.fno_fp8_quantize_workspace_size(d) >= -(-rows // 128) * cols * 4
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 19, 1 << 19), (129, MOST), (MOST, 129)])
+def test_codes_of_2_38_values_are_refused(rows, cols):
+    with pytest.raises(B.FnoError) as e:
+        B.fno_fp8_quantize_workspace_size(B.make_fp8_quantize_desc(rows, cols))
+    assert e.value.status == B.FNO_ERR_UNSUPPORTED
+
+
+def test_linear_maps_over_large_grids():
+    """Four grids of 512^3 points."""
+    F = pytest.importorskip("paper_2307_15034_amd.fp8")
+    for c_in, c_out in ((8, 32), (64, 64), (20, 80)):
+        op = F.Fp8Linear(1 << 29, c_in, c_out)
+        assert op.q_x.shape_t.codes == (c_in, 1 << 29)
