@@ -101,7 +101,20 @@ struct Values {
       __builtin_memcpy(p[i], t, sizeof(t));
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[i][j] = ACT ? act32_of((float)t[j], act) : (float)t[j];
+      for (int j = 0; j < 8; ++j) f[i][j] = ACT ? act32_of((float)t[j], act) : quiet(t[j]);
+    }
+  }
+  // In fp32, a signaling NaN made quiet: fmax leaves out a quiet one, but of a
+  // signaling one makes NaN, behind which the largest size so far is lost.  (fp16's
+  // conversion quiets, so does arithmetic; bfloat16's is a shift.)
+  static __device__ __forceinline__ float quiet(T v) {
+    if constexpr (std::is_same_v<T, float>) {
+      return __builtin_canonicalizef(v);
+    } else if constexpr (std::is_same_v<T, _Float16>) {
+      return (float)v;
+    } else {
+      return __builtin_canonicalizef(
+          __builtin_bit_cast(float, (unsigned)__builtin_bit_cast(unsigned short, v) << 16));
     }
   }
   __device__ __forceinline__ float at(int i, int j) const {
