@@ -613,7 +613,8 @@ fno_status fno_residual_norm_fwd(const fno_residual_norm_desc *desc,
  *     g_u = (gradient of the first norm at u)(gate G),
  * and the parameters' gradients, sums over rows.  y (the forward's) is needed
  * with g_h, x only for the scale's gradient.  Without u, x takes the place of y
- * and g_u is null.  g_x may be the buffer of g_y or g_h, g_u that of u or g_h. */
+ * and g_u is null.  g_x may be the buffer of g_y or g_h, g_u that of u or g_h; no
+ * two results share a buffer. */
 fno_status fno_residual_norm_workspace_size(const fno_residual_norm_desc *desc, size_t *bytes);
 fno_status fno_residual_norm_bwd(const fno_residual_norm_desc *desc,
                                  const fno_residual_norm_params *params, const void *x,
@@ -658,7 +659,7 @@ typedef struct {
  * 1 where a = 0; the code is v times the scale's reciprocal (an fp32 product)
  * rounded to nearest, ties to even.  NaN stays NaN; an infinity becomes NaN in
  * e4m3.  col_sums, if not null, receives the sums of v over rows (fp32 [cols],
- * fixed order: what a bias's gradient is). */
+ * fixed order: what a bias's gradient is).  No two results share a buffer. */
 int64_t fno_fp8_pitch(int64_t cols);
 fno_status fno_fp8_quantize_workspace_size(const fno_fp8_quantize_desc *desc, size_t *bytes);
 fno_status fno_fp8_quantize(const fno_fp8_quantize_desc *desc, const void *x, void *codes,

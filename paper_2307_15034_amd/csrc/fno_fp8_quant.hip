@@ -581,6 +581,7 @@ extern "C" fno_status fno_fp8_quantize(const fno_fp8_quantize_desc* d, const voi
     if (ws_len < ws_bytes(*d)) return FNO_ERR_WORKSPACE_TOO_SMALL;
     if (!fp8_ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
   }
+  if (any_twice({codes, scale, codes_t, scale_t, col_sums})) return FNO_ERR_INVALID_ARGUMENT;
   QuantLaunch L{{}, d->dtype, d->format, col_sums, stream};
   QuantArgs& a = L.a;
   a.x = x;

@@ -3,6 +3,8 @@
 // (fno_block.hip).  Not part of the ABI.
 #pragma once
 
+#include <initializer_list>
+
 #include "fno_spectral_conv.h"
 
 namespace fno {
@@ -17,6 +19,14 @@ fno_status fwd_impl(const fno_conv_desc* d, const void* x, const fno_weights* w,
 // Records a HIP failure as the thread's last error (fno_last_error) and
 // returns FNO_ERR_HIP.
 fno_status report_hip_error(hipError_t e, const char* what);
+
+// Whether two of these pointers, null ones aside, are the same.
+inline bool any_twice(std::initializer_list<const void*> p) {
+  for (auto a = p.begin(); a != p.end(); ++a)
+    for (auto b = a + 1; *a && b != p.end(); ++b)
+      if (*a == *b) return true;
+  return false;
+}
 
 // Runs launch(ctx) bracketed by profiling events (fno_profile_enable) under
 // the kernel name `name`.

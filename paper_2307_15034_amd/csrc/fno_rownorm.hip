@@ -276,6 +276,9 @@ extern "C" fno_status fno_residual_norm_bwd(const fno_residual_norm_desc* d,
     if (ws_len < (size_t)ws_bytes(*d, L.p)) return FNO_ERR_WORKSPACE_TOO_SMALL;
     if (!ok16(ws)) return FNO_ERR_INVALID_ARGUMENT;
   }
+  if (any_twice({g_x, g_u, grads->post_w, grads->post_b, grads->gate, grads->scale, grads->pre_w,
+                 grads->pre_b}))
+    return FNO_ERR_INVALID_ARGUMENT;
   a.part = static_cast<float*>(ws);
   a.g_gate = row_gate ? grads->gate : nullptr;
   a.x = x;

@@ -302,6 +302,9 @@ class Fp8Linear:
         agw = _addr(gw, (self.c_out, self.c_in), torch.float32, "gw", dev)
         bias = bias or gb is not None
         agb = _addr(gb, (self.c_out,), torch.float32, "gb", dev)
+        given = [a for a in (agx, agw, agb) if a]
+        if len(set(given)) < len(given):
+            raise ValueError("gx, gw and gb: one buffer is given twice")
         s = _stream_of(dev, stream)
         if need_x and gx is None:
             _given(stream, "gx")

@@ -1,5 +1,6 @@
 """Checks of the wrappers of the operators over channels, and the scratch memory that
 they keep (no GPU needed: the memory is the CPU's, and streams are numbers)."""
+import itertools
 import types
 import weakref
 
@@ -32,3 +33,25 @@ def test_a_gate_in_the_place_of_another_parameter_is_refused():
         p = {**dict.fromkeys(op.PARAMS), "gate": one, k: one}
         with pytest.raises(ValueError, match=k):
             op._params(tuple(p.values()), False)  # (layout checks alone: no GPU)
+
+
+def test_a_buffer_for_two_results_is_refused():
+    """Refused before any device call, whichever two they are."""
+    B = L.B
+    at = 1 << 20  # aligned addresses that are never reached
+    d = B.make_residual_norm_desc(96, 64, 4)
+    names = ("g_x", "g_u") + L.ResidualNorm.PARAMS
+    params = B.FnoResidualNormParams(gate=at)
+    for a, b in itertools.combinations(names, 2):
+        to = {k: (i + 2) * at for i, k in enumerate(names)}
+        to[b] = to[a]
+        grads = B.FnoResidualNormParams(**{k: v for k, v in to.items() if k not in ("g_x", "g_u")})
+        assert B.fno_residual_norm_bwd(d, params, at, at, at, at, at, to["g_x"], to["g_u"], grads, at, 1 << 40,
+                                       0, check=False) == B.FNO_ERR_INVALID_ARGUMENT, (a, b)
+    d = B.make_fp8_quantize_desc(96, 64)
+    names = ("codes", "scale", "codes_t", "scale_t", "col_sums")
+    for a, b in itertools.combinations(names, 2):
+        to = {k: (i + 2) * at for i, k in enumerate(names)}
+        to[b] = to[a]
+        assert B.fno_fp8_quantize(d, at, ws=at, ws_bytes=1 << 40, stream=0, check=False,
+                                  **to) == B.FNO_ERR_INVALID_ARGUMENT, (a, b)

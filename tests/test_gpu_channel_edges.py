@@ -8,7 +8,8 @@ pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
 
 from tests.gpu_util import say  # noqa: E402
-from paper_2307_15034_amd.fp8 import Fp8Quantize  # noqa: E402
+from paper_2307_15034_amd import binding as B  # noqa: E402
+from paper_2307_15034_amd.fp8 import Fp8Linear, Fp8Quantize  # noqa: E402
 from paper_2307_15034_amd.layer import ResidualNorm  # noqa: E402
 
 
@@ -85,3 +86,23 @@ def test_codes_of_the_tallest_and_widest_matrices(rows, cols):
         assert bool(((sums.double() - want).abs() <= 16 * 2.0 ** -24 * size + 2.0 ** -24 * want.abs()).all())
     only, _, _ = op.run(x)
     _same_codes("rows alone", only, q)
+
+
+def test_a_buffer_for_two_gradients_is_refused():
+    op = Fp8Linear(48, 32, 48, torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    x, w, gy = r(48, 32), r(48, 32), r(48, 48)
+    p = op.pack(w)
+    _, kept = op.fwd(x, p)
+    want = op.bwd(gy, p, kept)
+    both = torch.zeros(48, 32, device="cuda")
+    with pytest.raises(ValueError, match="twice"):
+        op.bwd(gy, p, kept, gx=both, gw=both)
+    assert not bool(both.any())
+    assert all(torch.equal(a, b) for a, b in zip(op.bwd(gy, p, kept, gx=both), want))
+    norm = ResidualNorm(48, 32, torch.float32)
+    one = torch.zeros(32, device="cuda")
+    with pytest.raises(B.FnoError):
+        norm.bwd(x, x, x=x, u=x, y=x, post_w=r(32), pre_w=r(32), out={"g_post_w": one, "g_pre_w": one})
+    assert not bool(one.any())
