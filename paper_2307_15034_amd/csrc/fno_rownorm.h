@@ -18,12 +18,14 @@ struct RowNormArgs {
   void *y, *h, *g_x, *g_u;
   const float *post_w, *post_b, *scale, *pre_w, *pre_b;
   const void* gate;
-  void* g_gate;         // one gate per row: written by the rows' own threads
+  void* g_gate;         // with `by_run`: written by the gate row's own team
   float* part;          // [units][sums][C]
   int64_t rows;
-  int64_t per_gate;     // rows that a row of the gate serves
-  int64_t span;         // rows that units share: per_gate, or all with one gate per row
+  int64_t span;         // rows that units share: those of a gate row, or all with `by_run`
   int64_t per_unit, units_per_gate;  // of a span
+  int64_t runs_per_unit;             // gate rows of a unit, with `by_run`
+  int run;              // rows in sequence that a team takes: a gate row's with `by_run`, else 1
+  int by_run;           // a team takes whole gate rows, of which a unit has many
   int C, nvec;
   int layer;            // FNO_ROW_NORM_LAYER
   int gate_f32;         // the gate is fp32 (else of the rows' type)
@@ -353,14 +355,35 @@ struct Param {
   }
 };
 
-// The rows of a unit: a piece of one span.
+// The rows of a unit, a piece of one span, as the team of one of SLOTS slots goes
+// through them: a run of rows, then the run SLOTS runs on.
+template <int SLOTS>
 struct UnitRows {
-  int64_t span, first, end;
-  __device__ __forceinline__ explicit UnitRows(const RowNormArgs& a) {
+  int64_t span, end;
+  int64_t row, gate;  // (gate: with `by_run`)
+  int left;           // rows of the run from this one on, the same for all teams
+  __device__ __forceinline__ UnitRows(const RowNormArgs& a, int slot) {
     span = (int64_t)blockIdx.x / a.units_per_gate;
-    first = span * a.span + ((int64_t)blockIdx.x - span * a.units_per_gate) * a.per_unit;
+    const int64_t first = span * a.span + ((int64_t)blockIdx.x - span * a.units_per_gate) * a.per_unit;
     const int64_t last = (span + 1) * a.span;
     end = first + a.per_unit < last ? first + a.per_unit : last;
+    row = first + (int64_t)slot * a.run;
+    gate = (int64_t)blockIdx.x * a.runs_per_unit + slot;
+    left = a.run;
+  }
+  __device__ __forceinline__ bool starts(const RowNormArgs& a) const { return left == a.run; }
+  __device__ __forceinline__ bool ends() const { return left == 1; }
+  __device__ __forceinline__ int64_t next(const RowNormArgs& a) const {
+    return row + (left > 1 ? 1 : (int64_t)(SLOTS - 1) * a.run + 1);
+  }
+  __device__ __forceinline__ void advance(const RowNormArgs& a) {
+    row = next(a);
+    if (left > 1) {
+      --left;
+    } else {
+      left = a.run;
+      gate += SLOTS;
+    }
   }
 };
 

@@ -107,6 +107,22 @@ void team_of(int nvec, int* team, int* vecs) {
   }
 }
 
+constexpr int64_t kChain = 128;
+
+// Whether teams take whole gate rows, many to a unit, instead of units a gate row
+// (or a part of it) each.  Backward: units of their own each leave a row of partial
+// sums, which past the data cost more than a gate row's rows one behind the other
+// (about 1.5 us each).  Gates of 2, 8, 32 and 128 rows meet there at about 4096
+// values of the gate for each of its rows: 64 channels, 8192 gates of 32 rows 263 us
+// so, 52 by whole gate rows (data 49), 1024 gates 41 and 45; 4096 channels, 1024
+// gates of 8 rows 1619 and 104.  Forward: nothing is summed, only teams without a
+// row are lost (64 channels, 32 teams: 32768 gates of 8 rows 82 and 25 us).
+bool by_run(const fno_residual_norm_desc& d, int64_t per_gate, int64_t slots, bool bwd) {
+  if (!d.gate_rows || per_gate == 1) return d.gate_rows != 0;
+  return per_gate <= kChain && d.gate_rows * d.channels >= 4096 * per_gate &&
+         (bwd || per_gate * 4 <= slots);
+}
+
 RowPlan plan_of(const fno_residual_norm_desc& d, bool bwd) {
   RowPlan p{};
   RowNormArgs& a = p.a;
@@ -122,19 +138,21 @@ RowPlan plan_of(const fno_residual_norm_desc& d, bool bwd) {
   a.shrink = 1.0f / (float)(1 << e);
   a.per_channel = (float)((double)(1 << e) / a.C);
   a.inv_c = (float)(1.0 / a.C);
-  a.per_gate = d.gate_rows ? d.rows / d.gate_rows : d.rows;
+  const int64_t per_gate = d.gate_rows ? d.rows / d.gate_rows : d.rows;
   team_of(a.nvec, &p.team, &p.vecs);
-  // A unit is rows of one gate row's share, in the backward at most 128 for a
-  // thread (its chain of additions); one gate per row needs no sums by gate row,
-  // so its units take any rows.
   const int64_t slots = row_threads(p.team) / p.team;
-  a.span = a.per_gate == 1 ? d.rows : a.per_gate;
-  const int64_t span = a.span, spans = d.rows / span;
   const int64_t fill = p.team <= 64 ? (bwd ? 1024 : 2048) : 131072 / p.team * (bwd ? 1 : 2);
-  a.units_per_gate = std::max(std::min(cdiv(fill, spans), cdiv(span, slots)),
-                              bwd ? cdiv(span, 128 * slots) : 1);
-  a.per_unit = cdiv(span, a.units_per_gate);
-  a.units_per_gate = cdiv(span, a.per_unit);
+  // A unit is rows of one gate row's share, in the backward at most kChain for a
+  // thread (its chain of additions).
+  a.by_run = by_run(d, per_gate, slots, bwd);
+  a.run = a.by_run ? (int)per_gate : 1;
+  const int64_t runs = a.by_run ? d.gate_rows : per_gate, spans = d.rows / a.run / runs;
+  a.units_per_gate = std::max(std::min(cdiv(fill, spans), cdiv(runs, slots)),
+                              bwd ? cdiv(runs, kChain / a.run * slots) : 1);
+  a.runs_per_unit = cdiv(runs, a.units_per_gate);
+  a.units_per_gate = cdiv(runs, a.runs_per_unit);
+  a.span = runs * a.run;
+  a.per_unit = a.runs_per_unit * a.run;
   p.units = a.units_per_gate * spans;
   return p;
 }
@@ -142,6 +160,9 @@ RowPlan plan_of(const fno_residual_norm_desc& d, bool bwd) {
 constexpr int64_t kMaxGrid = (int64_t)1 << 20;
 // Work-groups of a launch: their threads (up to 1024) stay below 2^32.
 constexpr int64_t kMaxUnits = ((int64_t)1 << 22) - 1;
+bool too_many(const fno_residual_norm_desc& d, const RowPlan& p) {
+  return p.units > kMaxUnits || (d.gate_rows > kMaxUnits && d.gate_rows != d.rows);
+}
 
 fno_status set_params(RowNormArgs* a, const fno_residual_norm_desc& d,
                       const fno_residual_norm_params* q, bool post, bool pre) {
@@ -194,9 +215,9 @@ hipError_t launch_bwd(void* ctx) {
   return hipGetLastError();
 }
 
-// Bytes of the backward's partial sums; negative where they are too many.
+// Bytes of the backward's partial sums.
 int64_t ws_bytes(const fno_residual_norm_desc& d, const RowPlan& p) {
-  const int64_t sums = RS_COUNT - (d.gate_rows == 0 || d.gate_rows == d.rows ? 1 : 0);
+  const int64_t sums = RS_COUNT - (d.gate_rows == 0 || p.a.by_run ? 1 : 0);
   return std::max<int64_t>(256, cdiv(p.units * sums * p.a.C * 4, 256) * 256);
 }
 
@@ -211,7 +232,7 @@ extern "C" fno_status fno_residual_norm_workspace_size(const fno_residual_norm_d
   if (st != FNO_OK) return st;
   if (!bytes) return FNO_ERR_INVALID_ARGUMENT;
   const RowPlan p = plan_of(*d, true);
-  if (p.units > kMaxUnits) return FNO_ERR_UNSUPPORTED;
+  if (too_many(*d, p)) return FNO_ERR_UNSUPPORTED;
   *bytes = (size_t)ws_bytes(*d, p);
   return FNO_OK;
 }
@@ -226,7 +247,7 @@ extern "C" fno_status fno_residual_norm_fwd(const fno_residual_norm_desc* d,
   RowLaunch L{plan_of(*d, false), d->dtype, u != nullptr, h != nullptr, {}, stream};
   st = set_params(&L.p.a, *d, params, L.post, L.pre);
   if (st != FNO_OK) return st;
-  if (L.p.units > kMaxUnits) return FNO_ERR_UNSUPPORTED;
+  if (too_many(*d, L.p)) return FNO_ERR_UNSUPPORTED;
   L.p.a.x = x;
   L.p.a.u = u;
   L.p.a.y = y;
@@ -260,8 +281,8 @@ extern "C" fno_status fno_residual_norm_bwd(const fno_residual_norm_desc* d,
   RowLaunch L{plan_of(*d, true), d->dtype, post, pre, {}, stream};
   st = set_params(&L.p.a, *d, params, post, pre);
   if (st != FNO_OK) return st;
-  if (L.p.units > kMaxUnits) return FNO_ERR_UNSUPPORTED;
-  const bool row_gate = d->gate_rows == d->rows;
+  if (too_many(*d, L.p)) return FNO_ERR_UNSUPPORTED;
+  const bool row_gate = L.p.a.by_run;
   RowNormArgs& a = L.p.a;
   void* const out[RS_COUNT] = {grads->post_w, grads->post_b, row_gate ? nullptr : grads->gate,
                                grads->scale, grads->pre_w, grads->pre_b};

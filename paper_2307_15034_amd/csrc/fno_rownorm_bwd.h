@@ -91,9 +91,9 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
 #pragma unroll
       for (int j = 0; j < V; ++j) sums[q][i][j] = 0.0f;
   Team<TEAM> team;
-  const UnitRows unit(a);
+  UnitRows<SLOTS> at_row(a, (int)threadIdx.x / TEAM);
   float gate[VPT][V];
-  if (POST && a.per_gate > 1) load_gate<T, VPT, MODE>(gate, a, unit.span, at.vec, at.valid);
+  if (POST && !a.by_run) load_gate<T, VPT, MODE>(gate, a, at_row.span, at.vec, at.valid);
   const bool with_x = POST && a.slot[RS_SCALE] >= 0;
   RawRow<T, VPT, MODE> ru, ry, rh, rg, rx;
   auto fetch = [&](int64_t row) {
@@ -106,11 +106,10 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
     if (a.g_y) rg.load(a.g_y, start, at.vec, at.valid, a.C);
     if (with_x) rx.load(a.x, start, at.vec, at.valid, a.C);
   };
-  int64_t row = unit.first + threadIdx.x / TEAM;
-  if (KEPT && row < unit.end) fetch(row);
-  for (; row < unit.end; row += SLOTS) {
-    const int64_t start = row * a.C;
-    if (!KEPT) fetch(row);
+  if (KEPT && at_row.row < at_row.end) fetch(at_row.row);
+  for (; at_row.row < at_row.end; at_row.advance(a)) {
+    const int64_t start = at_row.row * a.C, next = at_row.next(a);
+    if (!KEPT) fetch(at_row.row);
     float v[K][VPT][V], G[VPT][V], t[VPT][V], xh[VPT][V], x[VPT][V];
     RowStat st[K];
     if constexpr (POST) ru.widen(v[0]);
@@ -127,7 +126,7 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
         for (int j = 0; j < V; ++j) G[i][j] = 0.0f;
     }
     if (with_x) rx.widen(x);
-    if (KEPT && row + SLOTS < unit.end) fetch(row + SLOTS);
+    if (KEPT && next < at_row.end) fetch(next);
     row_stats<K, VPT, V, TEAM>(team, v, at.valid, a, st);
     if constexpr (PRE) {
 #pragma unroll
@@ -157,7 +156,13 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
           for (int j = 0; j < V; ++j)
             sums[RS_SCALE][i][j] = __builtin_fmaf(G[i][j], x[i][j], sums[RS_SCALE][i][j]);
       }
-      if (a.per_gate == 1) load_gate<T, VPT, MODE>(gate, a, row, at.vec, at.valid);
+      if (a.by_run && at_row.starts(a)) {
+        load_gate<T, VPT, MODE>(gate, a, at_row.gate, at.vec, at.valid);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) sums[RS_GATE][i][j] = 0.0f;
+      }
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         float w[V], b[V];
@@ -166,11 +171,11 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           xh[i][j] = (v[0][i][j] - st[0].mean) * st[0].r;
-          t[i][j] = G[i][j] * __builtin_fmaf(xh[i][j], w[j], b[j]);
-          sums[RS_GATE][i][j] += t[i][j];
+          sums[RS_GATE][i][j] += G[i][j] * __builtin_fmaf(xh[i][j], w[j], b[j]);
         }
       }
-      if (a.g_gate) {
+      if (a.g_gate && at_row.ends()) {
+        const int64_t to = at_row.gate * a.C;
         if (a.gate_f32) {
 #pragma unroll
           for (int i = 0; i < VPT; ++i)
@@ -178,12 +183,12 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_bwd_kernel(RowNorm
             for (int q = 0; q < V / 4; ++q) {
               RowVec<float> r;
 #pragma unroll
-              for (int j = 0; j < 4; ++j) r.e[j] = t[i][4 * q + j];
+              for (int j = 0; j < 4; ++j) r.e[j] = sums[RS_GATE][i][4 * q + j];
               if (at.valid[i] > 4 * q)
-                store_row_vec<float, ROW_TAIL>(static_cast<float*>(a.g_gate) + start, at.vec[i] * (V / 4) + q, a.C, r);
+                store_row_vec<float, ROW_TAIL>(static_cast<float*>(a.g_gate) + to, at.vec[i] * (V / 4) + q, a.C, r);
             }
         } else {
-          store_row<T, VPT, MODE>(a.g_gate, start, at.vec, at.valid, a.C, t);
+          store_row<T, VPT, MODE>(a.g_gate, to, at.vec, at.valid, a.C, sums[RS_GATE]);
         }
       }
 #pragma unroll

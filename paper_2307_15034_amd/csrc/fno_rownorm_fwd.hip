@@ -18,25 +18,24 @@ __global__ __launch_bounds__(row_threads(TEAM)) void row_norm_fwd_kernel(RowNorm
   const Param<KEPT, VPT, V> pre_w(a.pre_w, 1.0f, at.vec, a.C), pre_b(a.pre_b, 0.0f, at.vec, a.C);
   Team<TEAM> team;
   RowStat st[1];
-  const UnitRows unit(a);
+  UnitRows<SLOTS> at_row(a, (int)threadIdx.x / TEAM);
   float gate[VPT][V];
-  if (a.u && a.per_gate > 1) load_gate<T, VPT, MODE>(gate, a, unit.span, at.vec, at.valid);
+  if (a.u && !a.by_run) load_gate<T, VPT, MODE>(gate, a, at_row.span, at.vec, at.valid);
   RawRow<T, VPT, MODE> nx, nu;
   auto fetch = [&](int64_t row) {
     nx.load(a.x, row * a.C, at.vec, at.valid, a.C);
     if (a.u) nu.load(a.u, row * a.C, at.vec, at.valid, a.C);
   };
-  int64_t row = unit.first + threadIdx.x / TEAM;
-  if (KEPT && row < unit.end) fetch(row);
-  for (; row < unit.end; row += SLOTS) {
-    const int64_t start = row * a.C;
-    if (!KEPT) fetch(row);
+  if (KEPT && at_row.row < at_row.end) fetch(at_row.row);
+  for (; at_row.row < at_row.end; at_row.advance(a)) {
+    const int64_t start = at_row.row * a.C, next = at_row.next(a);
+    if (!KEPT) fetch(at_row.row);
     float y[1][VPT][V], u[1][VPT][V];
     nx.widen(y[0]);
     if (a.u) nu.widen(u[0]);
-    if (KEPT && row + SLOTS < unit.end) fetch(row + SLOTS);
+    if (KEPT && next < at_row.end) fetch(next);
     if (a.u) {
-      if (a.per_gate == 1) load_gate<T, VPT, MODE>(gate, a, row, at.vec, at.valid);
+      if (a.by_run && at_row.starts(a)) load_gate<T, VPT, MODE>(gate, a, at_row.gate, at.vec, at.valid);
       row_stats<1, VPT, V, TEAM>(team, u, at.valid, a, st);
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {

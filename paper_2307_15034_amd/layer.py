@@ -505,7 +505,7 @@ class ResidualNorm:
     [rows, C] per row (None: 1).
 
     The backward keeps one workspace, memory of the first call's stream (and the
-    smaller ones before it, where a gate of more rows needed more), so an object's
+    smaller ones before it, where a gate's sums needed more), so an object's
     backward calls belong on one stream (or on streams that wait for each other),
     and an object outlives the graphs that hold its calls.  Where `stream` is given,
     outputs are the caller's too.

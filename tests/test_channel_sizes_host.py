@@ -28,3 +28,11 @@ def test_linear_maps_over_large_grids():
     for c_in, c_out in ((8, 32), (64, 64), (20, 80)):
         op = F.Fp8Linear(1 << 29, c_in, c_out)
         assert op.q_x.shape_t.codes == (c_in, 1 << 29)
+
+
+@pytest.mark.parametrize("rows,c,each", [(1 << 20, 64, 2), (1 << 19, 64, 32), (8192, 4096, 2), (1 << 16, 4096, 8),
+                                         (1 << 21, 64, 128), (1 << 22, 8, 2), (600000, 520, 3), (1 << 20, 64, 256)])
+def test_partial_sums_of_gates_of_a_few_rows_stay_below_the_rows(rows, c, each):
+    """The backward's workspace against one of its tensors, 16-bit."""
+    d = B.make_residual_norm_desc(rows, c, rows // each)
+    assert B.fno_residual_norm_workspace_size(d) < rows * c * 2 / 3

@@ -55,6 +55,53 @@ def test_gates_of_a_few_rows(c, each, gate_dt):
     R._check(60, c, "bf16", "rms", "exit", 60 // each, gate_dt, seed=each)
 
 
+@pytest.mark.parametrize("c,each", [(3, 2), (20, 3), (20, 5), (64, 2), (64, 8), (64, 20), (333, 3), (333, 2), (520, 5),
+                                    (520, 16), (2050, 7), (4096, 2), (4099, 3), (8192, 2), (16380, 2)])
+@pytest.mark.parametrize("dt,gate_dt", [("bf16", "fp32"), ("fp16", "fp16"), ("fp32", "fp32")])
+def test_many_gates_of_a_few_rows(c, each, dt, gate_dt):
+    """So many that teams take whole gate rows (4096 values of the gate for each of its
+    rows), and a few more, so that the last unit is not full; in place too."""
+    gates = -(-4096 * each // c) + 5
+    op, x, u, p, gy, gh, y, h, got = R._check(gates * each, c, dt, "layer", "both", gates, gate_dt, seed=each)
+    u2, gy2, x2, u3 = u.clone(), gy.clone(), x.clone(), u.clone()
+    again = op.bwd(gy2, gh, x=x, u=u2, y=y, out={"g_x": gy2, "g_u": u2}, **p)
+    assert all(torch.equal(again[k], v) for k, v in got.items())
+    op.fwd(x2, u3, y=x2, h=u3, **p)
+    assert torch.equal(x2, y) and torch.equal(u3, h)
+    R._check(gates * each, c, dt, "rms", "exit", gates, gate_dt, seed=each)
+
+
+@pytest.mark.parametrize("c,each", [(64, 128), (64, 100), (520, 127), (4096, 65)])
+def test_gates_of_up_to_128_rows_against_a_gate_a_row(c, each):
+    """The longest runs that a team takes: rows and their gradients are those of the
+    same gate given for each row, bit for bit, and the gate's gradient is the sum of
+    its rows' (chains of up to 128 fp32 additions), which end where the next begins."""
+    gates = -(-4096 * each // c) + 3
+    rows = gates * each
+    say(f"residual norm {rows}x{c}, gates of {each} rows")
+    g = torch.Generator(device="cuda").manual_seed(each)
+    row = lambda: torch.randn(rows, c, device="cuda", generator=g).half()  # noqa: E731
+    x, u, gy, gh = row(), row(), row(), row()
+    w = 1 + 0.2 * torch.randn(c, device="cuda", generator=g)
+    gate = torch.randn(gates, c, device="cuda", generator=g)
+    op = ResidualNorm(rows, c)
+    p = dict(post_w=w, scale=w, pre_w=w)
+    y, h = op.fwd(x, u, gate=gate, **p)
+    got = op.bwd(gy, gh, x=x, u=u, y=y, gate=gate, **p)
+    alone = gate.repeat_interleave(each, 0)
+    y2, h2 = op.fwd(x, u, gate=alone, **p)
+    assert torch.equal(y, y2) and torch.equal(h, h2)
+    want = op.bwd(gy, gh, x=x, u=u, y=y, gate=alone, **p)
+    assert torch.equal(got["g_x"], want["g_x"]) and torch.equal(got["g_u"], want["g_u"])
+    for a in range(0, gates, 1024):
+        terms = want["g_gate"][a * each:(a + 1024) * each].double().view(-1, each, c)
+        off = (got["g_gate"][a:a + 1024].double() - terms.sum(1)).abs()
+        assert bool((off <= each * 2.0 ** -24 * terms.abs().sum(1)).all())
+    # either order: chains of up to 128, a tree, doubles, of terms whose sizes are below 4 in the mean
+    for k in ("g_post_w", "g_scale", "g_pre_w"):
+        assert bool(((got[k] - want[k]).abs() <= 2 * RB.CHAIN * RB.E * rows * 4).all()), k
+
+
 @pytest.mark.parametrize("dt", ["fp32", "bf16"])
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("c", [40, 3000])
