@@ -572,7 +572,9 @@ fno_status fno_adamw_moments(const fno_adamw_tensor *tensors, int64_t count, fno
  * A row's sums are fp32; the parameters' are fp32 chains of at most 128
  * additions, joined in double.  Every sum has a fixed order: results are
  * bit-identical from run to run.  h is formed from y before its rounding.  A row with a
- * value that is not finite, or beyond 2^126 in size, gives NaN throughout.
+ * value that is not finite, or with LAYER a distance from its mean past fp32's
+ * largest, gives NaN throughout; rows up to that size keep fp32's precision but for
+ * two bits of 1 / sqrt(var), which is subnormal beyond 2^126.
  * ------------------------------------------------------------------------ */
 typedef enum { FNO_ROW_NORM_LAYER = 0, FNO_ROW_NORM_RMS = 1 } fno_row_norm;
 
@@ -581,7 +583,9 @@ typedef struct {
   int32_t norm;        /* fno_row_norm */
   int32_t gate_dtype;  /* FNO_DTYPE_F32 or dtype */
   float eps;           /* >= 0, finite */
-  int64_t rows;        /* 1 .. 2^40, rows x channels up to 2^42 */
+  int64_t rows;        /* 1 .. 2^40, rows x channels up to 2^42; a backward of
+                          2^29 rows and more: FNO_ERR_UNSUPPORTED where one launch
+                          does not hold it */
   int64_t channels;    /* 1 .. 16384 */
   int64_t gate_rows;   /* 0, or a divisor of rows; up to 2^22 - 1 unless it is
                           rows (FNO_ERR_UNSUPPORTED) */
@@ -655,7 +659,9 @@ typedef struct {
  * Either pair of codes and scales may be null.  With F the format's largest
  * value and a the largest size of a block's finite values, the scale is
  *     POW2   2^max(e, -126), e the least with a <= F 2^e
- *     F32    max(a (1 / F), 2^-126), both operations in fp32,
+ *     F32    max(a (1 / F), 2^-126), both operations in fp32 (a or one unit in the
+ *            last place from the quotient a / F: what torch makes, on the GPU,
+ *            of a tensor divided by a number, so that codes formed there agree),
  * 1 where a = 0; the code is v times the scale's reciprocal (an fp32 product)
  * rounded to nearest, ties to even.  NaN stays NaN; an infinity becomes NaN in
  * e4m3.  col_sums, if not null, receives the sums of v over rows (fp32 [cols],
@@ -683,8 +689,11 @@ typedef struct {
  * out_dtype.  For out_dtype F32 every product enters them exactly; for 16-bit
  * results the matrix instruction for 8-bit codes joins eight consecutive products
  * at a time, each cut towards zero to a multiple of 2^-13 of the power of two below
- * the largest of the eight.  A row of codes is read whole, fno_fp8_pitch(inner)
- * bytes: what stands behind `inner` has to be zero. */
+ * the largest of the eight.  For F32 with powers of two, values (codes times their
+ * scales) below 2^-126 count as the nearest multiple of 2^-133, past fp32's largest
+ * as infinite; with fp32 scales the product of two scales is an fp32 number.  A row
+ * of codes is read whole, fno_fp8_pitch(inner) bytes: what stands behind `inner` has
+ * to be zero. */
 fno_status fno_fp8_matmul_workspace_size(const fno_fp8_matmul_desc *desc, size_t *bytes);
 fno_status fno_fp8_matmul(const fno_fp8_matmul_desc *desc, const void *a, const void *scale_a,
                           const void *b, const void *scale_b, const void *z, const float *bias,

@@ -5,8 +5,10 @@
 // block.  That instruction joins eight neighbouring products at a time in fewer
 // bits than fp32: each is cut towards zero to a multiple of 2^-13 of the power of
 // two below the largest of the eight (measured, as for the 8-bit products of inner
-// length 32); the eights are joined in fp32.  On normally distributed codes the
-// sums are 1.5e-5 off in the 2-norm, a thirtieth of fp16's rounding of the result.
+// length 32); the eights are joined in fp32.  In the 2-norm the sums of normally
+// distributed codes are 1.5e-5 off, a fourteenth of fp16's rounding of the result
+// (with one value in a thousand twenty times as large 3.8e-5 to 4.6e-5; with values of
+// one sign, which the cut all makes smaller, 2.5e-6).
 // fp32 results, whose rounding is below that: the codes are widened to bfloat16,
 // which holds them exactly, and multiplied at half the rate by products that keep
 // fp32 throughout (8e-9 off).
@@ -274,9 +276,9 @@ __device__ __forceinline__ float scale_of(int four, int m) {
 // The tile's product.  Two stages of LDS: a block's tiles arrive while the one
 // before is multiplied; the matrix cores bound it (256 x 256, eight waves of 128 x
 // 64: their operands take 75% of LDS's rate; 128 x 128 tiles would take all of it).
-// 16384 x 4096 x 4096: 222 to 249 us with powers of two (2.2 to 2.5 PFLOP/s), 370 with fp32 scales, which the vector unit bounds
-// (eight operations for a 16 x 16 product of 32 cycles).  Wide, 4096 x 4096 x 8192:
-// 207 us (1.33 PFLOP/s).
+// 16384 x 4096 x 4096: 237 to 265 us with powers of two (2.1 to 2.3 PFLOP/s), 389 to
+// 395 with fp32 scales, which the vector unit bounds (eight operations for a 16 x 16
+// product of 32 cycles).  Wide, 4096 x 4096 x 8192: 200 to 207 us (1.3 to 1.4 PFLOP/s).
 template <int FA, int FB, bool F32S, bool WIDE, int BM, int BN, int WGM, int WGN, int STAGES = 2>
 __global__ __launch_bounds__(64 * WGM * WGN, STAGES == 1 ? 3 : 1) void gemm_kernel(MatmulArgs g) {
   constexpr int THREADS = 64 * WGM * WGN;
@@ -638,8 +640,9 @@ MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
   // the rows' bytes: more work-groups at a time); else 128 x 128.
   const bool pow2 = d.scale_type == FNO_SCALE_POW2;
   const int64_t of256 = fp8_cdiv(g.M, 256) * fp8_cdiv(g.N, 256);
-  // Few rows of B's worth: up to 64 rows, while a wave's share of the inner axis
-  // stays short (products of weights' gradients have few rows and a long one).
+  // Few rows: up to 64, while a wave's share of the inner axis stays short.  (With few
+  // columns too, as a gradient of 64 x 64 weights over up to 32768 points, that is a
+  // few work-groups: not measured against split tiles.)
   p.tile = g.M <= 64 && g.kb <= 256 && g.N < ((int64_t)1 << 26) ? FEW_ROWS
            : g.kb == 1 && g.N <= 64 && g.M > 128 ? TILE_NARROW
            : pow2 && of256 >= 192 && g.N > 128 ? TILE_256

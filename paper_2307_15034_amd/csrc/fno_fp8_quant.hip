@@ -84,9 +84,9 @@ __device__ __forceinline__ float act32_of(float z, int act) {
 // The 8 x 8 values of a thread.  16-bit values without an activation stay in
 // pairs: sizes are compared as whole numbers, two at a time, and with powers of
 // two the conversion takes pairs and divides them itself (exactly).  Three
-// operations a value for both directions, where single floats take thirteen,
-// which the passes were bound by (33.5 M values both ways 41 us, 32 so; 67 M
-// weights 61 and 48, 5.6 TB/s).
+// operations a value for both directions, where single floats take thirteen
+// (33.5 M values both ways 27 us, with fp32 scales, so as single floats, 30; 67 M
+// 48 and 55; from the memory-side cache.  67 M weights from memory 50, 5.4 TB/s).
 template <typename T, int FMT, bool ACT, bool POW2>
 struct Values {
   static constexpr bool PAIRS = sizeof(T) == 2 && !ACT && POW2;

@@ -4,8 +4,8 @@
 // Both rows' statistics are formed again from the rows, which a team of threads
 // holds whole; the parameters' sums stay in registers over a unit's rows and
 // leave as one partial row a unit.  Bound by memory, as long as the next row is on
-// its way while one is worked on: 32 x 128^2 rows of 64, fp16, seven tensors, 97 us
-// (4.9 TB/s), 8192 rows of 4096, bf16, six tensors, 89 (4.5); without the row ahead,
+// its way while one is worked on: 32 x 128^2 rows of 64, fp16, seven tensors, 103 us
+// (4.6 TB/s), 8192 rows of 4096, bf16, six tensors, 98 (4.1); without the row ahead,
 // its loads in branches, 163 and 180.
 #pragma once
 

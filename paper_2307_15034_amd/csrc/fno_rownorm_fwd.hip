@@ -1,7 +1,7 @@
 // Residual norm, forward: y = scale x + gate (post_w norm(u) + post_b) and h =
 // pre_w norm(y) + pre_b, a row held by a team of threads from its loads to its
 // stores, the next row's loads under way.  Bound by memory: 32 x 128^2 rows of 64,
-// fp16, four tensors, 45 us (6.0 TB/s; 72 with a division for each row's gate and no
+// fp16, four tensors, 46 us (5.8 TB/s; 72 with a division for each row's gate and no
 // row ahead).
 #include "fno_rownorm.h"
 

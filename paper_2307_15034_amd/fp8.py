@@ -95,8 +95,7 @@ class Fp8Quantize:
 
     A block's scale is the least power of two (`pow2_scales`) that brings its
     largest size within the format's, or that size times the fp32 reciprocal of the
-    format's.
-    Blocks are 128 columns of a row, and 128 rows of a column for the transpose;
+    format's.  Blocks are 128 columns of a row, and 128 rows of a column for the transpose;
     with `tile`, 128 x 128 for both.
 
     An object keeps one workspace, memory of the first call's stream, so its
@@ -242,7 +241,9 @@ class Fp8Linear:
         return places
 
     def pack(self, w, out: Optional[Fp8Weights] = None, stream: Optional[int] = None) -> Fp8Weights:
-        """The weights' codes, both ways, from w [c_out, c_in] of `dtype`."""
+        """The weights' codes, both ways, from w [c_out, c_in] of `dtype`.  (fp32 weights
+        beside 16-bit rows need not be rounded to those first: Fp8Quantize(c_out, c_in,
+        torch.float32, tile=True) forms the same codes from them.)"""
         if out is not None and (out.codes_t is None or out.scale_t is None):
             raise ValueError("out: codes_t and scale_t are written too")
         q, t, _ = self.q_w.run(w, transpose=True, out=None if out is None else Fp8Codes(*out[:2]),

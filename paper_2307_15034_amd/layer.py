@@ -321,6 +321,7 @@ def _stream_of(device: torch.device, stream: Optional[int]) -> int:
     """The stream a call runs on: `stream`, or torch's current one on
     `device`, which has to be the current device (the library launches
     there)."""
+    # (the calls behind torch.cuda's, without the objects that those make)
     current = torch._C._cuda_getDevice()
     if device.index != current:
         raise ValueError(f"the current device is cuda:{current}, the tensors live on {device}")

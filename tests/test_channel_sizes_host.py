@@ -36,3 +36,13 @@ def test_partial_sums_of_gates_of_a_few_rows_stay_below_the_rows(rows, c, each):
     """The backward's workspace against one of its tensors, 16-bit."""
     d = B.make_residual_norm_desc(rows, c, rows // each)
     assert B.fno_residual_norm_workspace_size(d) < rows * c * 2 / 3
+
+
+def test_backwards_of_the_residual_norm_that_one_launch_does_not_hold():
+    size = lambda rows, c: B.fno_residual_norm_workspace_size(B.make_residual_norm_desc(rows, c))  # noqa: E731
+    for rows, c in (((1 << 29) - 128, 4096), ((1 << 29) - 128, 8192), ((1 << 34), 1)):
+        assert size(rows, c) > 0
+    for rows, c in ((1 << 36, 1), (1 << 29, 8192)):
+        with pytest.raises(B.FnoError) as e:
+            size(rows, c)
+        assert e.value.status == B.FNO_ERR_UNSUPPORTED

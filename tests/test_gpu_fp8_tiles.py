@@ -67,3 +67,27 @@ def test_scales_and_codes_that_are_not_a_number_in_every_tile(m, n, dt):
     bad[m - 2] = True
     bad[:, [n - 1, n - 3]] = True
     assert bool(got[bad].isnan().all()) and torch.equal(got[~bad], out[~bad])
+
+
+@pytest.mark.parametrize("m,n", [(8, 20), (200, 150), (300, 40), (4096, 3100)])
+def test_scales_at_the_ends_of_their_range(m, n):
+    """Products of a small value and a large one.  16-bit results: every pair of
+    scales.  fp32 results: values (code times scale) of 2^-126 to fp32's largest."""
+    k = 100
+    e8 = lambda v, r: torch.full((1, r), v, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)  # noqa: E731
+    for dt in ("fp32", "bf16"):
+        op = F.Fp8Matmul(m, n, k, F.DT[dt])
+        for byte_a, byte_b in ((1, 253), (0, 254), (254, 0), (3, 250), (246, 8), (120, 134), (60, 70)):
+            for code, value in ((0x38, 1.0), (0x01, 2.0 ** -9), (0x7E, 448.0)):
+                size = value * 2.0 ** (byte_a - 127)
+                if dt == "fp32" and not 2.0 ** -126 <= size < 2.0 ** 128:
+                    continue
+                if dt == "fp32" and 2.0 ** (byte_b - 127) < 2.0 ** -126:
+                    continue
+                a = torch.zeros(m, 112, dtype=torch.uint8, device="cuda")
+                b = torch.zeros(n, 112, dtype=torch.uint8, device="cuda")
+                a[:, 5], b[:, 5] = code, 0x38
+                f = lambda c, s: Fp8Codes(c.view(torch.float8_e4m3fn), s)  # noqa: E731
+                got = op.run(f(a, e8(byte_a, m)), f(b, e8(byte_b, n)))
+                want = torch.tensor(size * 2.0 ** (byte_b - 127), dtype=torch.float64).to(F.DT[dt])
+                assert bool((got == want.cuda()).all()), (dt, byte_a, byte_b, code)
