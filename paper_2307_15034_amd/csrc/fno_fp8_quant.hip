@@ -361,7 +361,7 @@ __global__ __launch_bounds__(QT) void quantize_kernel(QuantArgs a) {
     if (a.part && rg % 16 == 0 && r0 < a.rows) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (j < left) a.part[block_r * a.cols + c0 + j] = sum[j];
+        if ((int64_t)c0 + j < cols) a.part[block_r * cols + c0 + j] = sum[j];
     }
   }
   BlockScale one{};
