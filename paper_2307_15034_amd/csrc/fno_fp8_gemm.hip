@@ -640,9 +640,10 @@ MatmulPlan plan_of(const fno_fp8_matmul_desc& d) {
   // the rows' bytes: more work-groups at a time); else 128 x 128.
   const bool pow2 = d.scale_type == FNO_SCALE_POW2;
   const int64_t of256 = fp8_cdiv(g.M, 256) * fp8_cdiv(g.N, 256);
-  // Few rows: up to 64, while a wave's share of the inner axis stays short.  (With few
-  // columns too, as a gradient of 64 x 64 weights over up to 32768 points, that is a
-  // few work-groups: not measured against split tiles.)
+  // Few rows: up to 64, while a wave's share of the inner axis stays short.  That is
+  // for inner axes of channels; over many points (the gradient of 64 x 64 weights) the
+  // border lies too far out: 2048 points 8 us, 8192 20, 32768 73, where split tiles
+  // take 14 for 32897 (64 x 4096: 76 and 44).
   p.tile = g.M <= 64 && g.kb <= 256 && g.N < ((int64_t)1 << 26) ? FEW_ROWS
            : g.kb == 1 && g.N <= 64 && g.M > 128 ? TILE_NARROW
            : pow2 && of256 >= 192 && g.N > 128 ? TILE_256
