@@ -659,9 +659,9 @@ typedef struct {
  * Either pair of codes and scales may be null.  With F the format's largest
  * value and a the largest size of a block's finite values, the scale is
  *     POW2   2^max(e, -126), e the least with a <= F 2^e
- *     F32    max(a (1 / F), 2^-126), both operations in fp32 (a or one unit in the
- *            last place from the quotient a / F: what torch makes, on the GPU,
- *            of a tensor divided by a number, so that codes formed there agree),
+ *     F32    max(a (1 / F), 2^-126), both operations in fp32 (at most one unit in
+ *            the last place from the rounded quotient: what torch makes, on the
+ *            GPU, of a tensor divided by a number, so that codes formed so agree),
  * 1 where a = 0; the code is v times the scale's reciprocal (an fp32 product)
  * rounded to nearest, ties to even.  NaN stays NaN; an infinity becomes NaN in
  * e4m3.  col_sums, if not null, receives the sums of v over rows (fp32 [cols],
